@@ -292,6 +292,72 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal,
                       const void* qkv, const void* o, const float* lse, const void* d_o,
                       void* dqkv, float* d_scratch, void* ws, size_t ws_bytes, void* hip_stream);
 
+/* ---- what a decoder trained on packed documents has on either side of the layer ----------------------------------------
+ * Rotary positions.  Rows of qkv are (q | k | v, head, dh) with nq query heads and nkv key and value heads on this rank
+ * (nq = nkv = nl: the layer's own qkv).  The first `rot` columns (even, at most dh) of every q and k head are turned; pair i is
+ * columns (i, i + rot / 2) with TPL_ROPE_HALF, (2 i, 2 i + 1) with TPL_ROPE_ADJACENT:
+ *   a = position * freq[i];   (x, y) -> factor * (x cos a - y sin a, x sin a + y cos a)
+ * backward: the transpose of that, (x, y) -> factor * (x cos a + y sin a, y cos a - x sin a).  The other columns and v are copied.
+ * freq: double [rot / 2] in device memory, radians per position.  positions: int32 [M] (16-byte aligned; the front of a pack plan is such
+ * an array), or NULL: row m has position m % seq (seq > 0; not looked at where there are positions).  Any int32 is a position; the angle is
+ * worked out in 64 bits.  qkv and out are [M, (nq + 2 nkv) dh], whole 16-byte rows; out may be qkv itself (then only what is turned is
+ * touched), but may not overlap it otherwise.
+ * tp_layer_rope_frequencies fills freq and factor in HOST memory: base^(-2 i / rot), for a context stretched `stretch` times
+ *   TPL_ROPE_LINEAR  every frequency divided by stretch
+ *   TPL_ROPE_BASE    base * stretch^(rot / (rot - 2)), which leaves pair 0 as it is and divides the last one
+ *   TPL_ROPE_PARTS   pairs that turn 32 times or more over `context` positions as they are, once or less divided by stretch, a linear
+ *                    ramp between, and factor = 0.1 ln(stretch) + 1 (Peng et al. 2023, arXiv 2309.00071); otherwise factor = 1. */
+enum { TPL_ROPE_HALF = 0, TPL_ROPE_ADJACENT = 1 };
+enum { TPL_ROPE_PLAIN = 0, TPL_ROPE_LINEAR = 1, TPL_ROPE_BASE = 2, TPL_ROPE_PARTS = 3 };
+int tp_layer_rope_frequencies(int rot, double base, int scaling, double stretch, double context, double* freq, float* factor);
+int tp_layer_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor,
+                      const int32_t* positions, int64_t seq, const void* qkv, void* out, void* hip_stream);
+int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor,
+                      const int32_t* positions, int64_t seq, const void* dqkv, void* out, void* hip_stream);
+
+/* Attention of packed sequences with grouped heads.  Sequence b is rows offsets[b] .. offsets[b + 1] - 1 of the [M, ...] tensors
+ * (lengths from 0 on); query head h reads key and value head h / (nq / nkv); causal: query i of a sequence sees its keys j <= i, otherwise
+ * all of its sequence, never another.
+ *   qkv [M, (nq + 2 nkv) dh] -> o [M, nq dh], lse [M, nq] float (natural log of the sum of exp(q . k / sqrt(dh)))
+ * Rows that belong to no sequence (behind the last one) are neither read nor written; their d_scratch may be.  A masked value is as if it
+ * were not there, infinities and NaN among them.  dh: a multiple of 8 up to 128; at most 128 query heads to a key head.
+ *
+ * The plan: tp_layer_pack_plan_bytes() of device memory that tp_layer_pack_plan fills on the stream from offsets (int32
+ * [sequences + 1], device memory, offsets[0] = 0, not decreasing, the last at most M), once for a batch; every layer's calls with the same
+ * (sequences, M, nq, nkv, causal) read it.  It begins with the position of every row in its sequence, int32 [M] (0 behind the last one),
+ * which the rotary entry points take.  Offsets are on the device, so they cannot be refused: a decreasing one is taken as the largest
+ * before it, and they end at 0 and M.  A call with another plan than its own (tokens, heads or mask differ) writes nothing.
+ * tp_layer_pack_plan may be captured into a graph, which then follows the offsets that its replays find.
+ * ws: at least tp_layer_attn_packed_workspace_bytes(..., bwd); d_scratch: [M, nq] float.  Results are deterministic. */
+size_t tp_layer_pack_plan_bytes(int64_t sequences, int64_t M, int nq, int nkv);
+int tp_layer_pack_plan(int64_t sequences, int64_t M, const int32_t* offsets, int nq, int nkv, int causal, void* plan, size_t plan_bytes,
+                       void* hip_stream);
+size_t tp_layer_attn_packed_workspace_bytes(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, int bwd);
+int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan,
+                             const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan,
+                             const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, float* d_scratch,
+                             void* ws, size_t ws_bytes, void* hip_stream);
+
+/* Softmax cross entropy over a vocabulary split over the ranks, without keeping the logits z = x w^T.  x [M, H] is replicated, w [V, H]
+ * (dtype, a row per token of the vocabulary) holds rows first .. first + V - 1 of the whole one; labels int32 [M], numbers in the whole
+ * vocabulary; a label outside [0, vocab) is ignored (loss 0, no gradient).
+ *   1. tp_layer_lm_loss_fwd : stats[m] = (log sum_v exp z[m, v] over the shard, z[m, label] or -inf where another rank holds it)
+ *      (the caller all-gathers `stats`: two floats per token)
+ *   2. tp_layer_lm_loss_join: from stats [ranks][M][2]: lse[m] over the whole vocabulary, loss[m] = lse[m] - z[m, label]
+ *   3. tp_layer_lm_loss_bwd : dz = (exp(z - lse) - onehot(label)) * dloss[m], worked out again piece by piece;
+ *      dx_partial [M, H] = dz w, which the ranks would all-reduce; dw [V, H] = dz^T x
+ * (x of an ignored token is multiplied by zero in dw: it has to be finite).  stats, loss, lse, dloss: float, natural logarithms.
+ * H whole 16-byte rows; V and M any number; x below 2 GiB.  ws_bytes >= tp_layer_lm_loss_workspace_bytes(..., bwd). */
+size_t tp_layer_lm_loss_workspace_bytes(int dtype, int64_t M, int64_t H, int64_t V, int bwd);
+int tp_layer_lm_loss_fwd(int dtype, int64_t M, int64_t H, int64_t V, int64_t first, const void* x, const void* w, const int32_t* labels,
+                         float* stats, void* ws, size_t ws_bytes, void* hip_stream);
+int tp_layer_lm_loss_join(int64_t M, int64_t ranks, int64_t vocab, const float* stats, const int32_t* labels, float* loss, float* lse,
+                          void* hip_stream);
+int tp_layer_lm_loss_bwd(int dtype, int64_t M, int64_t H, int64_t V, int64_t first, int64_t vocab, const void* x, const void* w,
+                         const int32_t* labels, const float* lse, const float* dloss, void* dx_partial, void* dw, void* ws,
+                         size_t ws_bytes, void* hip_stream);
+
 /* Diagnostics for benchmarks (not thread-safe, off by default).  tp_layer_profile(1) makes every
  * GEMM launch of this library (inside tp_layer_fwd / tp_layer_bwd / tp_layer_gemm) be bracketed by
  * two HIP events on its launch stream and restarts the record; tp_layer_profile(0) stops.  A launch

@@ -18,6 +18,11 @@ from .binding import (  # noqa: F401
     tp_layer_ln_apply_workspace_bytes, tp_layer_ln_apply_bwd,
     tp_layer_slice_epilogue_fwd, tp_layer_slice_epilogue_workspace_bytes, tp_layer_slice_epilogue_bwd,
     TPL_ACT_NONE, TPL_ACT_GELU, tp_layer_static_scratch_bytes, tp_layer_slice_epilogue_bwd_static,
+    TPL_ROPE_HALF, TPL_ROPE_ADJACENT, TPL_ROPE_PLAIN, TPL_ROPE_LINEAR, TPL_ROPE_BASE, TPL_ROPE_PARTS,
+    tp_layer_rope_frequencies, tp_layer_rope_fwd, tp_layer_rope_bwd,
+    tp_layer_pack_plan_bytes, tp_layer_pack_plan,
+    tp_layer_attn_packed_workspace_bytes, tp_layer_attn_packed_fwd, tp_layer_attn_packed_bwd,
+    tp_layer_lm_loss_workspace_bytes, tp_layer_lm_loss_fwd, tp_layer_lm_loss_join, tp_layer_lm_loss_bwd,
 )
 
 

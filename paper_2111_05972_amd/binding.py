@@ -14,6 +14,8 @@ TPL_F32, TPL_BF16 = 0, 1
 TPL_CAUSAL, TPL_ROW_EPILOGUE, TPL_SIDE_STREAM = 1, 2, 4
 TPL_EPI_NONE, TPL_EPI_GELU, TPL_EPI_DGELU = 0, 1, 2
 TPL_ACT_NONE, TPL_ACT_GELU = 0, 1
+TPL_ROPE_HALF, TPL_ROPE_ADJACENT = 0, 1
+TPL_ROPE_PLAIN, TPL_ROPE_LINEAR, TPL_ROPE_BASE, TPL_ROPE_PARTS = range(4)
 
 _vp = ctypes.c_void_p
 
@@ -98,6 +100,18 @@ def load_library():
         "tp_layer_slice_epilogue_bwd": (ci, [ci, ci, i64, i64, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
         "tp_layer_static_scratch_bytes": (sz, []),
         "tp_layer_slice_epilogue_bwd_static": (ci, [ci, ci, i64, i64, _vp, _vp, _vp, _vp, _vp]),
+        "tp_layer_rope_frequencies": (ci, [ci, ctypes.c_double, ci, ctypes.c_double, ctypes.c_double, _vp, _vp]),
+        "tp_layer_rope_fwd": (ci, [ci, i64, ci, ci, ci, ci, ci, _vp, ctypes.c_float, _vp, i64, _vp, _vp, _vp]),
+        "tp_layer_rope_bwd": (ci, [ci, i64, ci, ci, ci, ci, ci, _vp, ctypes.c_float, _vp, i64, _vp, _vp, _vp]),
+        "tp_layer_pack_plan_bytes": (sz, [i64, i64, ci, ci]),
+        "tp_layer_pack_plan": (ci, [i64, i64, _vp, ci, ci, ci, _vp, sz, _vp]),
+        "tp_layer_attn_packed_workspace_bytes": (sz, [ci, i64, i64, ci, ci, ci, ci, ci]),
+        "tp_layer_attn_packed_fwd": (ci, [ci, i64, i64, ci, ci, ci, ci, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
+        "tp_layer_attn_packed_bwd": (ci, [ci, i64, i64, ci, ci, ci, ci, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
+        "tp_layer_lm_loss_workspace_bytes": (sz, [ci, i64, i64, i64, ci]),
+        "tp_layer_lm_loss_fwd": (ci, [ci, i64, i64, i64, i64, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
+        "tp_layer_lm_loss_join": (ci, [i64, i64, i64, _vp, _vp, _vp, _vp, _vp]),
+        "tp_layer_lm_loss_bwd": (ci, [ci, i64, i64, i64, i64, i64, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
         "tp_layer_set_option": (ci, [ctypes.c_char_p, ctypes.c_char_p]),
         "tp_layer_profile": (ci, [ci]),
         "tp_layer_profile_read": (ci, [ctypes.POINTER(ctypes.c_float), ci, ctypes.POINTER(ci)]),
@@ -382,3 +396,73 @@ def tp_layer_attn_bwd(dtype, B, S, nl, dh, causal, qkv, o, lse, d_o, dqkv, d_scr
     if check and rc != TPL_OK:
         raise TpLayerError(rc, "tp_layer_attn_bwd")
     return rc
+
+
+def tp_layer_rope_frequencies(rot, base=10000.0, scaling=TPL_ROPE_PLAIN, stretch=1.0, context=0.0, check=True):
+    """(radians per position of each pair, as a list; factor)."""
+    freq, factor = (ctypes.c_double * max(1, rot // 2))(), ctypes.c_float(1.0)
+    rc = load_library().tp_layer_rope_frequencies(rot, float(base), scaling, float(stretch), float(context), freq, ctypes.byref(factor))
+    _checked(rc, "tp_layer_rope_frequencies", check)
+    return list(freq)[:rot // 2], factor.value
+
+
+def tp_layer_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, qkv, out, seq=0, stream=None, check=True):
+    rc = load_library().tp_layer_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(qkv),
+                                          _ptr(out), _stream(stream))
+    return _checked(rc, "tp_layer_rope_fwd", check)
+
+
+def tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, dqkv, out, seq=0, stream=None, check=True):
+    rc = load_library().tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(dqkv),
+                                          _ptr(out), _stream(stream))
+    return _checked(rc, "tp_layer_rope_bwd", check)
+
+
+def tp_layer_pack_plan_bytes(sequences, M, nq, nkv):
+    return load_library().tp_layer_pack_plan_bytes(sequences, M, nq, nkv)
+
+
+def tp_layer_pack_plan(sequences, M, offsets, nq, nkv, causal, plan, plan_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_pack_plan(sequences, M, _ptr(offsets), nq, nkv, int(bool(causal)), _ptr(plan),
+                                           (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_pack_plan", check)
+
+
+def tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, bwd):
+    return load_library().tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), int(bool(bwd)))
+
+
+def tp_layer_attn_packed_fwd(dtype, sequences, M, nq, nkv, dh, causal, plan, qkv, o, lse, ws, ws_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_attn_packed_fwd(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), _ptr(plan), _ptr(qkv), _ptr(o), _ptr(lse),
+                                                 _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_attn_packed_fwd", check)
+
+
+def tp_layer_attn_packed_bwd(dtype, sequences, M, nq, nkv, dh, causal, plan, qkv, o, lse, d_o, dqkv, d_scratch, ws, ws_bytes=None,
+                             stream=None, check=True):
+    rc = load_library().tp_layer_attn_packed_bwd(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), _ptr(plan), _ptr(qkv), _ptr(o), _ptr(lse),
+                                                 _ptr(d_o), _ptr(dqkv), _ptr(d_scratch), _ptr(ws),
+                                                 (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_attn_packed_bwd", check)
+
+
+def tp_layer_lm_loss_workspace_bytes(dtype, M, H, V, bwd):
+    return load_library().tp_layer_lm_loss_workspace_bytes(dtype, M, H, V, int(bool(bwd)))
+
+
+def tp_layer_lm_loss_fwd(dtype, M, H, V, first, x, w, labels, stats, ws, ws_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_lm_loss_fwd(dtype, M, H, V, first, _ptr(x), _ptr(w), _ptr(labels), _ptr(stats), _ptr(ws),
+                                             (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_lm_loss_fwd", check)
+
+
+def tp_layer_lm_loss_join(M, ranks, vocab, stats, labels, loss, lse, stream=None, check=True):
+    rc = load_library().tp_layer_lm_loss_join(M, ranks, vocab, _ptr(stats), _ptr(labels), _ptr(loss), _ptr(lse), _stream(stream))
+    return _checked(rc, "tp_layer_lm_loss_join", check)
+
+
+def tp_layer_lm_loss_bwd(dtype, M, H, V, first, vocab, x, w, labels, lse, dloss, dx_partial, dw, ws, ws_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_lm_loss_bwd(dtype, M, H, V, first, vocab, _ptr(x), _ptr(w), _ptr(labels), _ptr(lse), _ptr(dloss),
+                                             _ptr(dx_partial), _ptr(dw), _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
+                                             _stream(stream))
+    return _checked(rc, "tp_layer_lm_loss_bwd", check)

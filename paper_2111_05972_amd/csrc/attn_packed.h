@@ -1,0 +1,94 @@
+// Attention of packed sequences with grouped heads: the plan of a batch, and how rows are numbered.  Shared by the plan kernel
+// (attn_packed_plan.hip) and the bf16 and float kernels.
+//
+// Flattened rows.  The G = nq / nkv query heads of a key head read the same keys, so to that key head they are one sequence of
+// len * G query rows: row r is head r % G of query r / G.  Its keys are 0 .. r / G under the causal mask, that is, key j is seen
+// by the rows r >= j G.  A block of 128 rows is then full where there are short sequences and many heads to a key head, crosses a
+// short piece of the diagonal, and dK, dV of a key head need no sum over heads besides the one over rows.
+//
+// Plan (device memory, 32-bit words): positions [M], a header, offsets of the sequences, block counts, and lists of work items.
+// A strip is a block of 128 rows (forward, dQ) or 128 keys (dK, dV) of a sequence with the 64-row tiles that it visits on the other
+// side.  Strips much longer than a compute unit's share of all tiles are cut into chunks, each an item of its own that leaves float
+// sums in a slot of the workspace, and joined in chunk order by another kernel.  Lists are ordered by length, longest first (what
+// starts last should be short); items of equal length come in any order, which no result depends on.
+#pragma once
+#include <hip/hip_runtime_api.h>
+
+#include <cstddef>
+#include <cstdint>
+
+namespace tpl {
+
+constexpr int PACK_BLK = 128, PACK_TILE = 64;
+constexpr int PACK_MAX_GROUP = 128;
+constexpr int PACK_MIN_CHUNK = 16;        // tiles; shorter chunks cost more in their ends than they save
+
+struct PackItem {
+    int t0, len;           // the sequence: first row of the batch, length
+    int first;             // first flattened row (forward, dQ) or key (dK, dV) of the strip
+    int tile0, tile1;      // tiles of the other side: [tile0, tile1)
+    int slot;              // of this chunk's sums (of chunk 0's in the join lists), -1: the whole strip
+    int chunks;            // of the strip
+    int pad;
+};
+struct PackHeader {
+    int sequences, tokens, nq, nkv, causal;
+    int items[2];          // [0]: forward and dQ, [1]: dK, dV
+    int joins[2];          // strips that were cut
+    int pad[7];
+};
+// Word offsets of the plan's parts; a function of what the host knows, so host and device agree without a copy.
+struct PackLayout {
+    int64_t header, start, pre[2], items[2], joins[2], words;
+    int64_t cap[2];        // items, also the slots
+    int64_t join_cap;
+};
+inline int64_t pack_up(int64_t x) { return (x + 63) / 64 * 64; }
+// `share_cap`: how many chunks of the average share there can be (pack_shares), 0: nothing is cut
+inline PackLayout pack_layout(int64_t sequences, int64_t M, int64_t nq, int64_t nkv, int64_t share_cap) {
+    PackLayout L;
+    const int64_t G = nq / nkv;
+    L.cap[0] = (M * G) / PACK_BLK + sequences + share_cap;      // a strip of n tiles has at most n / chunk + 1 chunks
+    L.cap[1] = M / PACK_BLK + sequences + share_cap;
+    L.join_cap = share_cap;                                     // strips longer than a chunk
+    int64_t w = pack_up(M);
+    L.header = w; w += pack_up(sizeof(PackHeader) / 4);
+    L.start = w; w += pack_up(sequences + 1);
+    for (int s = 0; s < 2; ++s) { L.pre[s] = w; w += pack_up(sequences + 1); }
+    for (int s = 0; s < 2; ++s) { L.items[s] = w; w += pack_up(L.cap[s] * 8); }
+    for (int s = 0; s < 2; ++s) { L.joins[s] = w; w += pack_up(L.join_cap * 8); }
+    L.words = w;
+    return L;
+}
+// Compute units' shares of the launch's tiles, per key head: a chunk is no shorter than all tiles divided by this.  Two shares to a
+// unit, so that one that gets a long item early gets fewer later.  None where no strip can have twice the shortest chunk.
+inline int64_t pack_shares(int64_t M, int64_t nq, int64_t nkv, int units) {
+    if (M * (nq / nkv) < (int64_t)2 * PACK_MIN_CHUNK * PACK_TILE) return 0;
+    return (2 * units + nkv - 1) / nkv;
+}
+
+#ifdef __HIPCC__
+__device__ __forceinline__ const PackItem* pack_items(const int* plan, int64_t at) { return reinterpret_cast<const PackItem*>(plan + at); }
+// Whether the plan at hand was made for this call.
+__device__ __forceinline__ bool pack_matches(const PackHeader* h, int tokens, int nq, int nkv, int causal) {
+    return h->tokens == tokens && h->nq == nq && h->nkv == nkv && h->causal == causal;
+}
+#endif
+
+// What an attention call of packed sequences works on.
+struct PackAttnArgs {
+    int dtype;
+    int64_t sequences, M;
+    int nq, nkv, dh, causal;
+    const int* plan;
+    const void* qkv; void* o; float* lse;                         // lse [M, nq]
+    const void* d_o; void* dqkv; float* dsum;                     // dsum [M, nq]
+    void* ws; size_t ws_bytes;
+    hipStream_t stream;
+};
+hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int causal, int* plan, hipStream_t s);
+size_t attn_packed_workspace_bytes(const PackAttnArgs& a, bool bwd);
+hipError_t attn_packed_bf16(const PackAttnArgs& a, bool bwd);
+hipError_t attn_packed_f32(const PackAttnArgs& a, bool bwd);
+
+}  // namespace tpl

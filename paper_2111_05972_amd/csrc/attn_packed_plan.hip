@@ -1,0 +1,201 @@
+// The plan of a packed batch (attn_packed.h), made on the device from the offsets of its sequences: one launch, no host copy, so
+// that it can be enqueued ahead of a step or captured with it.  Workgroup 0 makes the lists, the others the positions.
+//
+// Offsets are taken as their running maximum, clamped to [0, M]: whatever the caller's memory holds, sequences neither overlap
+// nor leave the rows, and the lists stay within their capacity.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "attn_packed_dev.h"
+#include "kernels.h"
+
+namespace tpl {
+namespace {
+
+constexpr int PLAN_THREADS = 1024;
+constexpr int BUCKETS = 1024;
+
+// Inclusive scan over the workgroup: sum, or maximum.
+template <bool MAX> __device__ int block_scan(int v, int* tmp) {
+    const int t = threadIdx.x;
+    tmp[t] = v;
+    __syncthreads();
+    for (int d = 1; d < PLAN_THREADS; d *= 2) {
+        const int o = t >= d ? tmp[t - d] : (MAX ? -1 : 0);
+        __syncthreads();
+        tmp[t] = MAX ? max(tmp[t], o) : tmp[t] + o;
+        __syncthreads();
+    }
+    return tmp[t];
+}
+
+struct PlanParams {
+    int n, M, nq, nkv, causal, shares;
+    const int* offsets;
+    int* plan;
+    PackLayout L;
+};
+
+// Strip `i` of a sequence: its first row or key and its tiles.
+__device__ __forceinline__ void strip_of(const PlanParams& p, int side, int len, int i, int& first, int& tile0, int& tile1) {
+    const int G = p.nq / p.nkv;
+    const int64_t rows = (int64_t)len * G;
+    first = i * PACK_BLK;
+    if (side == 0) {
+        const int64_t last = min(rows, (int64_t)first + PACK_BLK) - 1;
+        tile0 = 0;
+        tile1 = p.causal ? (int)(last / G) / PACK_TILE + 1 : (len + PACK_TILE - 1) / PACK_TILE;
+    } else {
+        tile0 = p.causal ? (int)((int64_t)first * G / PACK_TILE) : 0;
+        tile1 = (int)((rows + PACK_TILE - 1) / PACK_TILE);
+    }
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
+    __shared__ int tmp[PLAN_THREADS];
+    __shared__ int hist[2][BUCKETS];
+    __shared__ int longest[2], slots[2], joins[2];
+    __shared__ unsigned long long tiles[2];
+    const int t = threadIdx.x, G = p.nq / p.nkv;
+    int* start = p.plan + p.L.start;
+    auto offset = [&](int i) { return min(max(p.offsets[i], 0), p.M); };
+    if (blockIdx.x > 0) {
+        // Positions: this workgroup's tokens, each looking for its sequence among the offsets.  Where these decrease the running
+        // maximum would be needed: the lists of workgroup 0 do not read positions, so a wrong one is no more than that.
+        for (int64_t m = (int64_t)(blockIdx.x - 1) * PLAN_THREADS + t; m < p.M; m += (int64_t)(gridDim.x - 1) * PLAN_THREADS) {
+            int lo = 0, hi = p.n;                                  // the last i with offset(i) <= m
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (offset(mid) <= m) lo = mid; else hi = mid - 1;
+            }
+            p.plan[m] = lo < p.n && offset(lo) <= m ? (int)m - offset(lo) : 0;
+        }
+        return;
+    }
+    if (t < 2) { longest[t] = 0; slots[t] = 0; joins[t] = 0; tiles[t] = 0; }
+    for (int i = t; i < 2 * BUCKETS; i += PLAN_THREADS) (&hist[0][0])[i] = 0;
+    __syncthreads();
+    // offsets as running maxima, and the strips before each sequence
+    int carry_max = 0, carry[2] = {0, 0};
+    for (int base = 0; base <= p.n; base += PLAN_THREADS) {
+        const int i = base + t;
+        const int c = max(block_scan<true>(i <= p.n ? offset(i) : 0, tmp), carry_max);
+        if (i <= p.n) start[i] = c;
+        __syncthreads();
+        carry_max = max(carry_max, tmp[PLAN_THREADS - 1]);
+        __syncthreads();
+    }
+    __threadfence_block();
+    __syncthreads();
+    for (int base = 0; base <= p.n; base += PLAN_THREADS) {
+        const int i = base + t;
+        const int len = i < p.n ? start[i + 1] - start[i] : 0;
+        for (int side = 0; side < 2; ++side) {
+            const int64_t rows = side == 0 ? (int64_t)len * G : len;
+            const int blocks = (int)((rows + PACK_BLK - 1) / PACK_BLK);
+            const int pre = block_scan<false>(blocks, tmp) + carry[side];
+            if (i <= p.n) (p.plan + p.L.pre[side])[i] = pre - blocks;
+            __syncthreads();
+            carry[side] += tmp[PLAN_THREADS - 1];
+            __syncthreads();
+        }
+    }
+    __threadfence_block();
+    __syncthreads();
+    auto find = [&](const int* pre, int item) {                    // the sequence that strip `item` belongs to
+        int lo = 0, hi = p.n - 1;                                  // the last i with pre[i] <= item: sequences without strips lie before it
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pre[mid] <= item) lo = mid; else hi = mid - 1;
+        }
+        return lo;
+    };
+    for (int side = 0; side < 2; ++side) {
+        const int* pre = p.plan + p.L.pre[side];
+        unsigned long long mine = 0;
+        int most = 0;
+        for (int k = t; k < carry[side]; k += PLAN_THREADS) {
+            const int b = find(pre, k);
+            int first, t0, t1;
+            strip_of(p, side, start[b + 1] - start[b], k - pre[b], first, t0, t1);
+            mine += (unsigned)(t1 - t0);
+            most = max(most, t1 - t0);
+        }
+        atomicAdd(&tiles[side], mine);
+        atomicMax(&longest[side], most);
+    }
+    __syncthreads();
+    for (int side = 0; side < 2; ++side) {
+        const int* pre = p.plan + p.L.pre[side];
+        int chunk = 1 << 30;
+        if (p.shares > 0) chunk = max(PACK_MIN_CHUNK, (int)((tiles[side] + p.shares - 1) / p.shares));
+        const int top = min(longest[side], chunk) + 1;
+        PackItem* items = reinterpret_cast<PackItem*>(p.plan + p.L.items[side]);
+        PackItem* join = reinterpret_cast<PackItem*>(p.plan + p.L.joins[side]);
+        for (int pass = 0; pass < 2; ++pass) {                     // count, then place
+            for (int k = t; k < carry[side]; k += PLAN_THREADS) {
+                const int b = find(pre, k);
+                PackItem it{};
+                it.t0 = start[b];
+                it.len = start[b + 1] - start[b];
+                int a, z;
+                strip_of(p, side, it.len, k - pre[b], it.first, a, z);
+                it.chunks = (z - a + chunk - 1) / chunk;
+                const int each = (z - a + it.chunks - 1) / it.chunks;
+                const int bucket = BUCKETS - 1 - (int)((int64_t)each * (BUCKETS - 1) / top);     // longest first
+                if (pass == 0) {
+                    atomicAdd(&hist[side][bucket], it.chunks);
+                    continue;
+                }
+                const int at = atomicAdd(&hist[side][bucket], it.chunks);
+                int slot = -1;
+                if (it.chunks > 1) {
+                    slot = atomicAdd(&slots[side], it.chunks);
+                    const int j = atomicAdd(&joins[side], 1);
+                    it.slot = slot;
+                    it.tile0 = a;
+                    it.tile1 = z;
+                    if (j < p.L.join_cap) join[j] = it;
+                }
+                for (int c = 0; c < it.chunks; ++c) {
+                    it.slot = slot < 0 ? -1 : slot + c;
+                    it.tile0 = a + c * each;
+                    it.tile1 = min(z, a + (c + 1) * each);
+                    if (at + c < p.L.cap[side]) items[at + c] = it;
+                }
+            }
+            __syncthreads();
+            if (pass == 0) {                                       // counts -> first places
+                const int v = hist[side][t], before = block_scan<false>(v, tmp) - v;
+                __syncthreads();
+                hist[side][t] = before;
+                __syncthreads();
+            }
+        }
+        if (t == 0) {
+            PackHeader* h = reinterpret_cast<PackHeader*>(p.plan + p.L.header);
+            h->items[side] = min(hist[side][BUCKETS - 1], (int)p.L.cap[side]);   // the end of the last bucket
+            h->joins[side] = min(joins[side], (int)p.L.join_cap);
+            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->causal = p.causal; }
+        }
+    }
+}
+
+}  // namespace
+
+size_t attn_packed_workspace_bytes(const PackAttnArgs& a, bool bwd) { return ws_of(a, bwd).total; }
+
+hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int causal, int* plan, hipStream_t s) {
+    PlanParams p{};
+    p.n = (int)sequences; p.M = (int)M; p.nq = nq; p.nkv = nkv; p.causal = causal;
+    p.shares = (int)pack_shares(M, nq, nkv, compute_units());
+    p.offsets = offsets; p.plan = plan;
+    p.L = pack_layout(sequences, M, nq, nkv, p.shares);
+    static_assert(BUCKETS == PLAN_THREADS, "a thread to a bucket");
+    const int64_t groups = std::min<int64_t>((M + PLAN_THREADS - 1) / PLAN_THREADS, 1024);
+    hipLaunchKernelGGL(pack_plan_kernel, dim3((unsigned)(1 + groups)), dim3(PLAN_THREADS), 0, s, p);
+    return hipGetLastError();
+}
+
+}  // namespace tpl

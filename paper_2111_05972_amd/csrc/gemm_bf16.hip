@@ -1359,7 +1359,7 @@ struct PPGroupParams {
     int layout[JOB_MAX], shares[JOB_MAX], first[JOB_MAX + 1];
     int n;
 };
-template <typename TL>
+template <typename TL, bool ACC>
 __global__ __launch_bounds__(512, 2) void gemm_bf16_group_pp_kernel(PPGroupParams gp) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     const int bid = blockIdx.x;
@@ -1372,16 +1372,16 @@ __global__ __launch_bounds__(512, 2) void gemm_bf16_group_pp_kernel(PPGroupParam
     if (layout == 0) pp_products<TL, true, false, false>(p, w, smem, acc);
     else if (layout == 1) pp_products<TL, true, true, false>(p, w, smem, acc);
     else pp_products<TL, false, false, true>(p, w, smem, acc);
-    pp_epilogue<TL>(p, acc, w.m0, w.n0, w.partial);
+    pp_epilogue<TL, ACC>(p, acc, w.m0, w.n0, w.partial);
 }
 // The tiles whose K was cut: a workgroup per 16 rows of a wavefront; [first[j], first[j+1]) are those of job j.
-template <typename TL>
+template <typename TL, bool ACC>
 __global__ __launch_bounds__(512) void gemm_group_pp_sum_kernel(PPGroupParams gp) {
     const int bid = blockIdx.x;
     int i = 0;
     while (i + 1 < gp.n && bid >= gp.first[i + 1]) ++i;
     const int pos = bid - gp.first[i];
-    pp_sum_rows<TL>(gp.g[i], gp.run[i], gp.shares[i], pos / (4 * TL::UA), pos % (4 * TL::UA));
+    pp_sum_rows<TL, ACC>(gp.g[i], gp.run[i], gp.shares[i], pos / (4 * TL::UA), pos % (4 * TL::UA));
 }
 // The sums over K shares of all GEMMs of a group that were cut (and of their column sums): GEMM i has the workgroups
 // [first[i], first[i+1]) of this launch, 256 chunks of 8 outputs each, the N / 8 chunks of the column sums last.
@@ -1705,7 +1705,8 @@ static GemmParams gemm_params(const GemmArgs& a) {
     p.bias = (const bf16_t*)a.bias; p.resid = (const bf16_t*)a.resid; p.aux = (bf16_t*)a.aux;
     p.M = (int)a.M; p.N = (int)a.N; p.K = (int)a.K;
     p.nt_store = a.c_streaming ? 1 : 0;
-    p.lda = a.trans_a ? (int)a.M : (int)a.K;
+    p.lda = a.lda ? (int)a.lda : a.trans_a ? (int)a.M : (int)a.K;
+    p.acc = a.acc; p.acc_mode = a.acc_mode;
     p.ldb = a.trans_b ? (int)a.K : (int)a.N;
     p.epi = a.epi;
     p.tiles_m = p.tiles_n = 0;
@@ -2075,10 +2076,12 @@ bool takes_wide_tile(const GemmArgs* g, int n, const GroupPlan& wide, const Grou
     return few_rows_us(g, n, wide) < (GROUP_TILES[other.tile].turns ? few_rows_us(g, n, other) / 1.035 : other_us / 1.25);
 }
 
+bool any_acc(const GemmArgs* g, int n) { return std::any_of(g, g + n, [](const GemmArgs& a) { return a.acc != nullptr; }); }
 GroupPlan make_group_plan(const GemmArgs* g, int n) {
-    const int forced = n == 1 ? 256 : options().gemm_group;       // one GEMM: see by_turns
+    const int forced = n == 1 ? 256 : any_acc(g, n) ? 0 : options().gemm_group;       // one GEMM: see by_turns
     double us = INFINITY;
-    GroupPlan best = make_small_plan(g, n, forced, &us);
+    GroupPlan best{};
+    if (!any_acc(g, n)) best = make_small_plan(g, n, forced, &us);    // running sums: the tiles by turns only, which have the epilogue
     const bool weight_grads = std::any_of(g, g + n, [](const GemmArgs& a) { return a.trans_a != 0; });
     for (int t = 0; t < GROUP_TILE_COUNT; ++t) {
         const GroupTile& gt = GROUP_TILES[t];
@@ -2091,7 +2094,7 @@ GroupPlan make_group_plan(const GemmArgs* g, int n) {
         const double put_at = p.us * (weight_grads && !at_once ? TURNS_LEAD : 1.0);
         if (put_at < us) { best = p; best.tile = t; us = put_at; }
     }
-    if (forced <= 0 && std::all_of(g, g + n, [](const GemmArgs& a) { return a.M <= FEW_TOKENS && !a.trans_a; })) {
+    if (forced <= 0 && !any_acc(g, n) && std::all_of(g, g + n, [](const GemmArgs& a) { return a.M <= FEW_TOKENS && !a.trans_a; })) {
         GroupPlan p = make_pp_plan(g, n, GROUP_TILES[WIDE_TILE], INFINITY);
         p.tile = WIDE_TILE;
         if (takes_wide_tile(g, n, p, best, us)) best = p;
@@ -2105,7 +2108,7 @@ GroupPlan plan_group(const GemmArgs* g, int n) {
     for (int i = 0; i < n; ++i) {
         int64_t* k = key + 2 + 4 * i;
         // a group of one is planned for its size alone (by_turns)
-        k[0] = g[i].M; k[1] = g[i].N; k[2] = g[i].K; k[3] = n == 1 ? 0 : (g[i].trans_a ? 1 : 0) | (g[i].trans_b ? 2 : 0) | g[i].epi << 2;
+        k[0] = g[i].M; k[1] = g[i].N; k[2] = g[i].K; k[3] = n == 1 ? 0 : (g[i].trans_a ? 1 : 0) | (g[i].trans_b ? 2 : 0) | g[i].epi << 2 | (g[i].acc ? 64 : 0);
     }
     return cache.get(key, [&] { return make_group_plan(g, n); });
 }
@@ -2140,7 +2143,7 @@ static hipError_t launch_group(void (*kernel)(Params), int threads, const Params
     return hipGetLastError();
 }
 
-template <typename TL>
+template <typename TL, bool ACC = false>
 static hipError_t launch_pp_jobs(const GroupPlan& pl, const GemmArgs* g, int n, void* ws, size_t ws_bytes, hipStream_t stream) {
     if (pp_bytes(pl, g, n) > (ws ? ws_bytes : 0)) return hipErrorInvalidValue;
     PPGroupParams gp{}, sp{};                                     // all jobs; the sums of those that were cut
@@ -2170,14 +2173,16 @@ static hipError_t launch_pp_jobs(const GroupPlan& pl, const GemmArgs* g, int n, 
         sp.first[sp.n + 1] = sp.first[sp.n] + job.count * 4 * TL::UA;
         ++sp.n;
     }
-    const hipError_t e = launch_group<TL>(&gemm_bf16_group_pp_kernel<TL>, 512, gp, stream);
+    const hipError_t e = launch_group<TL>(&gemm_bf16_group_pp_kernel<TL, ACC>, 512, gp, stream);
     if (e != hipSuccess || sp.n == 0) return e;
-    hipLaunchKernelGGL(gemm_group_pp_sum_kernel<TL>, dim3((unsigned)sp.first[sp.n]), dim3(512), 0, stream, sp);
+    hipLaunchKernelGGL((gemm_group_pp_sum_kernel<TL, ACC>), dim3((unsigned)sp.first[sp.n]), dim3(512), 0, stream, sp);
     return hipGetLastError();
 }
 
 static hipError_t launch_pp(const GroupPlan& pl, const GemmArgs* g, int n, void* ws, size_t ws_bytes, hipStream_t stream) {
     const GroupTile& t = GROUP_TILES[pl.tile];
+    if (any_acc(g, n))
+        return t.bn == 128 ? launch_pp_jobs<PPTile<4, 1>, true>(pl, g, n, ws, ws_bytes, stream) : launch_pp_jobs<PPTile<2, 2>, true>(pl, g, n, ws, ws_bytes, stream);
     return t.bn == 128   ? launch_pp_jobs<PPTile<4, 1>>(pl, g, n, ws, ws_bytes, stream)
            : t.bm == 128 ? launch_pp_jobs<PPTile<2, 1>>(pl, g, n, ws, ws_bytes, stream)
                          : launch_pp_jobs<PPTile<2, 2>>(pl, g, n, ws, ws_bytes, stream);

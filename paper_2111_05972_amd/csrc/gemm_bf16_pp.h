@@ -158,6 +158,17 @@ template <int KIND>
 __device__ __forceinline__ void pp_emit(const GemmParams& p, int row, int col, float (&v)[8], const float* bias, const uint4& in) {
     if (row >= p.M || col >= p.N) return;
     const int64_t idx = (int64_t)row * p.N + col;
+    if constexpr (KIND == KIND_ACC) {
+        if (p.acc_mode & ACC_ADD) {
+            float r8[8];
+            load8(p.acc + idx, r8);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += r8[e];
+        }
+        if (p.acc_mode & ACC_LAST) *reinterpret_cast<uint4*>(p.C + idx) = pack8(v);
+        else store8(p.acc + idx, v);
+        return;
+    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += bias[e];
     if (KIND == KIND_RESID || (KIND == KIND_ANY && p.resid)) {
@@ -241,13 +252,19 @@ __device__ __forceinline__ void pp_store_partial(const GemmParams& p, const PPAc
         pp_store_partial<TL, BLOCK + 1>(p, acc, row0, partial);
     }
 }
-template <typename TL>
+// ACC: some GEMM of the launch adds to running sums (kernels of their own, so that the others stay as they are).
+template <typename TL, bool ACC>
 __device__ __forceinline__ void pp_epilogue(const GemmParams& p, const PPAcc<TL>& acc, int m0, int n0, float* partial) {
     if (partial) {
         pp_store_partial<TL, 0>(p, acc, m0 + pp_wave() / TL::WN * 64, partial);
         return;
     }
     const PPLane el = pp_lane<TL>(p, m0, n0);
+    if constexpr (ACC) {
+        if (p.acc) pp_rows<TL, KIND_ACC>(p, acc, el);
+        else pp_rows<TL, KIND_PLAIN>(p, acc, el);
+        return;
+    }
     if (p.epi == EPI_NONE && !p.resid) pp_rows<TL, KIND_PLAIN>(p, acc, el);
     else if (p.epi == EPI_NONE) pp_rows<TL, KIND_RESID>(p, acc, el);
     else if (p.epi == EPI_GELU && !p.resid) pp_rows<TL, KIND_GELU>(p, acc, el);
@@ -255,7 +272,7 @@ __device__ __forceinline__ void pp_epilogue(const GemmParams& p, const PPAcc<TL>
     else pp_rows<TL, KIND_ANY>(p, acc, el);
 }
 // Row block `block` of tile `local` of a run whose K was cut: the shares' sums in share order, then the epilogue.
-template <typename TL>
+template <typename TL, bool ACC>
 __device__ __forceinline__ void pp_sum_rows(const GemmParams& p, const PPRun& r, int shares, int local, int block) {
     int tm, tn;
     tile_coords(r.tile0 + local, p.tiles_m, p.tiles_n, p.band, tm, tn);
@@ -277,7 +294,8 @@ __device__ __forceinline__ void pp_sum_rows(const GemmParams& p, const PPRun& r,
             }
         }
         const uint4 none[2] = {};
-        pp_row_block<KIND_ANY>(p, el, row, x, none);
+        if (ACC && p.acc) pp_row_block<KIND_ACC>(p, el, row, x, none);
+        else pp_row_block<KIND_ANY>(p, el, row, x, none);
     }
     const int col = n0 + (int)threadIdx.x;
     if (block == 0 && tm == 0 && p.colsum && threadIdx.x < TL::BN && col < p.N) {

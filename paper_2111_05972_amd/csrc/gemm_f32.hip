@@ -54,6 +54,7 @@ struct GemmF32Params {
     const float* A; const float* B; float* C;
     const float* bias; const float* resid; float* aux;
     int M, N, K, lda, ldb, epi;
+    int b_rows;                                 // rows of B as stored
     int tiles_m, tiles_n, nk, nk_total;         // nk: k-steps of one share
     float* partial;                             // [share][M][N], or null
     float* colsum;                              // [N]: sum over k of B[k][n] (weight gradients of a group), or null
@@ -100,7 +101,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmF32Params& p, int list_p
     const int nk = p.nk_total - kt0 < p.nk ? p.nk_total - kt0 : p.nk;
 
     const i32x4 ra = make_rsrc(p.A, (unsigned)((int64_t)(A_KMAJ ? p.M : p.K) * p.lda * 4));
-    const i32x4 rb = make_rsrc(p.B, (unsigned)((int64_t)(B_KMAJ ? p.N : p.K) * p.ldb * 4));
+    const i32x4 rb = make_rsrc(p.B, (unsigned)((int64_t)p.b_rows * p.ldb * 4));
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
     unsigned offa[LA], offb[LB];
     int ka[LA], kb[LB];                          // k of the chunk inside a stage (K contiguous), 0 otherwise
@@ -116,7 +117,7 @@ __device__ __forceinline__ void gemm_f32_tile(const GemmF32Params& p, int list_p
     for (int i = 0; i < LB; ++i) {
         int r, c;
         f32_chunk_src<B_KMAJ, BN>(t + 256 * i, r, c);
-        const bool ok = B_KMAJ ? n0 + r < p.N : n0 + 4 * c < p.N;
+        const bool ok = B_KMAJ ? n0 + r < p.b_rows : n0 + 4 * c < p.N;
         offb[i] = ok ? (unsigned)(B_KMAJ ? ((int64_t)(n0 + r) * p.ldb + 4 * c) * 4 : ((int64_t)r * p.ldb + n0 + 4 * c) * 4) : F_OOB;
         kb[i] = B_KMAJ ? 4 * c : 0;
     }
@@ -431,7 +432,8 @@ static GemmF32Params f32_params(const GemmArgs& a) {
     p.A = (const float*)a.A; p.B = (const float*)a.B; p.C = (float*)a.C;
     p.bias = (const float*)a.bias; p.resid = (const float*)a.resid; p.aux = (float*)a.aux;
     p.M = (int)a.M; p.N = (int)a.N; p.K = (int)a.K; p.epi = a.epi;
-    p.lda = a.trans_a ? p.M : p.K;
+    p.lda = a.lda ? (int)a.lda : a.trans_a ? p.M : p.K;
+    p.b_rows = a.trans_b ? (a.b_rows ? (int)a.b_rows : p.N) : p.K;
     p.ldb = a.trans_b ? p.K : p.N;
     p.nk_total = (p.K + FK - 1) / FK;
     return p;

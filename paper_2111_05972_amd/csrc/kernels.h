@@ -48,7 +48,13 @@ struct GemmArgs {
     void* colsum_b;     // [N] or null: where the kernel may also leave sum_k B[k][n] (the bias gradient that goes with a
                         // weight gradient); whether it did is reported by gemm_bf16 / run through colsum_done
     bool colsum_done;
+    int64_t lda;        // row stride of A as stored, 0: dense (only the group launches look at it)
+    int64_t b_rows;     // rows of a K-major B that exist, 0: N (float only): columns of C past them come out as 0
+    // bf16 groups: C is one of several products that are added up in float: acc [M,N] = what ACC_ADD takes in, C is written with ACC_LAST only
+    float* acc;
+    int acc_mode;
 };
+enum { ACC_ADD = 1, ACC_LAST = 2 };
 
 struct AttnArgs {
     int dtype;
@@ -142,5 +148,34 @@ bool attn_bf16_supported(const AttnArgs& a);
 hipError_t attn_bf16_fwd(const AttnArgs& a);
 hipError_t attn_bf16_bwd(const AttnArgs& a);
 size_t attn_bf16_workspace_bytes(const AttnArgs& a, bool bwd);
+
+// Rotary positions on rows of (q | k | v, head, dh): see tp_layer_rope_fwd.
+struct RopeArgs {
+    int dtype;
+    int64_t M, seq;
+    int nq, nkv, dh, rot, adjacent;
+    const double* freq; float factor;
+    const int* positions;
+    const void* in; void* out;
+    hipStream_t stream;
+};
+hipError_t rope(const RopeArgs& a, bool back);
+
+// Softmax cross entropy of a vocabulary shard: see tp_layer_lm_loss_fwd.
+struct LmLossArgs {
+    int dtype;
+    int64_t M, H, V, first, vocab;
+    const void* x; const void* w;
+    const int* labels;
+    float* stats;                               // fwd: [M][2]
+    const float* lse; const float* dloss;       // bwd
+    void* dx; void* dw;
+    void* ws; size_t ws_bytes;
+    hipStream_t stream;
+};
+size_t lm_loss_workspace_bytes(int dtype, int64_t M, int64_t H, int64_t V, bool bwd);
+hipError_t lm_loss_fwd(const LmLossArgs& a);
+hipError_t lm_loss_bwd(const LmLossArgs& a);
+hipError_t lm_loss_join(int64_t M, int64_t ranks, int64_t vocab, const float* stats, const int* labels, float* loss, float* lse, hipStream_t s);
 
 }  // namespace tpl

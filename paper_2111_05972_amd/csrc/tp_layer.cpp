@@ -3,10 +3,12 @@
 #include "../../include/tp_layer.h"
 
 #include <algorithm>
+#include <cmath>
 #include <cstdlib>
 #include <cstring>
 #include <initializer_list>
 
+#include "attn_packed.h"
 #include "kernels.h"
 
 using namespace tpl;
@@ -881,6 +883,158 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal, const
     a.dqkv = dqkv; a.dsum = d_scratch; a.ws = ws; a.ws_bytes = ws_bytes; a.own_chunking = 1;
     a.stream = (hipStream_t)hip_stream;
     return run_attn(a, true);
+}
+
+// ---- rotary positions, attention of packed sequences, loss of a vocabulary shard ---------------------------------------
+int tp_layer_rope_frequencies(int rot, double base, int scaling, double stretch, double context, double* freq, float* factor) {
+    if (rot <= 0 || rot % 2 || !freq || !factor || !(base > 0.0)) return TPL_EINVAL;
+    if (scaling < TPL_ROPE_PLAIN || scaling > TPL_ROPE_PARTS) return TPL_EINVAL;
+    if (scaling != TPL_ROPE_PLAIN && !(stretch > 0.0)) return TPL_EINVAL;
+    if (scaling == TPL_ROPE_PARTS && !(context > 0.0)) return TPL_EINVAL;
+    const double circle = 6.28318530717958647692;
+    if (scaling == TPL_ROPE_BASE && rot > 2) base *= std::pow(stretch, (double)rot / (rot - 2));
+    for (int i = 0; i < rot / 2; ++i) {
+        double f = std::pow(base, -2.0 * i / rot);
+        if (scaling == TPL_ROPE_LINEAR) f /= stretch;
+        if (scaling == TPL_ROPE_PARTS) {
+            const double turns = context * f / circle, keep = std::min(1.0, std::max(0.0, (turns - 1.0) / (32.0 - 1.0)));
+            f = keep * f + (1.0 - keep) * f / stretch;
+        }
+        freq[i] = f;
+    }
+    *factor = scaling == TPL_ROPE_PARTS && stretch > 1.0 ? (float)(0.1 * std::log(stretch) + 1.0) : 1.0f;
+    return TPL_OK;
+}
+
+static int rope_call(bool back, int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor, const int32_t* positions,
+                     int64_t seq, const void* in, void* out, void* hip_stream) {
+    if (dtype != TPL_F32 && dtype != TPL_BF16) return TPL_EINVAL;
+    if (M <= 0 || nq <= 0 || nkv <= 0 || dh <= 0 || rot <= 0 || rot % 2 || rot > dh) return TPL_EINVAL;
+    if (pairs != TPL_ROPE_HALF && pairs != TPL_ROPE_ADJACENT) return TPL_EINVAL;
+    if (!freq || !in || !out || (!positions && seq <= 0)) return TPL_EINVAL;
+    if (M > (int64_t)1 << 24 || nq > 1 << 16 || nkv > 1 << 16 || dh > 8192) return TPL_EUNSUPPORTED;
+    if (((int64_t)nq + 2 * nkv) * dh % (dtype == TPL_BF16 ? 8 : 4) || ((int64_t)nq + 2 * nkv) * dh > 1 << 24) return TPL_EUNSUPPORTED;
+    if (misaligned(in) || misaligned(out) || misaligned(freq) || misaligned(positions)) return TPL_EALIGN;
+    RopeArgs a{};
+    a.dtype = dtype; a.M = M; a.seq = seq; a.nq = nq; a.nkv = nkv; a.dh = dh; a.rot = rot; a.adjacent = pairs == TPL_ROPE_ADJACENT;
+    a.freq = freq; a.factor = factor; a.positions = positions; a.in = in; a.out = out; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(rope(a, back));
+}
+int tp_layer_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor, const int32_t* positions, int64_t seq,
+                      const void* qkv, void* out, void* hip_stream) {
+    return rope_call(false, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, qkv, out, hip_stream);
+}
+int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor, const int32_t* positions, int64_t seq,
+                      const void* dqkv, void* out, void* hip_stream) {
+    return rope_call(true, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, dqkv, out, hip_stream);
+}
+
+static int pack_check(int64_t sequences, int64_t M, int nq, int nkv) {
+    if (sequences <= 0 || M <= 0 || nq <= 0 || nkv <= 0 || nq % nkv) return TPL_EINVAL;
+    const int64_t G = nq / nkv;
+    if (sequences > (int64_t)1 << 20 || M > (int64_t)1 << 24 || nq > 1 << 12 || G > PACK_MAX_GROUP || (M + 256) * G >= (int64_t)1 << 30) return TPL_EUNSUPPORTED;
+    // workgroups of a launch
+    const PackLayout L = pack_layout(sequences, M, nq, nkv, pack_shares(M, nq, nkv, compute_units()));
+    return (L.cap[0] + L.cap[1]) * nkv < (int64_t)1 << 30 ? TPL_OK : TPL_EUNSUPPORTED;
+}
+size_t tp_layer_pack_plan_bytes(int64_t sequences, int64_t M, int nq, int nkv) {
+    if (pack_check(sequences, M, nq, nkv)) return 0;
+    return up((size_t)pack_layout(sequences, M, nq, nkv, pack_shares(M, nq, nkv, compute_units())).words * sizeof(int));
+}
+int tp_layer_pack_plan(int64_t sequences, int64_t M, const int32_t* offsets, int nq, int nkv, int causal, void* plan, size_t plan_bytes, void* hip_stream) {
+    const int rc = pack_check(sequences, M, nq, nkv);
+    if (rc) return rc;
+    if (!offsets || !plan) return TPL_EINVAL;
+    if (((uintptr_t)offsets & 3u) != 0 || misaligned(plan)) return TPL_EALIGN;
+    if (plan_bytes < tp_layer_pack_plan_bytes(sequences, M, nq, nkv)) return TPL_EWORKSPACE;
+    return hip_rc(pack_plan(sequences, M, offsets, nq, nkv, causal != 0, (int*)plan, (hipStream_t)hip_stream));
+}
+
+static int attn_packed_check(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh) {
+    if (dtype != TPL_F32 && dtype != TPL_BF16) return TPL_EINVAL;
+    if (dh <= 0) return TPL_EINVAL;
+    const int rc = pack_check(sequences, M, nq, nkv);
+    if (rc) return rc;
+    return dh <= 128 && dh % 8 == 0 ? TPL_OK : TPL_EUNSUPPORTED;
+}
+static PackAttnArgs attn_packed_args(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal) {
+    PackAttnArgs a{};
+    a.dtype = dtype; a.sequences = sequences; a.M = M; a.nq = nq; a.nkv = nkv; a.dh = dh; a.causal = causal != 0;
+    return a;
+}
+size_t tp_layer_attn_packed_workspace_bytes(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, int bwd) {
+    if (attn_packed_check(dtype, sequences, M, nq, nkv, dh)) return 0;
+    return std::max(ALIGN, up(attn_packed_workspace_bytes(attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal), bwd != 0)));
+}
+int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, const void* qkv, void* o, float* lse,
+                             void* ws, size_t ws_bytes, void* hip_stream) {
+    const int rc = attn_packed_check(dtype, sequences, M, nq, nkv, dh);
+    if (rc) return rc;
+    if (!plan || !qkv || !o || !lse || !ws) return TPL_EINVAL;
+    const void* ptrs[] = {plan, qkv, o, lse, ws};
+    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
+    if (ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 0)) return TPL_EWORKSPACE;
+    PackAttnArgs a = attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal);
+    a.plan = (const int*)plan; a.qkv = qkv; a.o = o; a.lse = lse; a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(dtype == TPL_BF16 ? attn_packed_bf16(a, false) : attn_packed_f32(a, false));
+}
+int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, const void* qkv, const void* o,
+                             const float* lse, const void* d_o, void* dqkv, float* d_scratch, void* ws, size_t ws_bytes, void* hip_stream) {
+    const int rc = attn_packed_check(dtype, sequences, M, nq, nkv, dh);
+    if (rc) return rc;
+    if (!plan || !qkv || !o || !lse || !d_o || !dqkv || !d_scratch || !ws) return TPL_EINVAL;
+    const void* ptrs[] = {plan, qkv, o, lse, d_o, dqkv, d_scratch, ws};
+    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
+    if (ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 1)) return TPL_EWORKSPACE;
+    PackAttnArgs a = attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal);
+    a.plan = (const int*)plan; a.qkv = qkv; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse); a.d_o = d_o; a.dqkv = dqkv; a.dsum = d_scratch;
+    a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(dtype == TPL_BF16 ? attn_packed_bf16(a, true) : attn_packed_f32(a, true));
+}
+
+static int lm_loss_check(int dtype, int64_t M, int64_t H, int64_t V, int64_t first) {
+    if (dtype != TPL_F32 && dtype != TPL_BF16) return TPL_EINVAL;
+    if (M <= 0 || H <= 0 || V <= 0 || first < 0) return TPL_EINVAL;
+    const int64_t es = dtype == TPL_BF16 ? 2 : 4;
+    if (H % (16 / es) || H > (int64_t)1 << 20 || V > (int64_t)1 << 24 || first > (int64_t)1 << 30 || M > (int64_t)1 << 21 || M * H * es >= 0x7FFFFFFFll) return TPL_EUNSUPPORTED;
+    return TPL_OK;
+}
+size_t tp_layer_lm_loss_workspace_bytes(int dtype, int64_t M, int64_t H, int64_t V, int bwd) {
+    if (lm_loss_check(dtype, M, H, V, 0)) return 0;
+    return std::max(ALIGN, up(lm_loss_workspace_bytes(dtype, M, H, V, bwd != 0)));
+}
+int tp_layer_lm_loss_fwd(int dtype, int64_t M, int64_t H, int64_t V, int64_t first, const void* x, const void* w, const int32_t* labels, float* stats, void* ws,
+                         size_t ws_bytes, void* hip_stream) {
+    const int rc = lm_loss_check(dtype, M, H, V, first);
+    if (rc) return rc;
+    if (!x || !w || !labels || !stats || !ws) return TPL_EINVAL;
+    if (misaligned(x) || misaligned(w) || misaligned(ws) || ((uintptr_t)labels & 3u) || ((uintptr_t)stats & 7u)) return TPL_EALIGN;
+    if (ws_bytes < tp_layer_lm_loss_workspace_bytes(dtype, M, H, V, 0)) return TPL_EWORKSPACE;
+    LmLossArgs a{};
+    a.dtype = dtype; a.M = M; a.H = H; a.V = V; a.first = first; a.x = x; a.w = w; a.labels = labels; a.stats = stats;
+    a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(lm_loss_fwd(a));
+}
+int tp_layer_lm_loss_join(int64_t M, int64_t ranks, int64_t vocab, const float* stats, const int32_t* labels, float* loss, float* lse, void* hip_stream) {
+    if (M <= 0 || ranks <= 0 || vocab <= 0 || !stats || !labels || !loss || !lse) return TPL_EINVAL;
+    if (M > (int64_t)1 << 24 || ranks > 1 << 16) return TPL_EUNSUPPORTED;
+    if (((uintptr_t)stats & 7u) || (((uintptr_t)labels | (uintptr_t)loss | (uintptr_t)lse) & 3u)) return TPL_EALIGN;
+    return hip_rc(lm_loss_join(M, ranks, vocab, stats, labels, loss, lse, (hipStream_t)hip_stream));
+}
+int tp_layer_lm_loss_bwd(int dtype, int64_t M, int64_t H, int64_t V, int64_t first, int64_t vocab, const void* x, const void* w, const int32_t* labels,
+                         const float* lse, const float* dloss, void* dx_partial, void* dw, void* ws, size_t ws_bytes, void* hip_stream) {
+    const int rc = lm_loss_check(dtype, M, H, V, first);
+    if (rc) return rc;
+    if (vocab < first + V) return TPL_EINVAL;
+    if (vocab > (int64_t)1 << 30) return TPL_EUNSUPPORTED;
+    if (!x || !w || !labels || !lse || !dloss || !dx_partial || !dw || !ws) return TPL_EINVAL;
+    if (misaligned(x) || misaligned(w) || misaligned(dx_partial) || misaligned(dw) || misaligned(ws)) return TPL_EALIGN;
+    if (((uintptr_t)labels | (uintptr_t)lse | (uintptr_t)dloss) & 3u) return TPL_EALIGN;
+    if (ws_bytes < tp_layer_lm_loss_workspace_bytes(dtype, M, H, V, 1)) return TPL_EWORKSPACE;
+    LmLossArgs a{};
+    a.dtype = dtype; a.M = M; a.H = H; a.V = V; a.first = first; a.vocab = vocab; a.x = x; a.w = w; a.labels = labels; a.lse = lse; a.dloss = dloss;
+    a.dx = dx_partial; a.dw = dw; a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(lm_loss_bwd(a));
 }
 
 int tp_layer_set_option(const char* name, const char* value) {

@@ -1,0 +1,230 @@
+"""Attention of packed sequences with grouped heads against its definition in 64 bits: lengths, head sizes, groups, cut strips, what a mask
+hides, rows of no sequence, plans, graphs."""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+import packed_ref as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+EDGES = [1, 0, 63, 64, 65, 1, 130, 0]
+
+
+def _pkg():
+    import paper_2111_05972_amd as pkg
+    return pkg
+
+
+def _rows(seed, *shape, dtype, sigma=1.0):
+    g = torch.Generator().manual_seed(seed)
+    return (torch.randn(*shape, generator=g) * sigma).to(dtype).cuda()
+
+
+class Batch:
+    """A packed batch with its plan and workspace; rows behind the last sequence hold `behind`."""
+
+    def __init__(self, lengths, nq, nkv, dh, causal, dtype, behind=0, seed=0, fill=math.nan):
+        pkg = _pkg()
+        self.pkg, self.dt = pkg, pkg.TPL_BF16 if dtype == torch.bfloat16 else pkg.TPL_F32
+        self.offsets = [0]
+        for n in lengths:
+            self.offsets.append(self.offsets[-1] + n)
+        self.M, self.used = self.offsets[-1] + behind, self.offsets[-1]
+        self.dims = (self.dt, len(lengths), self.M, nq, nkv, dh, causal)
+        self.shape, self.dtype = (nq, nkv, dh, causal), dtype
+        self.qkv = _rows(seed, self.M, (nq + 2 * nkv) * dh, dtype=dtype)
+        self.d_o = _rows(seed + 1, self.M, nq * dh, dtype=dtype)
+        self.qkv[self.used:] = fill
+        self.d_o[self.used:] = fill
+        self.on_gpu = torch.tensor(self.offsets, dtype=torch.int32, device="cuda")
+        self.plan = torch.full((pkg.tp_layer_pack_plan_bytes(len(lengths), self.M, nq, nkv),), 255, dtype=torch.uint8, device="cuda")
+        self.ws = torch.full((max(pkg.tp_layer_attn_packed_workspace_bytes(*self.dims, b) for b in (0, 1)),), 255, dtype=torch.uint8, device="cuda")
+        self.o = torch.full((self.M, nq * dh), 7.0, dtype=dtype, device="cuda")
+        self.lse = torch.full((self.M, nq), 7.0, device="cuda")
+        self.dsum = torch.empty(self.M, nq, device="cuda")
+        self.dqkv = torch.full_like(self.qkv, 7.0)
+
+    def make_plan(self):
+        self.pkg.tp_layer_pack_plan(self.dims[1], self.M, self.on_gpu, *self.dims[3:5], self.dims[6], self.plan, stream=torch.cuda.current_stream())
+
+    def run(self):
+        st = torch.cuda.current_stream()
+        self.pkg.tp_layer_attn_packed_fwd(*self.dims, self.plan, self.qkv, self.o, self.lse, self.ws, stream=st)
+        self.pkg.tp_layer_attn_packed_bwd(*self.dims, self.plan, self.qkv, self.o, self.lse, self.d_o, self.dqkv, self.dsum, self.ws, stream=st)
+
+    def outputs(self):
+        return {"o": self.o, "lse": self.lse, "dqkv": self.dqkv}
+
+    def check(self):
+        nq, nkv, dh, causal = self.shape
+        val, tol = ref.attention(self.qkv, self.offsets, nq, nkv, dh, causal, self.d_o)
+        for k, x in self.outputs().items():
+            ref.check(x, val[k], tol[k], k)
+            assert (x[self.used:] == 7.0).all(), f"{k}: rows behind the last sequence"
+
+
+def _run(*args, **kw):
+    b = Batch(*args, **kw)
+    b.make_plan()
+    b.run()
+    torch.cuda.synchronize()
+    b.check()
+    return b
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("nq,nkv", [(2, 2), (6, 2), (8, 1)])
+@pytest.mark.parametrize("dh", [64, 128, 80])
+def test_edges(dh, nq, nkv, causal):
+    _run(EDGES, nq, nkv, dh, causal, torch.bfloat16, behind=3)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("dh", [8, 32, 40, 96, 104])
+def test_head_sizes(dh, dtype):
+    _run([33, 1, 100], 5, 1, dh, True, dtype, behind=1)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("nq,nkv,dh", [(2, 2, 64), (6, 2, 64), (3, 1, 128)])
+def test_float(dh, nq, nkv, causal):
+    _run(EDGES, nq, nkv, dh, causal, torch.float32, behind=3)
+
+
+@pytest.mark.parametrize("lengths,nq", [([1], 1), ([1], 128), ([2, 1, 1, 3], 7), ([0, 0, 5], 2), ([1] * 70, 3), ([17] * 40, 4)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_few_tokens(lengths, nq, dtype):
+    _run(lengths, nq, 1, 64, True, dtype)
+
+
+# strips long enough to be cut on both sides: in chunks of 16 tiles and a shorter last one
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dtype,dh,nq", [(torch.bfloat16, 128, 1), (torch.bfloat16, 64, 3), (torch.bfloat16, 80, 2), (torch.float32, 64, 2), (torch.float32, 32, 1)])
+def test_cut_strips(dtype, dh, nq, causal):
+    _run([2300, 5, 700], nq, 1, dh, causal, dtype, behind=2)
+
+
+def test_results_do_not_change_from_run_to_run():
+    b = _run([1500, 3, 800], 4, 2, 64, True, torch.bfloat16)
+    first = {k: x.clone() for k, x in b.outputs().items()}
+    for _ in range(3):
+        b.make_plan()
+        b.run()
+        assert all(torch.equal(x, first[k]) for k, x in b.outputs().items())
+
+
+def test_positions_begin_the_plan():
+    b = Batch([3, 0, 70, 1], 2, 1, 64, True, torch.bfloat16, behind=4)
+    b.make_plan()
+    want = [i for n in (3, 0, 70, 1) for i in range(n)] + [0] * 4
+    assert b.plan.view(torch.int32)[:b.M].tolist() == want
+
+
+# What a mask hides is as if it were not there: later tokens of the sequence under the causal mask, other sequences, rows of none.
+@pytest.mark.parametrize("dtype,dh", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_hidden_values_do_not_matter(dtype, dh, bad):
+    nq, nkv, cut = 4, 2, 40
+    b = Batch([70, 90], nq, nkv, dh, True, dtype, behind=2)
+    val, tol = ref.attention(b.qkv, b.offsets, nq, nkv, dh, True, b.d_o)
+    b.qkv.view(b.M, nq + 2 * nkv, dh)[cut:70, nq:] = bad             # K and V of the first sequence's later tokens
+    b.make_plan()
+    b.run()
+    for k in ("o", "lse"):
+        ref.check(b.outputs()[k][:cut], val[k][:cut], tol[k][:cut], k)
+    for k, x in b.outputs().items():
+        ref.check(x[70:160], val[k][70:160], tol[k][70:160], k)
+
+
+# Backward: a query that does not see a key leaves it alone, whatever its dO and Q hold.
+@pytest.mark.parametrize("dtype,dh", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+def test_hidden_queries_do_not_matter(dtype, dh):
+    cut = 40
+    b = Batch([70, 5], 2, 1, dh, True, dtype)
+    val, tol = ref.attention(b.qkv, b.offsets, 2, 1, dh, True, b.d_o)
+    b.d_o[:cut] = math.inf
+    b.qkv.view(b.M, 4, dh)[:cut, :2] = math.nan
+    b.make_plan()
+    b.run()
+    ref.check(b.dqkv[cut:75], val["dqkv"][cut:75], tol["dqkv"][cut:75], "dqkv")   # keys that no spoilt query sees, and their own queries
+
+
+def test_offsets_that_decrease_stay_in_bounds():
+    b = Batch([40, 30, 30], 2, 1, 64, True, torch.bfloat16)
+    b.on_gpu = torch.tensor([-5, 60, 20, 1000], dtype=torch.int32, device="cuda")      # taken as 0, 60, 60, 100
+    b.make_plan()
+    b.run()
+    b.offsets = [0, 60, 60, 100]
+    b.check()
+
+
+def test_another_plan_writes_nothing():
+    b = Batch([40, 30], 2, 1, 64, True, torch.bfloat16)
+    other = Batch([40, 30], 2, 1, 64, False, torch.bfloat16)
+    other.make_plan()
+    b.plan = other.plan
+    b.run()
+    assert all((x == 7.0).all() for x in b.outputs().values())
+
+
+# A captured step follows the offsets that a replay finds, also between the program's own eager work.
+def test_graph_follows_the_offsets():
+    b = Batch([100, 60, 40], 4, 2, 64, True, torch.bfloat16)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        b.make_plan()
+        b.run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        b.make_plan()
+        b.run()
+    for lengths in ([100, 60, 40], [1, 198, 1], [0, 77, 123], [100, 60, 40]):
+        b.offsets = [0, lengths[0], lengths[0] + lengths[1], sum(lengths)]
+        b.on_gpu.copy_(torch.tensor(b.offsets, dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = {k: x.clone() for k, x in b.outputs().items()}
+        b.check()
+        b.make_plan()
+        b.run()
+        assert all(torch.equal(x, got[k]) for k, x in b.outputs().items())
+
+
+def test_two_batches_on_two_streams():
+    a, b = Batch([300, 20], 4, 2, 64, True, torch.bfloat16), Batch([50, 400], 2, 1, 128, False, torch.bfloat16, seed=5)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for s, x in zip(streams, (a, b)):
+        with torch.cuda.stream(s):
+            x.make_plan()
+            x.run()
+    torch.cuda.synchronize()
+    a.check()
+    b.check()
+
+
+# dQ, dK, dV against differences of the forward pass in float
+def test_gradient_against_differences():
+    nq, nkv, dh, lengths = 2, 1, 8, [5, 3]
+    b = Batch(lengths, nq, nkv, dh, True, torch.float32)
+    b.make_plan()
+    b.run()
+    x, step = b.qkv.clone(), 2.0 ** -6
+    d_o = b.d_o.double()
+
+    def value(qkv):
+        b.pkg.tp_layer_attn_packed_fwd(*b.dims, b.plan, qkv, b.o, b.lse, b.ws, stream=torch.cuda.current_stream())
+        return (b.o.double() * d_o).sum().item()
+    for i, j in [(0, 0), (2, 3), (4, 17), (3, 25), (5, 9), (7, 30), (6, 20)]:
+        f = []
+        for k in (1, -1, 2, -2):
+            y = x.clone()
+            y[i, j] += k * step
+            f.append(value(y))
+        diff = (8 * (f[0] - f[1]) - (f[2] - f[3])) / (12 * step)
+        # fifth derivative times step^4 / 30 (softmax of unit values: below 100), and the float outputs' rounding over the step
+        tol = 100 * step ** 4 / 30 + 64 * ref.F32 * float((b.o.double().abs() * d_o.abs()).sum()) / step
+        assert abs(diff - b.dqkv[i, j].item()) <= tol, (i, j)
