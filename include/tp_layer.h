@@ -319,23 +319,23 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
  * (lengths from 0 on); query head h reads key and value head h / (nq / nkv); causal: query i of a sequence sees its keys j <= i, otherwise
  * all of its sequence, never another.
  *   qkv [M, (nq + 2 nkv) dh] -> o [M, nq dh], lse [M, nq] float (natural log of the sum of exp(q . k / sqrt(dh)))
- * Rows that belong to no sequence (behind the last one) are neither read nor written; their d_scratch may be.  A masked value is as if it
+ * Rows that belong to no sequence (behind the last one) are neither read nor written.  A masked value is as if it
  * were not there, infinities and NaN among them.  dh: a multiple of 8 up to 128; at most 128 query heads to a key head.
  *
  * The plan: tp_layer_pack_plan_bytes() of device memory that tp_layer_pack_plan fills on the stream from offsets (int32
  * [sequences + 1], device memory, offsets[0] = 0, not decreasing, the last at most M), once for a batch; every layer's calls with the same
  * (sequences, M, nq, nkv, causal) read it.  It begins with the position of every row in its sequence, int32 [M] (0 behind the last one),
  * which the rotary entry points take.  Offsets are on the device, so they cannot be refused: a decreasing one is taken as the largest
- * before it, and they end at 0 and M.  A call with another plan than its own (tokens, heads or mask differ) writes nothing.
+ * before it, and they end at 0 and M.  A call with another plan than its own (sequences, tokens, heads or mask differ) writes nothing.
  * tp_layer_pack_plan may be captured into a graph, which then follows the offsets that its replays find.
  * ws: at least tp_layer_attn_packed_workspace_bytes(..., bwd); d_scratch: [M, nq] float.  Results are deterministic. */
 size_t tp_layer_pack_plan_bytes(int64_t sequences, int64_t M, int nq, int nkv);
 int tp_layer_pack_plan(int64_t sequences, int64_t M, const int32_t* offsets, int nq, int nkv, int causal, void* plan, size_t plan_bytes,
                        void* hip_stream);
 size_t tp_layer_attn_packed_workspace_bytes(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, int bwd);
-int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan,
+int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, size_t plan_bytes,
                              const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
-int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan,
+int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, size_t plan_bytes,
                              const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, float* d_scratch,
                              void* ws, size_t ws_bytes, void* hip_stream);
 

@@ -6,7 +6,7 @@
 // by the rows r >= j G.  A block of 128 rows is then full where there are short sequences and many heads to a key head, crosses a
 // short piece of the diagonal, and dK, dV of a key head need no sum over heads besides the one over rows.
 //
-// Plan (device memory, 32-bit words): positions [M], a header, offsets of the sequences, block counts, and lists of work items.
+// Plan (device memory, 32-bit words): positions [M], keys that a token sees [M] (0: it is in no sequence), a header, offsets of the sequences, block counts, and lists of work items.
 // A strip is a block of 128 rows (forward, dQ) or 128 keys (dK, dV) of a sequence with the 64-row tiles that it visits on the other
 // side.  Strips much longer than a compute unit's share of all tiles are cut into chunks, each an item of its own that leaves float
 // sums in a slot of the workspace, and joined in chunk order by another kernel.  Lists are ordered by length, longest first (what
@@ -21,7 +21,7 @@ namespace tpl {
 
 constexpr int PACK_BLK = 128, PACK_TILE = 64;
 constexpr int PACK_MAX_GROUP = 128;
-constexpr int PACK_MIN_CHUNK = 16;        // tiles; shorter chunks cost more in their ends than they save
+constexpr int PACK_MIN_CHUNK = 8;         // tiles; shorter chunks cost more in their ends than they save
 
 struct PackItem {
     int t0, len;           // the sequence: first row of the batch, length
@@ -35,43 +35,48 @@ struct PackHeader {
     int sequences, tokens, nq, nkv, causal;
     int items[2];          // [0]: forward and dQ, [1]: dK, dV
     int joins[2];          // strips that were cut
-    int pad[7];
+    int first_short;       // strips of one or two tiles of list 0 are items from here on (longer ones may be among them)
+    int pad[6];
 };
 // Word offsets of the plan's parts; a function of what the host knows, so host and device agree without a copy.
 struct PackLayout {
-    int64_t header, start, pre[2], items[2], joins[2], words;
-    int64_t cap[2];        // items, also the slots
-    int64_t join_cap;
+    int64_t seen, header, start, pre[2], items[2], joins[2], words;
+    int64_t cap[2], join_cap[2];
 };
 inline int64_t pack_up(int64_t x) { return (x + 63) / 64 * 64; }
-// `share_cap`: how many chunks of the average share there can be (pack_shares), 0: nothing is cut
-inline PackLayout pack_layout(int64_t sequences, int64_t M, int64_t nq, int64_t nkv, int64_t share_cap) {
+// Shares[side]: all tiles of a launch, per key head, are cut into that many of the average length at most (0: nothing is cut).
+struct PackShares { int64_t of[2]; };
+inline PackLayout pack_layout(int64_t sequences, int64_t M, int64_t nq, int64_t nkv, const PackShares& shares) {
     PackLayout L;
     const int64_t G = nq / nkv;
-    L.cap[0] = (M * G) / PACK_BLK + sequences + share_cap;      // a strip of n tiles has at most n / chunk + 1 chunks
-    L.cap[1] = M / PACK_BLK + sequences + share_cap;
-    L.join_cap = share_cap;                                     // strips longer than a chunk
     int64_t w = pack_up(M);
+    L.seen = w; w += pack_up(M);
     L.header = w; w += pack_up(sizeof(PackHeader) / 4);
     L.start = w; w += pack_up(sequences + 1);
-    for (int s = 0; s < 2; ++s) { L.pre[s] = w; w += pack_up(sequences + 1); }
-    for (int s = 0; s < 2; ++s) { L.items[s] = w; w += pack_up(L.cap[s] * 8); }
-    for (int s = 0; s < 2; ++s) { L.joins[s] = w; w += pack_up(L.join_cap * 8); }
+    for (int s = 0; s < 2; ++s) {
+        L.cap[s] = M * (s == 0 ? G : 1) / PACK_BLK + sequences + shares.of[s];      // a strip of n tiles has less than n / chunk + 1 chunks
+        L.join_cap[s] = shares.of[s];                                               // strips longer than a chunk
+        L.pre[s] = w; w += pack_up(sequences + 1);
+        L.items[s] = w; w += pack_up(L.cap[s] * 8);
+        L.joins[s] = w; w += pack_up(L.join_cap[s] * 8);
+    }
     L.words = w;
     return L;
 }
-// Compute units' shares of the launch's tiles, per key head: a chunk is no shorter than all tiles divided by this.  Two shares to a
-// unit, so that one that gets a long item early gets fewer later.  None where no strip can have twice the shortest chunk.
-inline int64_t pack_shares(int64_t M, int64_t nq, int64_t nkv, int units) {
-    if (M * (nq / nkv) < (int64_t)2 * PACK_MIN_CHUNK * PACK_TILE) return 0;
-    return (2 * units + nkv - 1) / nkv;
+// A chunk is no shorter than what a compute unit would have of all tiles if they were spread evenly, one workgroup to a unit: twice and four times
+// as many shares took 320, 330 and 351 us instead of 314 backward (12 documents of 8192 tokens, 16 / 2 heads of 128), 88, 92 and 110 instead of 87
+// forward, in sums written and read.  None where no strip can have two of the shortest chunks.
+inline PackShares pack_shares(int64_t M, int64_t nq, int64_t nkv, int units) {
+    if (M * (nq / nkv) < (int64_t)2 * PACK_MIN_CHUNK * PACK_TILE) return PackShares{{0, 0}};
+    const int64_t each = (units + nkv - 1) / nkv;
+    return PackShares{{each, each}};
 }
 
 #ifdef __HIPCC__
 __device__ __forceinline__ const PackItem* pack_items(const int* plan, int64_t at) { return reinterpret_cast<const PackItem*>(plan + at); }
 // Whether the plan at hand was made for this call.
-__device__ __forceinline__ bool pack_matches(const PackHeader* h, int tokens, int nq, int nkv, int causal) {
-    return h->tokens == tokens && h->nq == nq && h->nkv == nkv && h->causal == causal;
+__device__ __forceinline__ bool pack_matches(const PackHeader* h, int sequences, int tokens, int nq, int nkv, int causal) {
+    return h->sequences == sequences && h->tokens == tokens && h->nq == nq && h->nkv == nkv && h->causal == causal;
 }
 #endif
 

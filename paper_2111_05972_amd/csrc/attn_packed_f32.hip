@@ -350,6 +350,11 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
     }
 }
 
+__global__ __launch_bounds__(256) void attn_packed_f32_dsum_kernel(FParams p) {
+    if (pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p.sequences, p.M, p.nq, p.nkv, p.causal))
+        dsum_rows(p, (int64_t)blockIdx.x * 16, (int64_t)gridDim.x * 16, 0);
+}
+
 // Two workgroups share a compute unit up to head size 64 (see attn_f32.hip); wider heads need more than 256 registers.
 template <int DH>
 __global__ __launch_bounds__(256, DH <= 64 ? 2 : 1) void attn_packed_f32_bwd_kernel(FParams p) {
@@ -369,26 +374,25 @@ hipError_t run(const PackAttnArgs& a, bool bwd) {
     static const hipError_t attr_f = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_fwd_kernel<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     static const hipError_t attr_b = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_bwd_kernel<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr_f != hipSuccess || attr_b != hipSuccess) return attr_f != hipSuccess ? attr_f : attr_b;
-    const int64_t shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
+    const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
     const PackLayout L = pack_layout(a.sequences, a.M, a.nq, a.nkv, shares);
     FParams p = make_params<float>(a, L);
     p.part[0] = (float*)a.ws;
-    const dim3 join((unsigned)(L.join_cap * JOIN_WGS * a.nkv), bwd ? 3 : 1);
+    const dim3 join(join_wgs(L, a.nkv));
     hipError_t e;
     if (!bwd) {
         hipLaunchKernelGGL(attn_packed_f32_fwd_kernel<DH>, dim3((unsigned)(L.cap[0] * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
-        if ((e = hipGetLastError()) != hipSuccess || shares == 0) return e;
-        hipLaunchKernelGGL((attn_packed_fwd_join_kernel<float, DH>), join, dim3(256), 0, a.stream, p);
+        if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
+        hipLaunchKernelGGL((attn_packed_fwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
         return hipGetLastError();
     }
     p.part[1] = (float*)((char*)a.ws + ws_of(a, true).part[0]);
-    const int64_t rows = a.M * a.nq;
-    hipLaunchKernelGGL(attn_packed_dsum_kernel<float>, dim3((unsigned)((rows + 15) / 16)), dim3(256), 0, a.stream, (const float*)a.o, (const float*)a.d_o, a.dsum, rows, a.dh);
+    hipLaunchKernelGGL(attn_packed_f32_dsum_kernel, dim3((unsigned)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units())), dim3(256), 0, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     p.kv_wgs = (int)(L.cap[1] * a.nkv);
     hipLaunchKernelGGL(attn_packed_f32_bwd_kernel<DH>, dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
-    if ((e = hipGetLastError()) != hipSuccess || shares == 0) return e;
-    hipLaunchKernelGGL((attn_packed_bwd_join_kernel<float, DH>), join, dim3(256), 0, a.stream, p);
+    if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
+    hipLaunchKernelGGL((attn_packed_bwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
 }  // namespace

@@ -16,22 +16,32 @@ namespace {
 constexpr int PLAN_THREADS = 1024;
 constexpr int BUCKETS = 1024;
 
-// Inclusive scan over the workgroup: sum, or maximum.
-template <bool MAX> __device__ int block_scan(int v, int* tmp) {
-    const int t = threadIdx.x;
-    tmp[t] = v;
-    __syncthreads();
-    for (int d = 1; d < PLAN_THREADS; d *= 2) {
-        const int o = t >= d ? tmp[t - d] : (MAX ? -1 : 0);
-        __syncthreads();
-        tmp[t] = MAX ? max(tmp[t], o) : tmp[t] + o;
-        __syncthreads();
+// Inclusive scan over the workgroup, sum or maximum, by wavefronts and then over their totals; total: of all.
+template <bool MAX> __device__ __forceinline__ int join(int a, int b) { return MAX ? max(a, b) : a + b; }
+template <bool MAX> __device__ int block_scan(int v, int* tmp, int& total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(v, d, 64);
+        if (lane >= d) v = join<MAX>(v, o);
     }
-    return tmp[t];
+    __syncthreads();                                               // the scan before has been read
+    if (lane == 63) tmp[wave] = v;
+    __syncthreads();
+    int before = MAX ? -1 : 0;
+    total = before;
+#pragma unroll
+    for (int w = 0; w < PLAN_THREADS / 64; ++w) {
+        const int o = tmp[w];
+        if (w < wave) before = join<MAX>(before, o);
+        total = join<MAX>(total, o);
+    }
+    return join<MAX>(v, before);
 }
 
 struct PlanParams {
-    int n, M, nq, nkv, causal, shares;
+    int n, M, nq, nkv, causal;
+    PackShares shares;
     const int* offsets;
     int* plan;
     PackLayout L;
@@ -53,26 +63,29 @@ __device__ __forceinline__ void strip_of(const PlanParams& p, int side, int len,
 }
 
 __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
-    __shared__ int tmp[PLAN_THREADS];
+    __shared__ int tmp[PLAN_THREADS / 64];
     __shared__ int hist[2][BUCKETS];
-    __shared__ int longest[2], slots[2], joins[2];
+    __shared__ int longest[2], slots[2], joins[2], first_short;
     __shared__ unsigned long long tiles[2];
     const int t = threadIdx.x, G = p.nq / p.nkv;
     int* start = p.plan + p.L.start;
     auto offset = [&](int i) { return min(max(p.offsets[i], 0), p.M); };
     if (blockIdx.x > 0) {
-        // Positions: this workgroup's tokens, each looking for its sequence among the offsets.  Where these decrease the running
-        // maximum would be needed: the lists of workgroup 0 do not read positions, so a wrong one is no more than that.
+        // This workgroup's tokens, each looking for its sequence among the offsets.  Where these decrease, their running maximum would be
+        // needed: the lists do not come from here, so what is wrong then is a position, or how exactly a row's D is summed.
         for (int64_t m = (int64_t)(blockIdx.x - 1) * PLAN_THREADS + t; m < p.M; m += (int64_t)(gridDim.x - 1) * PLAN_THREADS) {
             int lo = 0, hi = p.n;                                  // the last i with offset(i) <= m
             while (lo < hi) {
                 const int mid = (lo + hi + 1) >> 1;
                 if (offset(mid) <= m) lo = mid; else hi = mid - 1;
             }
-            p.plan[m] = lo < p.n && offset(lo) <= m ? (int)m - offset(lo) : 0;
+            const bool in = lo < p.n && offset(lo) <= m;
+            p.plan[m] = in ? (int)m - offset(lo) : 0;
+            p.plan[p.L.seen + m] = !in ? 0 : p.causal ? (int)m - offset(lo) + 1 : offset(lo + 1) - offset(lo);
         }
         return;
     }
+    if (t == 0) first_short = 0;
     if (t < 2) { longest[t] = 0; slots[t] = 0; joins[t] = 0; tiles[t] = 0; }
     for (int i = t; i < 2 * BUCKETS; i += PLAN_THREADS) (&hist[0][0])[i] = 0;
     __syncthreads();
@@ -80,11 +93,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     int carry_max = 0, carry[2] = {0, 0};
     for (int base = 0; base <= p.n; base += PLAN_THREADS) {
         const int i = base + t;
-        const int c = max(block_scan<true>(i <= p.n ? offset(i) : 0, tmp), carry_max);
+        int all;
+        const int c = max(block_scan<true>(i <= p.n ? offset(i) : 0, tmp, all), carry_max);
         if (i <= p.n) start[i] = c;
-        __syncthreads();
-        carry_max = max(carry_max, tmp[PLAN_THREADS - 1]);
-        __syncthreads();
+        carry_max = max(carry_max, all);
     }
     __threadfence_block();
     __syncthreads();
@@ -94,11 +106,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         for (int side = 0; side < 2; ++side) {
             const int64_t rows = side == 0 ? (int64_t)len * G : len;
             const int blocks = (int)((rows + PACK_BLK - 1) / PACK_BLK);
-            const int pre = block_scan<false>(blocks, tmp) + carry[side];
+            int all;
+            const int pre = block_scan<false>(blocks, tmp, all) + carry[side];
             if (i <= p.n) (p.plan + p.L.pre[side])[i] = pre - blocks;
-            __syncthreads();
-            carry[side] += tmp[PLAN_THREADS - 1];
-            __syncthreads();
+            carry[side] += all;
         }
     }
     __threadfence_block();
@@ -129,7 +140,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     for (int side = 0; side < 2; ++side) {
         const int* pre = p.plan + p.L.pre[side];
         int chunk = 1 << 30;
-        if (p.shares > 0) chunk = max(PACK_MIN_CHUNK, (int)((tiles[side] + p.shares - 1) / p.shares));
+        if (p.shares.of[side] > 0) chunk = max(PACK_MIN_CHUNK, (int)((tiles[side] + p.shares.of[side] - 1) / p.shares.of[side]));
         const int top = min(longest[side], chunk) + 1;
         PackItem* items = reinterpret_cast<PackItem*>(p.plan + p.L.items[side]);
         PackItem* join = reinterpret_cast<PackItem*>(p.plan + p.L.joins[side]);
@@ -156,7 +167,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                     it.slot = slot;
                     it.tile0 = a;
                     it.tile1 = z;
-                    if (j < p.L.join_cap) join[j] = it;
+                    if (j < p.L.join_cap[side]) join[j] = it;
                 }
                 for (int c = 0; c < it.chunks; ++c) {
                     it.slot = slot < 0 ? -1 : slot + c;
@@ -167,17 +178,18 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
             }
             __syncthreads();
             if (pass == 0) {                                       // counts -> first places
-                const int v = hist[side][t], before = block_scan<false>(v, tmp) - v;
-                __syncthreads();
+                int all;
+                const int v = hist[side][t], before = block_scan<false>(v, tmp, all) - v;
                 hist[side][t] = before;
+                if (side == 0 && t == BUCKETS - 1 - 2 * (BUCKETS - 1) / top) first_short = before;
                 __syncthreads();
             }
         }
         if (t == 0) {
             PackHeader* h = reinterpret_cast<PackHeader*>(p.plan + p.L.header);
             h->items[side] = min(hist[side][BUCKETS - 1], (int)p.L.cap[side]);   // the end of the last bucket
-            h->joins[side] = min(joins[side], (int)p.L.join_cap);
-            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->causal = p.causal; }
+            h->joins[side] = min(joins[side], (int)p.L.join_cap[side]);
+            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->causal = p.causal; h->first_short = first_short; }
         }
     }
 }
@@ -189,7 +201,7 @@ size_t attn_packed_workspace_bytes(const PackAttnArgs& a, bool bwd) { return ws_
 hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int causal, int* plan, hipStream_t s) {
     PlanParams p{};
     p.n = (int)sequences; p.M = (int)M; p.nq = nq; p.nkv = nkv; p.causal = causal;
-    p.shares = (int)pack_shares(M, nq, nkv, compute_units());
+    p.shares = pack_shares(M, nq, nkv, compute_units());
     p.offsets = offsets; p.plan = plan;
     p.L = pack_layout(sequences, M, nq, nkv, p.shares);
     static_assert(BUCKETS == PLAN_THREADS, "a thread to a bucket");

@@ -141,6 +141,10 @@ struct EpilogueLane {
             unpack8(KIND == KIND_DGELU ? in : *reinterpret_cast<const uint4*>(p.aux + idx), u8);
 #pragma unroll
             for (int e = 0; e < 8; ++e) v8[e] *= gelu_grad_f(u8[e]);
+        } else if (KIND == KIND_ANY && p.epi == EPI_SCALE) {
+            const float alpha = *p.alpha;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v8[e] *= alpha;
         }
         const uint4 out = pack8(v8);
         if (p.nt_store) {
@@ -893,6 +897,10 @@ __device__ __forceinline__ void sum_shares(const GemmParams& p, int shares, int6
         unpack8(*reinterpret_cast<const uint4*>(p.aux + idx), u8);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v8[e] *= gelu_grad_f(u8[e]);
+    } else if (p.epi == EPI_SCALE) {
+        const float alpha = *p.alpha;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v8[e] *= alpha;
     }
     *reinterpret_cast<uint4*>(p.C + idx) = pack8(v8);
 }
@@ -1706,7 +1714,7 @@ static GemmParams gemm_params(const GemmArgs& a) {
     p.M = (int)a.M; p.N = (int)a.N; p.K = (int)a.K;
     p.nt_store = a.c_streaming ? 1 : 0;
     p.lda = a.lda ? (int)a.lda : a.trans_a ? (int)a.M : (int)a.K;
-    p.acc = a.acc; p.acc_mode = a.acc_mode;
+    p.acc = a.acc; p.acc_mode = a.acc_mode; p.alpha = a.alpha;
     p.ldb = a.trans_b ? (int)a.K : (int)a.N;
     p.epi = a.epi;
     p.tiles_m = p.tiles_n = 0;
@@ -1839,7 +1847,7 @@ GroupPlan make_pp_plan(const GemmArgs* g, int n, const GroupTile& gt, double lim
         }
         return m;
     };
-    auto length = [&](int i, int steps, bool whole) { return steps * gt.step_us + gt.wg_us + (whole && g[i].epi != EPI_NONE ? gt.gelu_us : 0.0); };
+    auto length = [&](int i, int steps, bool whole) { return steps * gt.step_us + gt.wg_us + (whole && (g[i].epi == EPI_GELU || g[i].epi == EPI_DGELU) ? gt.gelu_us : 0.0); };
     // What a plan cannot take less than, GEMM by GEMM: its longest job and its work over all units, unless list_time takes whole rounds of a
     // job at once behind longer ones (it may come out below the work then), and the sums of the shares.
     struct Bound {
@@ -2181,7 +2189,7 @@ static hipError_t launch_pp_jobs(const GroupPlan& pl, const GemmArgs* g, int n, 
 
 static hipError_t launch_pp(const GroupPlan& pl, const GemmArgs* g, int n, void* ws, size_t ws_bytes, hipStream_t stream) {
     const GroupTile& t = GROUP_TILES[pl.tile];
-    if (any_acc(g, n))
+    if (g[0].epi == EPI_SCALE)
         return t.bn == 128 ? launch_pp_jobs<PPTile<4, 1>, true>(pl, g, n, ws, ws_bytes, stream) : launch_pp_jobs<PPTile<2, 2>, true>(pl, g, n, ws, ws_bytes, stream);
     return t.bn == 128   ? launch_pp_jobs<PPTile<4, 1>>(pl, g, n, ws, ws_bytes, stream)
            : t.bm == 128 ? launch_pp_jobs<PPTile<2, 1>>(pl, g, n, ws, ws_bytes, stream)

@@ -18,7 +18,7 @@ typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4_ptr;
 
-enum EpiKind { KIND_PARTIAL, KIND_PLAIN, KIND_RESID, KIND_GELU, KIND_DGELU, KIND_ANY, KIND_ACC };
+enum EpiKind { KIND_PARTIAL, KIND_PLAIN, KIND_RESID, KIND_GELU, KIND_DGELU, KIND_ANY, KIND_ACC, KIND_SCALE };
 
 constexpr int DK = 32;                      // k per stage
 constexpr unsigned OOB_OFFSET = 0xFFFFFFF0u;   // beyond any buffer this kernel accepts
@@ -39,6 +39,7 @@ struct GemmParams {
     float* colsum_part;    // with K split: [share][N], the same sums of one share; gemm_group_sum_kernel adds them
     float* acc;            // running sums that this product is added to (see GemmArgs), else null
     int acc_mode;
+    const float* alpha;    // EPI_SCALE
 };
 
 // Which K share a workgroup computes.  The workgroup list is share-major (all tiles of share 0, then all

@@ -129,6 +129,7 @@ __device__ __forceinline__ int pp_wave() { return __builtin_amdgcn_readfirstlane
 struct PPLane {
     int row, col[2];
     bool odd;                         // the blocks of a pair hold their column groups in swapped order in odd lane groups
+    float alpha;                      // KIND_SCALE, KIND_ACC
     float bias[16];
 };
 template <typename TL>
@@ -154,21 +155,29 @@ __device__ __forceinline__ uint4 pp_fetch(const GemmParams& p, int row, int col)
         v = *reinterpret_cast<const uint4*>((KIND == KIND_RESID ? p.resid : p.aux) + (int64_t)row * p.N + col);
     return v;
 }
+// KIND_SCALE: alpha v; KIND_ACC: v is added to running sums, and the last time alpha times those are stored.
+template <int KIND>
+__device__ __forceinline__ void pp_emit_scaled(const GemmParams& p, int row, int col, float (&v)[8], float alpha) {
+    if (row >= p.M || col >= p.N) return;
+    const int64_t idx = (int64_t)row * p.N + col;
+    if (KIND == KIND_ACC && (p.acc_mode & ACC_ADD)) {
+        float r8[8];
+        load8(p.acc + idx, r8);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] += r8[e];
+    }
+    if (KIND == KIND_ACC && !(p.acc_mode & ACC_LAST)) {
+        store8(p.acc + idx, v);
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] *= alpha;
+    *reinterpret_cast<uint4*>(p.C + idx) = pack8(v);
+}
 template <int KIND>
 __device__ __forceinline__ void pp_emit(const GemmParams& p, int row, int col, float (&v)[8], const float* bias, const uint4& in) {
     if (row >= p.M || col >= p.N) return;
     const int64_t idx = (int64_t)row * p.N + col;
-    if constexpr (KIND == KIND_ACC) {
-        if (p.acc_mode & ACC_ADD) {
-            float r8[8];
-            load8(p.acc + idx, r8);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += r8[e];
-        }
-        if (p.acc_mode & ACC_LAST) *reinterpret_cast<uint4*>(p.C + idx) = pack8(v);
-        else store8(p.acc + idx, v);
-        return;
-    }
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] += bias[e];
     if (KIND == KIND_RESID || (KIND == KIND_ANY && p.resid)) {
@@ -204,7 +213,8 @@ __device__ __forceinline__ void pp_row_block(const GemmParams& p, const PPLane& 
             v[e] = el.odd ? x[2 * u + 1][e] : x[2 * u][e];
             v[4 + e] = el.odd ? x[2 * u][e] : x[2 * u + 1][e];
         }
-        pp_emit<KIND>(p, row, el.col[u], v, el.bias + 8 * u, in[u]);
+        if constexpr (KIND == KIND_ACC || KIND == KIND_SCALE) pp_emit_scaled<KIND>(p, row, el.col[u], v, el.alpha);
+        else pp_emit<KIND>(p, row, el.col[u], v, el.bias + 8 * u, in[u]);
     }
 }
 template <typename TL, int KIND>
@@ -252,17 +262,18 @@ __device__ __forceinline__ void pp_store_partial(const GemmParams& p, const PPAc
         pp_store_partial<TL, BLOCK + 1>(p, acc, row0, partial);
     }
 }
-// ACC: some GEMM of the launch adds to running sums (kernels of their own, so that the others stay as they are).
+// ACC: every GEMM of the launch is scaled, some add to running sums (kernels of their own, so that the others stay as they are).
 template <typename TL, bool ACC>
 __device__ __forceinline__ void pp_epilogue(const GemmParams& p, const PPAcc<TL>& acc, int m0, int n0, float* partial) {
     if (partial) {
         pp_store_partial<TL, 0>(p, acc, m0 + pp_wave() / TL::WN * 64, partial);
         return;
     }
-    const PPLane el = pp_lane<TL>(p, m0, n0);
+    PPLane el = pp_lane<TL>(p, m0, n0);
     if constexpr (ACC) {
+        el.alpha = *p.alpha;
         if (p.acc) pp_rows<TL, KIND_ACC>(p, acc, el);
-        else pp_rows<TL, KIND_PLAIN>(p, acc, el);
+        else pp_rows<TL, KIND_SCALE>(p, acc, el);
         return;
     }
     if (p.epi == EPI_NONE && !p.resid) pp_rows<TL, KIND_PLAIN>(p, acc, el);
@@ -277,7 +288,8 @@ __device__ __forceinline__ void pp_sum_rows(const GemmParams& p, const PPRun& r,
     int tm, tn;
     tile_coords(r.tile0 + local, p.tiles_m, p.tiles_n, p.band, tm, tn);
     const int m0 = tm * TL::BM, n0 = tn * TL::BN;
-    const PPLane el = pp_lane<TL>(p, m0, n0);
+    PPLane el = pp_lane<TL>(p, m0, n0);
+    if (ACC) el.alpha = *p.alpha;
     const int row = el.row + (block >> 2) * TL::A_ROWS + (block & 3) * 16;
     if (__builtin_amdgcn_readfirstlane(row - (int)(threadIdx.x & 15)) < p.M) {
         f32x4 x[4];
@@ -294,8 +306,12 @@ __device__ __forceinline__ void pp_sum_rows(const GemmParams& p, const PPRun& r,
             }
         }
         const uint4 none[2] = {};
-        if (ACC && p.acc) pp_row_block<KIND_ACC>(p, el, row, x, none);
-        else pp_row_block<KIND_ANY>(p, el, row, x, none);
+        if constexpr (ACC) {
+            if (p.acc) pp_row_block<KIND_ACC>(p, el, row, x, none);
+            else pp_row_block<KIND_SCALE>(p, el, row, x, none);
+        } else {
+            pp_row_block<KIND_ANY>(p, el, row, x, none);
+        }
     }
     const int col = n0 + (int)threadIdx.x;
     if (block == 0 && tm == 0 && p.colsum && threadIdx.x < TL::BN && col < p.N) {

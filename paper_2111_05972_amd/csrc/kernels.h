@@ -27,7 +27,7 @@ const Options& options();
 // name: "gemm_tile", "gemm_shares", "gemm_band", "gemm_force", "gemm_group", "attn_chunk", "fuse_colsum", "side_chains"; value null or "": back to unset.
 // Returns false for an unknown name or a value that does not parse.
 bool set_option(const char* name, const char* value);
-enum Epi { EPI_NONE = 0, EPI_GELU = 1, EPI_DGELU = 2 };
+enum Epi { EPI_NONE = 0, EPI_GELU = 1, EPI_DGELU = 2, EPI_SCALE = 3 };   // EPI_SCALE (bf16 groups): v times *alpha
 
 // C[M,N] = epi(opA(A) opB(B)); see tp_layer_gemm in tp_layer.h for the meaning of each field.
 struct GemmArgs {
@@ -53,6 +53,7 @@ struct GemmArgs {
     // bf16 groups: C is one of several products that are added up in float: acc [M,N] = what ACC_ADD takes in, C is written with ACC_LAST only
     float* acc;
     int acc_mode;
+    const float* alpha; // EPI_SCALE: device memory
 };
 enum { ACC_ADD = 1, ACC_LAST = 2 };
 

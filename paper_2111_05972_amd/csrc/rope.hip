@@ -19,9 +19,14 @@ constexpr int ROPE_LDS_PAIRS = 4096;    // (token, pair) values of a workgroup a
 
 struct RopeParams {
     int64_t M, seq;
-    int heads, turned, dh, rot, adjacent, in_place, tokens;   // heads of a row, of which the first `turned` are turned; tokens of a workgroup
+    int heads, turned, dh, rot;           // heads of a row, of which the first `turned` are turned
+    int tokens;                           // of a workgroup
+    // Units of work, E elements or a pair of E elements: of a turned head (pairs, then what is copied), of a row.
+    int turn_units, head_units, row_units;
+    unsigned div_head;                    // u / head_units = u * div_head >> 31
+    int next_token, next_unit;            // RT units further
     const double* freq;
-    float factor, back;                                       // back: -1 in backward
+    float factor, back;                   // back: -1 in backward
     const int* pos;
 };
 
@@ -34,73 +39,89 @@ template <typename T, int E> __device__ __forceinline__ void store_e(T* p, const
     if constexpr (E == 8) store8(p, v);
     else p[0] = from_f32<T>(v[0]);
 }
+// Where a unit lies: element offsets of its two places (the same where there is one), its first pair, -1: copied.
+struct Place { int64_t a, b; int pair; };
 
-// A unit of a head: E pairs (their 2 E elements; E / 2 pairs where neighbours are pairs and E is 8), or E elements that are copied.
+// A thread takes every RT-th unit of its workgroup's tokens, AHEAD of them at a time: their loads go out before the first is used, those of
+// the first ones before the angles are worked out.
 template <typename T, int E, bool ADJ>
 __global__ __launch_bounds__(RT) void rope_kernel(RopeParams p, const T* in, T* out) {
     extern __shared__ float2 cs[];
+    constexpr int AHEAD = 4;
+    constexpr int STEP = ADJ && E == 1 ? 2 : E;               // elements of a turned unit in one place
+    constexpr bool TWO = !(ADJ && E == 8);                    // a turned unit lies in two places
+    constexpr int PAIRS = ADJ && E == 8 ? 4 : E;              // of a turned unit
     const int t = threadIdx.x, pairs = p.rot / 2;
-    const int64_t m0 = (int64_t)blockIdx.x * p.tokens;
+    const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.heads * p.dh;
     const int tokens = (int)(p.M - m0 < p.tokens ? p.M - m0 : p.tokens);
+    int token = t / p.row_units, unit = t - token * p.row_units;
+    Place at[AHEAD];
+    int of[AHEAD];                                            // token, or past the last
+    float x[AHEAD][E], y[AHEAD][E];
+    auto request = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            of[j] = token;
+            if (token < tokens) {
+                const int h = (int)(((uint64_t)(unsigned)unit * p.div_head) >> 31);
+                Place q;
+                if (h < p.turned) {
+                    const int u = unit - h * p.head_units;
+                    const bool copy = u >= p.turn_units;
+                    q.a = (m0 + token) * row + (int64_t)h * p.dh + (copy ? p.rot + (u - p.turn_units) * E : u * STEP);
+                    q.pair = copy ? -1 : u * PAIRS;
+                    q.b = q.a + (copy ? 0 : ADJ ? 1 : pairs);
+                } else {
+                    q.a = q.b = (m0 + token) * row + (int64_t)p.turned * p.dh + (int64_t)(unit - p.turned * p.head_units) * E;
+                    q.pair = -1;
+                }
+                at[j] = q;
+                load_e<T, E>(in + q.a, x[j]);
+                if (TWO && q.pair >= 0) load_e<T, E>(in + q.b, y[j]);
+            }
+            token += p.next_token;
+            unit += p.next_unit;
+            if (unit >= p.row_units) { unit -= p.row_units; ++token; }
+        }
+    };
+    request();
     for (int i = t; i < tokens * pairs; i += RT) {
         const int k = i / pairs;
         const int64_t m = m0 + k;
-        const double at = p.pos ? (double)p.pos[m] : (double)(m % p.seq);
-        const double turns = at * p.freq[i - k * pairs] * 0.15915494309189533577;     // of a whole circle
+        const double where = p.pos ? (double)p.pos[m] : (double)(m % p.seq);
+        const double turns = where * p.freq[i - k * pairs] * 0.15915494309189533577;     // of a whole circle
         float s, c;
         sincosf((float)((turns - rint(turns)) * 6.28318530717958647692), &s, &c);
         cs[i] = make_float2(c * p.factor, s * p.factor * p.back);
     }
     __syncthreads();
-    constexpr int STEP = ADJ && E == 1 ? 2 : E;               // elements of a turned unit in one place
-    const int nturn = ADJ ? p.rot / STEP : pairs / E;         // units of a turned head, then those that are copied
-    const int ncopy = p.in_place ? 0 : (p.dh - p.rot) / E, nv = p.in_place ? 0 : p.dh / E;
-    const int per_turned = nturn + ncopy, per_token = p.turned * per_turned + (p.heads - p.turned) * nv;
-    const int64_t row = (int64_t)p.heads * p.dh;
-    for (int i = t; i < tokens * per_token; i += RT) {
-        const int k = i / per_token;
-        int u = i - k * per_token, h;
-        int64_t at = (m0 + k) * row;
-        bool copy = true;
-        if (u < p.turned * per_turned) {
-            h = u / per_turned;
-            u -= h * per_turned;
-            copy = u >= nturn;
-            at += (int64_t)h * p.dh + (copy ? p.rot + (u - nturn) * E : u * STEP);
-        } else {
-            u -= p.turned * per_turned;
-            at += (int64_t)p.turned * p.dh + (int64_t)u * E;
-        }
-        float a[E], b[E];
-        if (copy) {
-            load_e<T, E>(in + at, a);
-            store_e<T, E>(out + at, a);
-            continue;
-        }
-        const float2* w = cs + k * pairs;
-        if constexpr (ADJ && E == 8) {
-            load_e<T, E>(in + at, a);
+    while (true) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float2 x = w[u * 4 + e];
-                b[2 * e] = fmaf(a[2 * e], x.x, -a[2 * e + 1] * x.y);
-                b[2 * e + 1] = fmaf(a[2 * e], x.y, a[2 * e + 1] * x.x);
+        for (int j = 0; j < AHEAD; ++j) {
+            if (of[j] >= tokens) return;
+            if (at[j].pair < 0) {
+                store_e<T, E>(out + at[j].a, x[j]);
+                continue;
             }
-            store_e<T, E>(out + at, b);
-        } else {
-            const int64_t other = at + (ADJ ? 1 : pairs);
-            load_e<T, E>(in + at, a);
-            load_e<T, E>(in + other, b);
+            const float2* w = cs + of[j] * pairs + at[j].pair;
             float c[E], d[E];
+            if constexpr (TWO) {
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                const float2 x = w[u * E + e];
-                c[e] = fmaf(a[e], x.x, -b[e] * x.y);
-                d[e] = fmaf(a[e], x.y, b[e] * x.x);
+                for (int e = 0; e < E; ++e) {
+                    c[e] = fmaf(x[j][e], w[e].x, -y[j][e] * w[e].y);
+                    d[e] = fmaf(x[j][e], w[e].y, y[j][e] * w[e].x);
+                }
+                store_e<T, E>(out + at[j].b, d);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    c[2 * e] = fmaf(x[j][2 * e], w[e].x, -x[j][2 * e + 1] * w[e].y);
+                    c[2 * e + 1] = fmaf(x[j][2 * e], w[e].y, x[j][2 * e + 1] * w[e].x);
+                }
             }
-            store_e<T, E>(out + at, c);
-            store_e<T, E>(out + other, d);
+            store_e<T, E>(out + at[j].a, c);
         }
+        request();
     }
 }
 
@@ -119,14 +140,19 @@ hipError_t launch(const RopeArgs& a, const RopeParams& p, bool wide) {
 }  // namespace
 
 hipError_t rope(const RopeArgs& a, bool back) {
+    const bool wide = a.dh % 8 == 0 && a.rot % (a.adjacent ? 8 : 16) == 0, in_place = a.in == a.out;
+    const int E = wide ? 8 : 1;
     RopeParams p{};
-    p.M = a.M; p.seq = a.seq; p.heads = a.nq + 2 * a.nkv; p.turned = a.nq + a.nkv; p.dh = a.dh; p.rot = a.rot; p.adjacent = a.adjacent;
-    p.in_place = a.in == a.out;
+    p.M = a.M; p.seq = a.seq; p.heads = a.nq + 2 * a.nkv; p.turned = a.nq + a.nkv; p.dh = a.dh; p.rot = a.rot;
     p.freq = a.freq; p.factor = a.factor; p.back = back ? -1.0f : 1.0f; p.pos = a.positions;
+    p.turn_units = a.adjacent && wide ? a.rot / 8 : a.rot / 2 / E;
+    p.head_units = p.turn_units + (in_place ? 0 : (a.dh - a.rot) / E);
+    p.row_units = p.turned * p.head_units + (in_place ? 0 : a.nkv * (a.dh / E));
+    p.div_head = ((1u << 31) + p.head_units - 1) / p.head_units;       // exact for row_units * head_units < 2^31: tp_layer.cpp
+    p.next_token = RT / p.row_units; p.next_unit = RT % p.row_units;
     // Tokens of a workgroup: enough for an angle to a thread, fewer where that would leave compute units without work.
-    const int64_t most = std::min<int64_t>(8, ROPE_LDS_PAIRS / (a.rot / 2)), spread = (a.M + 4 * compute_units() - 1) / (4 * compute_units());
+    const int64_t most = std::min<int64_t>(8, std::max(1, ROPE_LDS_PAIRS / (a.rot / 2))), spread = (a.M + 4 * compute_units() - 1) / (4 * compute_units());
     p.tokens = (int)std::max<int64_t>(1, std::min(most, spread));
-    const bool wide = a.dh % 8 == 0 && a.rot % (a.adjacent ? 8 : 16) == 0;
     return a.dtype == BF16 ? launch<bf16_t>(a, p, wide) : launch<float>(a, p, wide);
 }
 

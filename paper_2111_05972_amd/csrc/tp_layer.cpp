@@ -913,7 +913,7 @@ static int rope_call(bool back, int dtype, int64_t M, int nq, int nkv, int dh, i
     if (pairs != TPL_ROPE_HALF && pairs != TPL_ROPE_ADJACENT) return TPL_EINVAL;
     if (!freq || !in || !out || (!positions && seq <= 0)) return TPL_EINVAL;
     if (M > (int64_t)1 << 24 || nq > 1 << 16 || nkv > 1 << 16 || dh > 8192) return TPL_EUNSUPPORTED;
-    if (((int64_t)nq + 2 * nkv) * dh % (dtype == TPL_BF16 ? 8 : 4) || ((int64_t)nq + 2 * nkv) * dh > 1 << 24) return TPL_EUNSUPPORTED;
+    if (((int64_t)nq + 2 * nkv) * dh % (dtype == TPL_BF16 ? 8 : 4) || ((int64_t)nq + 2 * nkv) * dh * dh >= (int64_t)1 << 31) return TPL_EUNSUPPORTED;
     if (misaligned(in) || misaligned(out) || misaligned(freq) || misaligned(positions)) return TPL_EALIGN;
     RopeArgs a{};
     a.dtype = dtype; a.M = M; a.seq = seq; a.nq = nq; a.nkv = nkv; a.dh = dh; a.rot = rot; a.adjacent = pairs == TPL_ROPE_ADJACENT;
@@ -932,7 +932,8 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
 static int pack_check(int64_t sequences, int64_t M, int nq, int nkv) {
     if (sequences <= 0 || M <= 0 || nq <= 0 || nkv <= 0 || nq % nkv) return TPL_EINVAL;
     const int64_t G = nq / nkv;
-    if (sequences > (int64_t)1 << 20 || M > (int64_t)1 << 24 || nq > 1 << 12 || G > PACK_MAX_GROUP || (M + 256) * G >= (int64_t)1 << 30) return TPL_EUNSUPPORTED;
+    if (sequences > (int64_t)1 << 20 || M > (int64_t)1 << 24 || nq > 1 << 12 || G > PACK_MAX_GROUP || (M + 256) * G >= (int64_t)1 << 30 ||
+        M * nq >= (int64_t)1 << 31) return TPL_EUNSUPPORTED;
     // workgroups of a launch
     const PackLayout L = pack_layout(sequences, M, nq, nkv, pack_shares(M, nq, nkv, compute_units()));
     return (L.cap[0] + L.cap[1]) * nkv < (int64_t)1 << 30 ? TPL_OK : TPL_EUNSUPPORTED;
@@ -966,26 +967,30 @@ size_t tp_layer_attn_packed_workspace_bytes(int dtype, int64_t sequences, int64_
     if (attn_packed_check(dtype, sequences, M, nq, nkv, dh)) return 0;
     return std::max(ALIGN, up(attn_packed_workspace_bytes(attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal), bwd != 0)));
 }
-int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, const void* qkv, void* o, float* lse,
+int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, size_t plan_bytes,
+                             const void* qkv, void* o, float* lse,
                              void* ws, size_t ws_bytes, void* hip_stream) {
     const int rc = attn_packed_check(dtype, sequences, M, nq, nkv, dh);
     if (rc) return rc;
     if (!plan || !qkv || !o || !lse || !ws) return TPL_EINVAL;
     const void* ptrs[] = {plan, qkv, o, lse, ws};
     for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
-    if (ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 0)) return TPL_EWORKSPACE;
+    if (plan_bytes < tp_layer_pack_plan_bytes(sequences, M, nq, nkv) ||
+        ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 0)) return TPL_EWORKSPACE;
     PackAttnArgs a = attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal);
     a.plan = (const int*)plan; a.qkv = qkv; a.o = o; a.lse = lse; a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
     return hip_rc(dtype == TPL_BF16 ? attn_packed_bf16(a, false) : attn_packed_f32(a, false));
 }
-int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, const void* qkv, const void* o,
+int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, size_t plan_bytes,
+                             const void* qkv, const void* o,
                              const float* lse, const void* d_o, void* dqkv, float* d_scratch, void* ws, size_t ws_bytes, void* hip_stream) {
     const int rc = attn_packed_check(dtype, sequences, M, nq, nkv, dh);
     if (rc) return rc;
     if (!plan || !qkv || !o || !lse || !d_o || !dqkv || !d_scratch || !ws) return TPL_EINVAL;
     const void* ptrs[] = {plan, qkv, o, lse, d_o, dqkv, d_scratch, ws};
     for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
-    if (ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 1)) return TPL_EWORKSPACE;
+    if (plan_bytes < tp_layer_pack_plan_bytes(sequences, M, nq, nkv) ||
+        ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 1)) return TPL_EWORKSPACE;
     PackAttnArgs a = attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal);
     a.plan = (const int*)plan; a.qkv = qkv; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse); a.d_o = d_o; a.dqkv = dqkv; a.dsum = d_scratch;
     a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
