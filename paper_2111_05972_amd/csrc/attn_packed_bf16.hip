@@ -418,14 +418,14 @@ __device__ __forceinline__ void dq_rows_again(float* q_s, const Params& p, const
 // ---- dK, dV -----------------------------------------------------------------------------------------------------------
 // Workgroup = (128 keys, key head), 8 wavefronts: w and w + 4 share 32 keys.  w works out scores and probabilities and accumulates
 // dV; w + 4 works out dP and accumulates dK from the same probabilities, which it gets through LDS in float one sub-tile of 32 rows
-// later.  Q, dO, LSE, D in tiles of 64 flattened rows through three stages, as dK still reads the tile before.
+// later.  Tiles of 64 flattened rows: Q, LSE and D through three stages, as dK still reads the tile before, dO through two.
 constexpr int WAVES8 = 512;
 constexpr int P_BYTES = 32 * 32 * 4;
-template <int DH> constexpr int dkv_lds() { return 3 * (2 * tile_bytes<DH>() + 2 * PACK_TILE * 4) + 2 * 4 * P_BYTES; }
+template <int DH> constexpr int dkv_lds() { return 5 * tile_bytes<DH>() + 3 * 2 * PACK_TILE * 4 + 2 * 4 * P_BYTES; }
 template <int DH, bool CAUSAL, bool DK_ROLE>
 __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStrip& s) {
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2;
-    constexpr int TERMS = 6 * TB, PS = TERMS + 3 * 2 * PACK_TILE * 4;  // three Q tiles, three dO tiles, three times LSE*log2e and D, P
+    constexpr int TERMS = 5 * TB, PS = TERMS + 3 * 2 * PACK_TILE * 4;  // three Q tiles, two dO tiles, three times LSE*log2e and D, P
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int len = s.it.len, rows = s.rows, G = p.G;
@@ -446,7 +446,7 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
     ft.init(p.dh, t);
     float rl = 0.0f, rd = 0.0f;
     auto g2r = [&](int qt, int stage) {
-        ft.load(p, s, dobase, qt, lds0 + stage * TB, lds0 + (3 + stage) * TB, wave);
+        ft.load(p, s, dobase, qt, lds0 + stage * TB, lds0 + (3 + ((qt - qt0) & 1)) * TB, wave);
         if (t < PACK_TILE) {
             const int r = qt * PACK_TILE + t;
             const Row w = row_of(p, r);
@@ -461,7 +461,8 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
             st[PACK_TILE + t] = rd;
         }
     };
-    // LDS addresses in stage 0: rows as they are (scores: Q, dP: dO), transposed (dV: dO, dK: Q), LSE or D, P
+    // LDS addresses in stage 0: rows as they are (scores: Q, dP: dO), transposed (dV: dO, dK: Q), LSE or D, P.  Those into dO move between
+    // its two stages from tile to tile; Q's stage is a constant of the code.
     unsigned ka[NF], ta[NT][2];
 #pragma unroll
     for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + (DK_ROLE ? 3 * TB : 0) + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
@@ -483,10 +484,11 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
 
     // rows that see one of this wavefront's keys, in scalar registers: with the products in the loop it spilled
     const int see_lo = __builtin_amdgcn_readfirstlane(CAUSAL ? k0 * G - 31 : 0), see_hi = __builtin_amdgcn_readfirstlane(k0 < len ? rows : 0);
+    unsigned other = TB;                                   // to the other stage of dO
     f32x16 x;                                              // scores, then P; or dP, then dS
     bool pending = false;                                  // dP of the sub-tile before waits for its P
     auto product = [&](auto stg, auto sbc) __attribute__((always_inline)) {
-        constexpr int OFF = decltype(stg)::value * TB + decltype(sbc)::value * HALF;
+        constexpr int OFF = (DK_ROLE ? 0 : decltype(stg)::value * TB) + decltype(sbc)::value * HALF;
         bf16x8 fr[NF];
 #pragma unroll
         for (int i = 0; i < NF; ++i) fr[i] = lds_frag_k<OFF>(ka[i]);
@@ -498,7 +500,7 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
         __builtin_amdgcn_s_setprio(0);
     };
     auto fetch_t = [&](auto stg, auto sbc, bf16x8 (&fr)[NF]) __attribute__((always_inline)) {
-        constexpr int OFF = decltype(stg)::value * TB + decltype(sbc)::value * HALF;
+        constexpr int OFF = (DK_ROLE ? decltype(stg)::value * TB : 0) + decltype(sbc)::value * HALF;
 #pragma unroll
         for (int k = 0; k < NF; ++k)
             fr[k] = k & 1 ? lds_frag_t<OFF + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF>(ta[k >> 1][0], ta[k >> 1][1]);
@@ -568,6 +570,14 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
         __builtin_amdgcn_sched_barrier(0);
         slot(qt, stg, C1{}, stg);
         if (more) r2s(decltype(next)::value);
+        if constexpr (DK_ROLE) {
+#pragma unroll
+            for (int ks = 0; ks < NF; ++ks) ka[ks] += other;
+        } else {
+#pragma unroll
+            for (int dt = 0; dt < NT; ++dt) { ta[dt][0] += other; ta[dt][1] += other; }
+        }
+        other = 0u - other;
         dma_wait();
         __syncthreads();
     };
@@ -769,8 +779,9 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
     dq_rows_again<DH>(reinterpret_cast<float*>(smem) + qs * (DH / 2) * 64, p, s, r0, lane);   // this wavefront alone reads its merge area
 }
 
+// Up to head size 64 two workgroups share a compute unit (128 registers, 80 KB of LDS each).
 template <int DH, bool CAUSAL>
-__global__ __launch_bounds__(WAVES8, 2) void attn_packed_bwd_kernel(Params p) {
+__global__ __launch_bounds__(WAVES8, DH <= 64 ? 4 : 2) void attn_packed_bwd_kernel(Params p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     BStrip s;
     if ((int)blockIdx.x >= p.kv_wgs) {
