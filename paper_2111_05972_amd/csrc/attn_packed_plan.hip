@@ -15,6 +15,7 @@ namespace {
 
 constexpr int PLAN_THREADS = 1024;
 constexpr int BUCKETS = 1024;
+constexpr int NEAR = 2048;
 
 // Inclusive scan over the workgroup, sum or maximum, by wavefronts and then over their totals; total: of all.
 template <bool MAX> __device__ __forceinline__ int join(int a, int b) { return MAX ? max(a, b) : a + b; }
@@ -47,28 +48,32 @@ struct PlanParams {
     PackLayout L;
 };
 
-// Strip `i` of a sequence: its first row or key and its tiles.
+// Strip `i` of a sequence: its first row or key and its tiles.  Rows are below 2^30.
 __device__ __forceinline__ void strip_of(const PlanParams& p, int side, int len, int i, int& first, int& tile0, int& tile1) {
-    const int G = p.nq / p.nkv;
-    const int64_t rows = (int64_t)len * G;
+    const unsigned G = (unsigned)(p.nq / p.nkv), rows = (unsigned)len * G;
     first = i * PACK_BLK;
     if (side == 0) {
-        const int64_t last = min(rows, (int64_t)first + PACK_BLK) - 1;
+        const unsigned last = min(rows, (unsigned)first + PACK_BLK) - 1;
         tile0 = 0;
         tile1 = p.causal ? (int)(last / G) / PACK_TILE + 1 : (len + PACK_TILE - 1) / PACK_TILE;
     } else {
-        tile0 = p.causal ? (int)((int64_t)first * G / PACK_TILE) : 0;
+        tile0 = p.causal ? (int)((unsigned)first * G / PACK_TILE) : 0;
         tile1 = (int)((rows + PACK_TILE - 1) / PACK_TILE);
     }
 }
+// Longest first, `top` above the longest.
+__device__ __forceinline__ int bucket_of(int tiles, int top) { return BUCKETS - 1 - min(BUCKETS - 1, (int)((float)tiles * ((float)(BUCKETS - 1) / (float)top))); }
 
 __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     __shared__ int tmp[PLAN_THREADS / 64];
     __shared__ int hist[2][BUCKETS];
     __shared__ int longest[2], slots[2], joins[2], first_short;
     __shared__ unsigned long long tiles[2];
+    __shared__ int near[3][NEAR];                                  // what the searches read, where it fits
     const int t = threadIdx.x, G = p.nq / p.nkv;
-    int* start = p.plan + p.L.start;
+    const bool fits = p.n < NEAR;
+    int* start = fits ? near[2] : p.plan + p.L.start;
+    int* const before[2] = {fits ? near[0] : p.plan + p.L.pre[0], fits ? near[1] : p.plan + p.L.pre[1]};   // strips before each sequence
     auto offset = [&](int i) { return min(max(p.offsets[i], 0), p.M); };
     if (blockIdx.x > 0) {
         // This workgroup's tokens, each looking for its sequence among the offsets.  Where these decrease, their running maximum would be
@@ -87,7 +92,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     }
     if (t == 0) first_short = 0;
     if (t < 2) { longest[t] = 0; slots[t] = 0; joins[t] = 0; tiles[t] = 0; }
-    for (int i = t; i < 2 * BUCKETS; i += PLAN_THREADS) (&hist[0][0])[i] = 0;
+    hist[0][t] = hist[1][t] = 0;
     __syncthreads();
     // offsets as running maxima, and the strips before each sequence
     int carry_max = 0, carry[2] = {0, 0};
@@ -104,11 +109,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         const int i = base + t;
         const int len = i < p.n ? start[i + 1] - start[i] : 0;
         for (int side = 0; side < 2; ++side) {
-            const int64_t rows = side == 0 ? (int64_t)len * G : len;
-            const int blocks = (int)((rows + PACK_BLK - 1) / PACK_BLK);
+            const int blocks = ((side == 0 ? len * G : len) + PACK_BLK - 1) / PACK_BLK;
             int all;
             const int pre = block_scan<false>(blocks, tmp, all) + carry[side];
-            if (i <= p.n) (p.plan + p.L.pre[side])[i] = pre - blocks;
+            if (i <= p.n) before[side][i] = pre - blocks;
             carry[side] += all;
         }
     }
@@ -123,7 +127,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         return lo;
     };
     for (int side = 0; side < 2; ++side) {
-        const int* pre = p.plan + p.L.pre[side];
+        const int* pre = before[side];
         unsigned long long mine = 0;
         int most = 0;
         for (int k = t; k < carry[side]; k += PLAN_THREADS) {
@@ -133,12 +137,14 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
             mine += (unsigned)(t1 - t0);
             most = max(most, t1 - t0);
         }
-        atomicAdd(&tiles[side], mine);
-        atomicMax(&longest[side], most);
+        if (mine) {
+            atomicAdd(&tiles[side], mine);
+            atomicMax(&longest[side], most);
+        }
     }
     __syncthreads();
     for (int side = 0; side < 2; ++side) {
-        const int* pre = p.plan + p.L.pre[side];
+        const int* pre = before[side];
         int chunk = 1 << 30;
         if (p.shares.of[side] > 0) chunk = max(PACK_MIN_CHUNK, (int)((tiles[side] + p.shares.of[side] - 1) / p.shares.of[side]));
         const int top = min(longest[side], chunk) + 1;
@@ -154,7 +160,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                 strip_of(p, side, it.len, k - pre[b], it.first, a, z);
                 it.chunks = (z - a + chunk - 1) / chunk;
                 const int each = (z - a + it.chunks - 1) / it.chunks;
-                const int bucket = BUCKETS - 1 - (int)((int64_t)each * (BUCKETS - 1) / top);     // longest first
+                const int bucket = bucket_of(each, top);
                 if (pass == 0) {
                     atomicAdd(&hist[side][bucket], it.chunks);
                     continue;
@@ -179,9 +185,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
             __syncthreads();
             if (pass == 0) {                                       // counts -> first places
                 int all;
-                const int v = hist[side][t], before = block_scan<false>(v, tmp, all) - v;
-                hist[side][t] = before;
-                if (side == 0 && t == BUCKETS - 1 - 2 * (BUCKETS - 1) / top) first_short = before;
+                const int v = hist[side][t], at = block_scan<false>(v, tmp, all) - v;
+                hist[side][t] = at;
+                if (side == 0 && t == bucket_of(2, top)) first_short = at;
                 __syncthreads();
             }
         }
