@@ -300,7 +300,7 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal,
  * backward: the transpose of that, (x, y) -> factor * (x cos a + y sin a, y cos a - x sin a).  The other columns and v are copied.
  * freq: double [rot / 2] in device memory, radians per position.  positions: int32 [M] (16-byte aligned; the front of a pack plan is such
  * an array), or NULL: row m has position m % seq (seq > 0; not looked at where there are positions).  Any int32 is a position; the angle is
- * worked out in 64 bits.  qkv and out are [M, (nq + 2 nkv) dh], whole 16-byte rows; out may be qkv itself (then only what is turned is
+ * worked out in 64 bits.  qkv and out are [M, (nq + 2 nkv) dh], M < 2^24, whole 16-byte rows; out may be qkv itself (then only what is turned is
  * touched), but may not overlap it otherwise.
  * tp_layer_rope_frequencies fills freq and factor in HOST memory: base^(-2 i / rot), for a context stretched `stretch` times
  *   TPL_ROPE_LINEAR  every frequency divided by stretch
@@ -319,8 +319,11 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
  * (lengths from 0 on); query head h reads key and value head h / (nq / nkv); causal: query i of a sequence sees its keys j <= i, otherwise
  * all of its sequence, never another.
  *   qkv [M, (nq + 2 nkv) dh] -> o [M, nq dh], lse [M, nq] float (natural log of the sum of exp(q . k / sqrt(dh)))
- * Rows that belong to no sequence (behind the last one) are neither read nor written.  A masked value is as if it
+ * Rows that belong to no sequence (behind the last one) are neither read nor written: what the caller's products make of whole tensors
+ * (dW of a projection) reads what they held, so o and dqkv are best zeroed once where a batch may end before M.  A masked value is as if it
  * were not there, infinities and NaN among them.  dh: a multiple of 8 up to 128; at most 128 query heads to a key head.
+ * TPL_EUNSUPPORTED: over 2^24 rows, 2^20 sequences, 2^31 (row, head) pairs, or 2^22 strips (of 128 (row, head) pairs or keys of one sequence
+ * and key head, those that may be cut counted twice).
  *
  * The plan: tp_layer_pack_plan_bytes() of device memory that tp_layer_pack_plan fills on the stream from offsets (int32
  * [sequences + 1], device memory, offsets[0] = 0, not decreasing, the last at most M), once for a batch; every layer's calls with the same
@@ -348,7 +351,7 @@ int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, in
  *   3. tp_layer_lm_loss_bwd : dz = (exp(z - lse) - onehot(label)) * dloss[m], worked out again piece by piece;
  *      dx_partial [M, H] = dz w, which the ranks would all-reduce; dw [V, H] = dz^T x
  * (x of an ignored token is multiplied by zero in dw: it has to be finite).  stats, loss, lse, dloss: float, natural logarithms.
- * H whole 16-byte rows; V and M any number; x below 2 GiB.  ws_bytes >= tp_layer_lm_loss_workspace_bytes(..., bwd). */
+ * H whole 16-byte rows; V up to 2^24, M up to 2^20, M V up to 2^37; x below 2 GiB.  ws_bytes >= tp_layer_lm_loss_workspace_bytes(..., bwd). */
 size_t tp_layer_lm_loss_workspace_bytes(int dtype, int64_t M, int64_t H, int64_t V, int bwd);
 int tp_layer_lm_loss_fwd(int dtype, int64_t M, int64_t H, int64_t V, int64_t first, const void* x, const void* w, const int32_t* labels,
                          float* stats, void* ws, size_t ws_bytes, void* hip_stream);

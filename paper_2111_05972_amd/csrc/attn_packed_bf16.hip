@@ -78,24 +78,22 @@ template <int DH, int NT> struct FlatTile {
 };
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
-// Workgroup = (128 flattened rows, key head), K and V in tiles of 64 through two LDS stages.  SPLIT = 1: four wavefronts of 32 rows each, two
-// workgroups to a unit.  SPLIT = 2: eight wavefronts, w takes rows 32 (w % 4) and one 32-key half (w / 4) of every tile; the halves are joined
-// through LDS at the end.  That is half the chain of dependent steps, and two wavefronts to a SIMD where a unit has one workgroup.
+// Workgroup = (128 flattened rows, key head), four wavefronts of 32 rows each, two workgroups to a unit; K and V in tiles of 64 through two LDS
+// stages.  Eight wavefronts, two to 32 rows with half of each tile's keys, halve the chain of dependent steps but read K and V by rows twice:
+// where a unit has one strip they took -5 to +10 % of the time, where it has two up to 38 % more (4096 tokens of 32 to 800, 16 / 2 heads of 128).
 constexpr int WAVES4 = 256;
-constexpr double FEW_STRIPS = 2.5;        // strips to a unit below which SPLIT = 2
-template <int DH, int SPLIT> constexpr int fwd_lds() { return SPLIT == 1 ? 4 * tile_bytes<DH>() : std::max(4 * tile_bytes<DH>(), 4 * 64 * (2 + DH / 2) * 4); }
+template <int DH> constexpr int fwd_lds() { return 4 * tile_bytes<DH>(); }
 
-template <int DH, bool CAUSAL, int SPLIT>
-__global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) void attn_packed_fwd_kernel(Params p) {
+template <int DH, bool CAUSAL>
+__global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2;
-    constexpr int NTHR = WAVES4 * SPLIT, NCH = NCHUNKS<DH, NTHR>, HALVES = 2 / SPLIT;
+    constexpr int NCH = NCHUNKS<DH, WAVES4>;
     BStrip s;
     if (!take_strip(p, 0, blockIdx.x, s)) return;
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
-    const int rw = wave & 3, kvh = SPLIT == 2 ? wave >> 2 : 0;    // rows and key half of this wavefront
-    const int r0 = s.it.first + rw * 32, r = r0 + (lane & 31), len = s.it.len;
+    const int r0 = s.it.first + wave * 32, r = r0 + (lane & 31), len = s.it.len;
     const bool valid = r < s.rows;
     const Row me = row_of(p, valid ? r : s.rows - 1);
     const int q_lo = (int)((unsigned)min(r0, s.rows - 1) / (unsigned)p.G), q_hi = (int)((unsigned)min(r0 + 31, s.rows - 1) / (unsigned)p.G);
@@ -113,18 +111,18 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
     const int kv_end = r0 >= s.rows ? 0 : CAUSAL ? q_hi + 1 : len;    // keys that any row of this wavefront sees
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
     unsigned off[NCH];
-    dma_offsets<DH, NTHR>(off, s.ld, p.dh, t);
+    dma_offsets<DH, WAVES4>(off, s.ld, p.dh, t);
     auto fetch_tile = [&](int kt, unsigned stage) {
-        tile_dma<DH, NTHR>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), stage, off, 0, wave);
-        tile_dma<DH, NTHR>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
+        tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), stage, off, 0, wave);
+        tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
     };
     unsigned ka[NF], va[NT][2];
 #pragma unroll
-    for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(kvh * 32, ks, lane); keep_in_register(ka[ks]); }
+    for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
 #pragma unroll
     for (int dt = 0; dt < NT; ++dt)
 #pragma unroll
-        for (int g = 0; g < 2; ++g) { va[dt][g] = lds0 + TB + frag_t_off<DH>(dt * 32, kvh * 32, g, lane); keep_in_register(va[dt][g]); }
+        for (int g = 0; g < 2; ++g) { va[dt][g] = lds0 + TB + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(va[dt][g]); }
     fetch_tile(s.it.tile0, lds0);
 #pragma unroll
     for (int ks = 0; ks < NF; ++ks) settle(qf[ks]);
@@ -133,23 +131,21 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
     auto step = [&](int kt, auto stg) __attribute__((always_inline)) {
         constexpr int SOFF = decltype(stg)::value * 2 * TB;
         if (kt + 1 < s.it.tile1) fetch_tile(kt + 1, lds0 + (1 - decltype(stg)::value) * 2 * TB);
-        const int kv0 = kt * PACK_TILE + kvh * 32;
+        const int kv0 = kt * PACK_TILE;
         if (kv0 < kv_end) {                                       // wavefront-uniform
-            f32x16 x[HALVES];
-            bf16x8 fr[HALVES * NF];                               // keys 0..31 and 32..63 in turn, a chain of products each
-#pragma unroll
-            for (int n = 0; n < HALVES; ++n) x[n] = zero16();
+            f32x16 x[2] = {zero16(), zero16()};
+            bf16x8 fr[2 * NF];                                    // keys 0..31 and 32..63 in turn, a chain of products each
 #pragma unroll
             for (int ks = 0; ks < NF; ++ks) {
-                fr[HALVES * ks] = lds_frag_k<SOFF>(ka[ks]);
-                if (HALVES == 2) fr[HALVES * ks + HALVES - 1] = lds_frag_k<SOFF + HALF>(ka[ks]);
+                fr[2 * ks] = lds_frag_k<SOFF>(ka[ks]);
+                fr[2 * ks + 1] = lds_frag_k<SOFF + HALF>(ka[ks]);
             }
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
             for (int ks = 0; ks < NF; ++ks) {
 #pragma unroll
-                for (int n = 0; n < HALVES; ++n) x[n] = MFMA(fr[HALVES * ks + n], qf[ks], x[n]);
+                for (int n = 0; n < 2; ++n) x[n] = MFMA(fr[2 * ks + n], qf[ks], x[n]);
             }
             __builtin_amdgcn_s_setprio(0);
             __builtin_amdgcn_sched_barrier(0);
@@ -157,22 +153,20 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
             for (int dt = 0; dt < NT; ++dt) {                     // [16 rows][dt]
                 fr[dt] = lds_frag_t<SOFF>(va[dt][0], va[dt][1]);
                 fr[NT + dt] = lds_frag_t<SOFF + HALF / 2>(va[dt][0], va[dt][1]);
-                if constexpr (HALVES == 2) {
-                    fr[2 * NT + dt] = lds_frag_t<SOFF + HALF>(va[dt][0], va[dt][1]);
-                    fr[3 * NT + dt] = lds_frag_t<SOFF + HALF + HALF / 2>(va[dt][0], va[dt][1]);
-                }
+                fr[2 * NT + dt] = lds_frag_t<SOFF + HALF>(va[dt][0], va[dt][1]);
+                fr[3 * NT + dt] = lds_frag_t<SOFF + HALF + HALF / 2>(va[dt][0], va[dt][1]);
             }
             __builtin_amdgcn_sched_barrier(0);
-            if (kv0 + 32 * HALVES - 1 >= len || (CAUSAL && kv0 + 32 * HALVES - 1 > q_lo)) {
+            if (kv0 + PACK_TILE > len || (CAUSAL && kv0 + PACK_TILE - 1 > q_lo)) {
                 const int seen = min(CAUSAL ? me.q : len, len - 1) - kv0 - half * 4;      // last key this row sees
 #pragma unroll
-                for (int g = 0; g < HALVES; ++g)
+                for (int g = 0; g < 2; ++g)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) x[g][v] = 32 * g + (v >> 2) * 8 + (v & 3) <= seen ? x[g][v] : -INFINITY;
             }
-            float mb = fmaxf(x[0][0], x[HALVES - 1][0]);
+            float mb = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
-            for (int v = 1; v < 16; ++v) mb = fmaxf(fmaxf(mb, x[0][v]), x[HALVES - 1][v]);
+            for (int v = 1; v < 16; ++v) mb = fmaxf(fmaxf(mb, x[0][v]), x[1][v]);
             mb = cross_half_max(mb) * c2;                         // c2 > 0: scaling commutes with max
             // The reference point moves only when the maximum has grown by more than RESCALE_LAG (log2 units): any reference point
             // gives the same result up to rounding, and weights reach 2^RESCALE_LAG at most.
@@ -184,7 +178,7 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
 #pragma unroll
             for (int v = 0; v < 16; ++v)
 #pragma unroll
-                for (int g = 0; g < HALVES; ++g) { x[g][v] = fast_exp2(fmaf(x[g][v], c2, -mu)); ps[g] += x[g][v]; }
+                for (int g = 0; g < 2; ++g) { x[g][v] = fast_exp2(fmaf(x[g][v], c2, -mu)); ps[g] += x[g][v]; }
             lsum = lsum * alpha + (ps[0] + ps[1]);
             if (__any(alpha != 1.0f)) {
 #pragma unroll
@@ -192,9 +186,9 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
 #pragma unroll
                     for (int v = 0; v < 16; ++v) oacc[dt][v] *= alpha;
             }
-            bf16x8 pb[2 * HALVES];
+            bf16x8 pb[4];
 #pragma unroll
-            for (int n = 0; n < 2 * HALVES; ++n) pb[n] = pack_regs(x[n >> 1], 8 * (n & 1));
+            for (int n = 0; n < 4; ++n) pb[n] = pack_regs(x[n >> 1], 8 * (n & 1));
             __builtin_amdgcn_s_setprio(1);
             auto add = [&](int n0) __attribute__((always_inline)) {
 #pragma unroll
@@ -203,7 +197,7 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
                     for (int dt = 0; dt < NT; ++dt) oacc[dt] = MFMA(fr[n * NT + dt], pb[n], oacc[dt]);
             };
             add(0);
-            if (HALVES == 2 && (!CAUSAL || kv0 + 32 <= q_hi)) add(2);   // uniform
+            if (!CAUSAL || kv0 + 32 <= q_hi) add(2);   // uniform
             __builtin_amdgcn_s_setprio(0);
         }
         dma_wait();
@@ -216,31 +210,9 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
         ++kt;
     }
     lsum += __shfl_xor(lsum, 32, 64);
-    if constexpr (SPLIT == 2) {
-        constexpr int NV = 2 + DH / 2;
-        float* mg = reinterpret_cast<float*>(smem) + rw * NV * 64 + lane;       // element i at mg[i * 64]; the ring has been read
-        if (kvh == 1) {
-            mg[0] = m;
-            mg[64] = lsum;
-#pragma unroll
-            for (int dt = 0; dt < NT; ++dt)
-#pragma unroll
-                for (int v = 0; v < 16; ++v) mg[(2 + dt * 16 + v) * 64] = oacc[dt][v];
-        }
-        __syncthreads();
-        if (kvh == 1) return;
-        const float m1 = mg[0], l1 = mg[64], mn = fmaxf(m, m1), mu = mn == -INFINITY ? 0.0f : mn;
-        const float f0 = fast_exp2(m - mu), f1 = fast_exp2(m1 - mu);
-        lsum = lsum * f0 + l1 * f1;
-        m = mn;
-#pragma unroll
-        for (int dt = 0; dt < NT; ++dt)
-#pragma unroll
-            for (int v = 0; v < 16; ++v) oacc[dt][v] = oacc[dt][v] * f0 + mg[(2 + dt * 16 + v) * 64] * f1;
-    }
     const bool whole = s.it.slot < 0;
     float* part = whole ? nullptr : p.part[0] + ((int64_t)s.it.slot * p.nkv + s.hk) * (PACK_BLK * (DH + 2));
-    const int rl = rw * 32 + (lane & 31);
+    const int rl = wave * 32 + (lane & 31);
     float z = 0.0f;
     if (!whole) {
         // one chunk of a strip: (reference point, sum, O not divided by it) of its keys, float, [row][dh]
@@ -268,7 +240,7 @@ __global__ __launch_bounds__(WAVES4 * SPLIT, SPLIT == 1 ? 2 : DH <= 64 ? 4 : 2) 
     }
     if (!CAUSAL || !any_nonfinite(z)) return;
     rows_stored();
-    float* q_s = reinterpret_cast<float*>(smem) + rw * (2 + DH / 2) * 64;   // the ring has been read, and this wavefront's other half
+    float* q_s = reinterpret_cast<float*>(smem) + wave * DH;   // the ring has been read
     for (int i = r0; i < r0 + 32 && i < s.rows; ++i) {
         const Row w = row_of(p, i);
         load_row(q_s, s.q + w.q * s.ld + w.g * p.dh, p.dh, lane);
@@ -794,18 +766,16 @@ __global__ __launch_bounds__(WAVES8, DH <= 64 ? 4 : 2) void attn_packed_bwd_kern
     else dkv_body<DH, CAUSAL, true>(smem, p, s);
 }
 
-// Whether a launch has few workgroups for the units, see attn_packed_fwd_kernel.
-bool few_strips(const PackAttnArgs& a) { return a.M * a.nq / PACK_BLK < FEW_STRIPS * compute_units(); }
-template <int DH, bool CAUSAL, int SPLIT>
+template <int DH, bool CAUSAL>
 hipError_t run_fwd(const PackAttnArgs& a) {
     const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
     const PackLayout L = pack_layout(a.sequences, a.M, a.nq, a.nkv, shares);
     Params p = make_params<bf16_t>(a, L);
     p.part[0] = (float*)a.ws;
-    constexpr int lds = fwd_lds<DH, SPLIT>();
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_fwd_kernel<DH, CAUSAL, SPLIT>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    constexpr int lds = fwd_lds<DH>();
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_fwd_kernel<DH, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, CAUSAL, SPLIT>), dim3((unsigned)(L.cap[0] * a.nkv)), dim3(WAVES4 * SPLIT), lds, a.stream, p);
+    hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, CAUSAL>), dim3((unsigned)(L.cap[0] * a.nkv)), dim3(WAVES4), lds, a.stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares.of[0] == 0) return e;
     hipLaunchKernelGGL((attn_packed_fwd_join_kernel<bf16_t, DH>), dim3(join_wgs(L, a.nkv)), dim3(32 * JOIN_ROWS), 0, a.stream, p);
@@ -833,15 +803,13 @@ hipError_t run_bwd(const PackAttnArgs& a) {
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<bf16_t, DH>), dim3(join_wgs(L, a.nkv)), dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
-template <int DH, bool CAUSAL>
-hipError_t fwd_by_strips(const PackAttnArgs& a) { return few_strips(a) ? run_fwd<DH, CAUSAL, 2>(a) : run_fwd<DH, CAUSAL, 1>(a); }
 template <bool CAUSAL>
 hipError_t run(const PackAttnArgs& a, bool bwd) {
     switch (padded(a.dh)) {
-        case 32: return bwd ? run_bwd<32, CAUSAL>(a) : fwd_by_strips<32, CAUSAL>(a);
-        case 64: return bwd ? run_bwd<64, CAUSAL>(a) : fwd_by_strips<64, CAUSAL>(a);
-        case 96: return bwd ? run_bwd<96, CAUSAL>(a) : fwd_by_strips<96, CAUSAL>(a);
-        default: return bwd ? run_bwd<128, CAUSAL>(a) : fwd_by_strips<128, CAUSAL>(a);
+        case 32: return bwd ? run_bwd<32, CAUSAL>(a) : run_fwd<32, CAUSAL>(a);
+        case 64: return bwd ? run_bwd<64, CAUSAL>(a) : run_fwd<64, CAUSAL>(a);
+        case 96: return bwd ? run_bwd<96, CAUSAL>(a) : run_fwd<96, CAUSAL>(a);
+        default: return bwd ? run_bwd<128, CAUSAL>(a) : run_fwd<128, CAUSAL>(a);
     }
 }
 }  // namespace

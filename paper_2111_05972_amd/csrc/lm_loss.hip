@@ -97,7 +97,7 @@ __device__ __forceinline__ void stats_row(const LossParams& lp, int row, int m0,
     for (int n = 0; n < TL::WN; ++n) s = fmaf(red[n * TL::BM + row - m0].y, __builtin_amdgcn_exp2f(red[n * TL::BM + row - m0].x - mu), s);
     lp.part[(int64_t)(lp.part0 + n0 / TL::BN) * lp.g.M + row] = make_float2(m, s);
 }
-__device__ __forceinline__ int label_of(const LossParams& lp, int row) { return row < lp.g.M ? lp.labels[row] - lp.first : -1; }
+__device__ __forceinline__ int label_of(const LossParams& lp, int row) { return row < lp.g.M ? (int)((unsigned)lp.labels[row] - (unsigned)lp.first) : -1; }
 
 template <typename TL>
 __device__ __forceinline__ void stats_epilogue(const LossParams& lp, const PPAcc<TL>& acc, const PPWork& w, char* smem) {
@@ -132,7 +132,7 @@ __device__ __forceinline__ void grad_block(const LossParams& lp, const PPLane& e
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
         if (el.col[u] >= lp.ldz) continue;
-        const int at = r.label - lp.first - el.col[u];
+        const int at = (int)((unsigned)r.label - (unsigned)lp.first) - el.col[u];
         float v[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -414,7 +414,7 @@ void products(const LmLossArgs& a, int64_t v0, int64_t n, void* dz, float* acc, 
     g[1].B = a.x;
     g[1].C = (char*)a.dw + v0 * a.H * es;
 }
-// The logits of a piece, float: a group of one, whose plan has the faster tile (512 x 7632 x 1024: 88 us by gemm_f32, 71 so).
+// The logits of a piece, float: a group of one, the launch whose B may end before N (512 x 7632 x 1024: 87 us, 92 TFLOP/s, by either launch).
 GemmArgs logits_f32(const LmLossArgs& a, int64_t v0, int64_t n) {
     GemmArgs g{};
     g.dtype = F32; g.trans_b = 1; g.M = a.M; g.N = row_stride(F32, n); g.K = a.H; g.epi = EPI_NONE;

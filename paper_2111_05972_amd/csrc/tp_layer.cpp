@@ -912,7 +912,7 @@ static int rope_call(bool back, int dtype, int64_t M, int nq, int nkv, int dh, i
     if (M <= 0 || nq <= 0 || nkv <= 0 || dh <= 0 || rot <= 0 || rot % 2 || rot > dh) return TPL_EINVAL;
     if (pairs != TPL_ROPE_HALF && pairs != TPL_ROPE_ADJACENT) return TPL_EINVAL;
     if (!freq || !in || !out || (!positions && seq <= 0)) return TPL_EINVAL;
-    if (M > (int64_t)1 << 24 || nq > 1 << 16 || nkv > 1 << 16 || dh > 8192) return TPL_EUNSUPPORTED;
+    if (M >= (int64_t)1 << 24 || nq > 1 << 16 || nkv > 1 << 16 || dh > 8192) return TPL_EUNSUPPORTED;    // 2^32 threads, 256 for a token at least
     if (((int64_t)nq + 2 * nkv) * dh % (dtype == TPL_BF16 ? 8 : 4) || ((int64_t)nq + 2 * nkv) * dh * dh >= (int64_t)1 << 31) return TPL_EUNSUPPORTED;
     if (misaligned(in) || misaligned(out) || misaligned(freq) || misaligned(positions)) return TPL_EALIGN;
     RopeArgs a{};
@@ -934,9 +934,9 @@ static int pack_check(int64_t sequences, int64_t M, int nq, int nkv) {
     const int64_t G = nq / nkv;
     if (sequences > (int64_t)1 << 20 || M > (int64_t)1 << 24 || nq > 1 << 12 || G > PACK_MAX_GROUP || (M + 256) * G >= (int64_t)1 << 30 ||
         M * nq >= (int64_t)1 << 31) return TPL_EUNSUPPORTED;
-    // workgroups of a launch
+    // a launch has less than 2^32 threads, an item of the plan and a key head up to 1024 of them (float backward)
     const PackLayout L = pack_layout(sequences, M, nq, nkv, pack_shares(M, nq, nkv, compute_units()));
-    return (L.cap[0] + L.cap[1]) * nkv < (int64_t)1 << 30 ? TPL_OK : TPL_EUNSUPPORTED;
+    return (L.cap[0] + L.cap[1]) * nkv < (int64_t)1 << 22 ? TPL_OK : TPL_EUNSUPPORTED;
 }
 size_t tp_layer_pack_plan_bytes(int64_t sequences, int64_t M, int nq, int nkv) {
     if (pack_check(sequences, M, nq, nkv)) return 0;
@@ -1001,7 +1001,8 @@ static int lm_loss_check(int dtype, int64_t M, int64_t H, int64_t V, int64_t fir
     if (dtype != TPL_F32 && dtype != TPL_BF16) return TPL_EINVAL;
     if (M <= 0 || H <= 0 || V <= 0 || first < 0) return TPL_EINVAL;
     const int64_t es = dtype == TPL_BF16 ? 2 : 4;
-    if (H % (16 / es) || H > (int64_t)1 << 20 || V > (int64_t)1 << 24 || first > (int64_t)1 << 30 || M > (int64_t)1 << 21 || M * H * es >= 0x7FFFFFFFll) return TPL_EUNSUPPORTED;
+    if (H % (16 / es) || H > (int64_t)1 << 20 || V > (int64_t)1 << 24 || first > (int64_t)1 << 30 || M > (int64_t)1 << 20 || M * H * es >= 0x7FFFFFFFll) return TPL_EUNSUPPORTED;
+    if (M * V > (int64_t)1 << 37) return TPL_EUNSUPPORTED;               // a launch has less than 2^32 threads, 512 to a tile of 256 x 128
     return TPL_OK;
 }
 size_t tp_layer_lm_loss_workspace_bytes(int dtype, int64_t M, int64_t H, int64_t V, int bwd) {
