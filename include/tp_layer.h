@@ -301,7 +301,7 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal,
  * freq: double [rot / 2] in device memory, radians per position.  positions: int32 [M] (16-byte aligned; the front of a pack plan is such
  * an array), or NULL: row m has position m % seq (seq > 0; not looked at where there are positions).  Any int32 is a position; the angle is
  * worked out in 64 bits.  qkv and out are [M, (nq + 2 nkv) dh], M < 2^24, whole 16-byte rows; out may be qkv itself (then only what is turned is
- * touched), but may not overlap it otherwise.
+ * touched), but may not overlap it otherwise (TPL_EINVAL).
  * tp_layer_rope_frequencies fills freq and factor in HOST memory: base^(-2 i / rot), for a context stretched `stretch` times
  *   TPL_ROPE_LINEAR  every frequency divided by stretch
  *   TPL_ROPE_BASE    base * stretch^(rot / (rot - 2)), which leaves pair 0 as it is and divides the last one

@@ -887,10 +887,10 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal, const
 
 // ---- rotary positions, attention of packed sequences, loss of a vocabulary shard ---------------------------------------
 int tp_layer_rope_frequencies(int rot, double base, int scaling, double stretch, double context, double* freq, float* factor) {
-    if (rot <= 0 || rot % 2 || !freq || !factor || !(base > 0.0)) return TPL_EINVAL;
+    if (rot <= 0 || rot % 2 || !freq || !factor || !(base > 0.0) || !std::isfinite(base)) return TPL_EINVAL;
     if (scaling < TPL_ROPE_PLAIN || scaling > TPL_ROPE_PARTS) return TPL_EINVAL;
-    if (scaling != TPL_ROPE_PLAIN && !(stretch > 0.0)) return TPL_EINVAL;
-    if (scaling == TPL_ROPE_PARTS && !(context > 0.0)) return TPL_EINVAL;
+    if (scaling != TPL_ROPE_PLAIN && (!(stretch > 0.0) || !std::isfinite(stretch))) return TPL_EINVAL;
+    if (scaling == TPL_ROPE_PARTS && (!(context > 0.0) || !std::isfinite(context))) return TPL_EINVAL;
     const double circle = 6.28318530717958647692;
     if (scaling == TPL_ROPE_BASE && rot > 2) base *= std::pow(stretch, (double)rot / (rot - 2));
     for (int i = 0; i < rot / 2; ++i) {
@@ -915,6 +915,8 @@ static int rope_call(bool back, int dtype, int64_t M, int nq, int nkv, int dh, i
     if (M >= (int64_t)1 << 24 || nq > 1 << 16 || nkv > 1 << 16 || dh > 8192) return TPL_EUNSUPPORTED;    // 2^32 threads, 256 for a token at least
     if (((int64_t)nq + 2 * nkv) * dh % (dtype == TPL_BF16 ? 8 : 4) || ((int64_t)nq + 2 * nkv) * dh * dh >= (int64_t)1 << 31) return TPL_EUNSUPPORTED;
     if (misaligned(in) || misaligned(out) || misaligned(freq) || misaligned(positions)) return TPL_EALIGN;
+    const uintptr_t lo = std::min((uintptr_t)in, (uintptr_t)out), hi = std::max((uintptr_t)in, (uintptr_t)out);
+    if (hi != lo && hi - lo < (uintptr_t)(M * ((int64_t)nq + 2 * nkv) * dh * (dtype == TPL_BF16 ? 2 : 4))) return TPL_EINVAL;
     RopeArgs a{};
     a.dtype = dtype; a.M = M; a.seq = seq; a.nq = nq; a.nkv = nkv; a.dh = dh; a.rot = rot; a.adjacent = pairs == TPL_ROPE_ADJACENT;
     a.freq = freq; a.factor = factor; a.positions = positions; a.in = in; a.out = out; a.stream = (hipStream_t)hip_stream;
