@@ -61,8 +61,14 @@ __device__ __forceinline__ void strip_of(const PlanParams& p, int side, int len,
         tile1 = (int)((rows + PACK_TILE - 1) / PACK_TILE);
     }
 }
-// Longest first, `top` above the longest.
-__device__ __forceinline__ int bucket_of(int tiles, int top) { return BUCKETS - 1 - min(BUCKETS - 1, (int)((float)tiles * ((float)(BUCKETS - 1) / (float)top))); }
+// Longest first, `top` above the longest.  Strips of up to LEVEL tiles, which memory bounds and not their length, stay in the order of the
+// rows: sorted, the units would all read the same part of every sequence at a time, and where lengths are equal and even those parts lie on the same channels
+// (forward, 8192 tokens, 16 / 2 heads of 128: 64 sequences of 128 42.5 -> 28.7 us, 32 of 256 37.6 -> 35.0, other lengths within 2 %; LEVEL = 4
+// takes 3 % more in backward).
+constexpr int LEVEL = 3;
+__device__ __forceinline__ int bucket_of(int tiles, int top) {
+    return BUCKETS - 1 - min(BUCKETS - 1, (int)((float)max(tiles, LEVEL) * ((float)(BUCKETS - 1) / (float)top)));
+}
 
 __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     __shared__ int tmp[PLAN_THREADS / 64];
