@@ -21,7 +21,7 @@ namespace tpl {
 
 constexpr int PACK_BLK = 128, PACK_TILE = 64;
 constexpr int PACK_MAX_GROUP = 128;
-constexpr int PACK_MIN_CHUNK = 8;         // tiles; shorter chunks cost more in their ends than they save
+constexpr int PACK_MIN_CHUNK = 8;         // tiles, half of it where strips are few, see pack_shares
 
 struct PackItem {
     int t0, len;           // the sequence: first row of the batch, length
@@ -65,9 +65,12 @@ inline PackLayout pack_layout(int64_t sequences, int64_t M, int64_t nq, int64_t 
 }
 // A chunk is no shorter than what a compute unit would have of all tiles if they were spread evenly, one workgroup to a unit: twice and four times
 // as many shares took 320, 330 and 351 us instead of 314 backward (12 documents of 8192 tokens, 16 / 2 heads of 128), 88, 92 and 110 instead of 87
-// forward, in sums written and read.  None where no strip can have two of the shortest chunks.
+// forward, in sums written and read.  At least 8 tiles, or 4 where all chunks then still find a unit (5 tiles of both sides to a share): 1000 tokens,
+// 8 heads of 128 forward 24.4 -> 16.3 us, backward 47.5 -> 40.4, 4 heads of 64 17.2 -> 13.0, 35.8 -> 24.9; 4 everywhere took 2 to 6 us more
+// of 15 and 30 us where strips fill the chip (4096 tokens in 24 sequences).  Nothing is cut, and no kernel joins, below 768 rows: 500 tokens of a head of 64
+// take 10.4 and 22.1 us, cut 11.3 and 20.3, 300 of 4 heads 8.1 and 15.5, with a join that finds nothing 9.7 and 17.8.
 inline PackShares pack_shares(int64_t M, int64_t nq, int64_t nkv, int units) {
-    if (M * (nq / nkv) < (int64_t)2 * PACK_MIN_CHUNK * PACK_TILE) return PackShares{{0, 0}};
+    if (M * (nq / nkv) < 768) return PackShares{{0, 0}};
     const int64_t each = (units + nkv - 1) / nkv;
     return PackShares{{each, each}};
 }

@@ -152,7 +152,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     for (int side = 0; side < 2; ++side) {
         const int* pre = before[side];
         int chunk = 1 << 30;
-        if (p.shares.of[side] > 0) chunk = max(PACK_MIN_CHUNK, (int)((tiles[side] + p.shares.of[side] - 1) / p.shares.of[side]));
+        const bool few = (int64_t)(tiles[0] + tiles[1]) <= 5 * p.shares.of[side];          // a compute unit and a quarter to a chunk at most
+        if (p.shares.of[side] > 0) chunk = max(few ? PACK_MIN_CHUNK / 2 : PACK_MIN_CHUNK, (int)((tiles[side] + p.shares.of[side] - 1) / p.shares.of[side]));
         const int top = min(longest[side], chunk) + 1;
         PackItem* items = reinterpret_cast<PackItem*>(p.plan + p.L.items[side]);
         PackItem* join = reinterpret_cast<PackItem*>(p.plan + p.L.joins[side]);
