@@ -150,6 +150,39 @@ def test_hidden_queries_do_not_matter(dtype, dh):
     ref.check(b.dqkv[cut:75], val["dqkv"][cut:75], tol["dqkv"][cut:75], "dqkv")   # keys that no spoilt query sees, and their own queries
 
 
+# The same where strips are cut into chunks: a chunk that holds a spoilt key or query is worked out again before it is joined.
+@pytest.mark.parametrize("dtype,dh", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+def test_hidden_values_in_cut_strips(dtype, dh):
+    nq, nkv, cut = 4, 2, 1370
+    b = Batch([1400, 60], nq, nkv, dh, True, dtype, behind=2)
+    val, tol = ref.attention(b.qkv, b.offsets, nq, nkv, dh, True, b.d_o)
+    b.qkv.view(b.M, nq + 2 * nkv, dh)[cut:1400, nq:] = math.inf
+    b.make_plan()
+    b.run()
+    for k in ("o", "lse"):
+        ref.check(b.outputs()[k][:cut], val[k][:cut], tol[k][:cut], k)
+    ref.check(b.dqkv[:cut, :nq * dh], val["dqkv"][:cut, :nq * dh], tol["dqkv"][:cut, :nq * dh], "dq")
+    for k, x in b.outputs().items():
+        ref.check(x[1400:1460], val[k][1400:1460], tol[k][1400:1460], k)
+
+
+@pytest.mark.parametrize("dtype,dh", [(torch.bfloat16, 64), (torch.bfloat16, 128), (torch.float32, 64)])
+def test_hidden_queries_in_cut_strips(dtype, dh):
+    nq, nkv, cut = 4, 2, 700
+    b = Batch([1400, 60], nq, nkv, dh, True, dtype)
+    val, tol = ref.attention(b.qkv, b.offsets, nq, nkv, dh, True, b.d_o)
+    b.d_o[:cut] = math.inf
+    b.qkv.view(b.M, nq + 2 * nkv, dh)[:cut, :nq] = math.nan
+    b.make_plan()
+    b.run()
+    ref.check(b.dqkv[cut:], val["dqkv"][cut:], tol["dqkv"][cut:], "dqkv")
+
+
+# Sequences of every length around a tile and a strip, all at once: chunks, whole strips, strips of one row
+def test_many_lengths():
+    _run(list(range(0, 70)) + [127, 128, 129, 255, 257, 1025], 3, 1, 64, True, torch.bfloat16, behind=1)
+
+
 def test_offsets_that_decrease_stay_in_bounds():
     b = Batch([40, 30, 30], 2, 1, 64, True, torch.bfloat16)
     b.on_gpu = torch.tensor([-5, 60, 20, 1000], dtype=torch.int32, device="cuda")      # taken as 0, 60, 60, 100
