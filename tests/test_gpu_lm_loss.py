@@ -91,6 +91,48 @@ def test_pieces(dtype, M, V):
     s.check()
 
 
+# Weights of more than 2 GiB: more than one piece also in forward.  Against 64 bits on the GPU, a slice of the vocabulary at a time.
+@pytest.mark.parametrize("dtype,M,H,V", [(torch.bfloat16, 24, 8192, 140000), (torch.float32, 9, 4096, 140000)])
+def test_many_weights(dtype, M, H, V):
+    import paper_2111_05972_amd as pkg
+    dt, st = pkg.TPL_BF16 if dtype == torch.bfloat16 else pkg.TPL_F32, torch.cuda.current_stream()
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x = torch.randn(M, H, device="cuda", generator=g).to(dtype)
+    w = (torch.randn(V, H, device="cuda", generator=g) * 0.02).to(dtype)
+    labels = torch.randint(0, V, (M,), device="cuda", generator=g, dtype=torch.int32)
+    labels[0] = V - 1
+    dloss = torch.rand(M, device="cuda", generator=g)
+    stats, loss, lse = torch.empty(1, M, 2, device="cuda"), torch.empty(M, device="cuda"), torch.empty(M, device="cuda")
+    ws = torch.empty(max(pkg.tp_layer_lm_loss_workspace_bytes(dt, M, H, V, b) for b in (0, 1)), dtype=torch.uint8, device="cuda")
+    dx, dw = torch.empty_like(x), torch.empty_like(w)
+    pkg.tp_layer_lm_loss_fwd(dt, M, H, V, 0, x, w, labels, stats, ws, stream=st)
+    pkg.tp_layer_lm_loss_join(M, 1, V, stats, labels, loss, lse, stream=st)
+    pkg.tp_layer_lm_loss_bwd(dt, M, H, V, 0, V, x, w, labels, lse, dloss, dx, dw, ws, stream=st)
+    torch.cuda.synchronize()
+    X, z, most = x.double(), torch.empty(M, V, dtype=torch.float64, device="cuda"), 0.0
+    for i in range(0, V, 10000):
+        t = w[i:i + 10000].double().t().contiguous()
+        z[:, i:i + 10000] = X @ t
+        most = max(most, (X.abs() @ t.abs()).max().item())
+    want = z.logsumexp(1)
+    off = (H + 8) * ref.F32 * most + (V + 32) * ref.F32 * (1 + want.abs().max().item())           # of a logit, of the sum
+    rows = torch.arange(M, device="cuda")
+    assert (lse.double() - want).abs().max().item() <= off
+    assert (loss.double() - (want - z[rows, labels.long()])).abs().max().item() <= 2 * off
+    dz = (z - want[:, None]).exp()
+    dz[rows, labels.long()] -= 1
+    dz *= dloss.double()[:, None]
+    # dz as an operand and what is stored: half a step each, as norms; float sums add far less
+    tol = 2 * ref.HALF[dtype] + (2 * off if dtype == torch.float32 else 0.0)
+    got_x, diff, norm = torch.zeros(M, H, dtype=torch.float64, device="cuda"), 0.0, 0.0
+    for i in range(0, V, 10000):
+        got_x += dz[:, i:i + 10000].contiguous() @ w[i:i + 10000].double()
+        t = dz[:, i:i + 10000].t().contiguous() @ X
+        diff, norm = diff + (dw[i:i + 10000].double() - t).norm().item() ** 2, norm + t.norm().item() ** 2
+    assert (dx.double() - got_x).norm() <= tol * got_x.norm()
+    assert diff ** 0.5 <= tol * norm ** 0.5
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 def test_all_ignored(dtype):
     s = Shards(40, 64, 100, 1, dtype)

@@ -183,6 +183,36 @@ def test_many_lengths():
     _run(list(range(0, 70)) + [127, 128, 129, 255, 257, 1025], 3, 1, 64, True, torch.bfloat16, behind=1)
 
 
+# Rows and values past 2^31 bytes and 2^31 elements: the last documents of a batch of a million tokens
+def test_a_long_batch():
+    pkg = _pkg()
+    nq, nkv, dh, each, tail = 16, 2, 128, 500, 1000
+    M = 1000000
+    n = M // each
+    st = torch.cuda.current_stream()
+    g = torch.Generator(device="cuda").manual_seed(4)
+    qkv = torch.empty(M, (nq + 2 * nkv) * dh, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    d_o = torch.empty(M, nq * dh, dtype=torch.bfloat16, device="cuda").normal_(generator=g)
+    before = qkv[-tail:].clone()
+    offsets = torch.arange(0, M + 1, each, dtype=torch.int32, device="cuda")
+    plan = torch.empty(pkg.tp_layer_pack_plan_bytes(n, M, nq, nkv), dtype=torch.uint8, device="cuda")
+    dims = (pkg.TPL_BF16, n, M, nq, nkv, dh, True)
+    ws = torch.empty(max(pkg.tp_layer_attn_packed_workspace_bytes(*dims, b) for b in (0, 1)), dtype=torch.uint8, device="cuda")
+    freq, factor = pkg.tp_layer_rope_frequencies(dh)
+    pkg.tp_layer_pack_plan(n, M, offsets, nq, nkv, True, plan, stream=st)
+    on_gpu = torch.tensor(freq, dtype=torch.float64, device="cuda")
+    pkg.tp_layer_rope_fwd(pkg.TPL_BF16, M, nq, nkv, dh, dh, 0, on_gpu, factor, plan[:4 * M].view(torch.int32), qkv, qkv, stream=st)
+    o, lse, dsum, dqkv = torch.empty_like(d_o), torch.empty(M, nq, device="cuda"), torch.empty(M, nq, device="cuda"), torch.empty_like(qkv)
+    pkg.tp_layer_attn_packed_fwd(*dims, plan, qkv, o, lse, ws, stream=st)
+    pkg.tp_layer_attn_packed_bwd(*dims, plan, qkv, o, lse, d_o, dqkv, dsum, ws, stream=st)
+    torch.cuda.synchronize()
+    val, tol = ref.rotary(before, nq, nkv, dh, dh, False, torch.arange(tail) % each, freq, factor, False)
+    ref.check(qkv[-tail:], val, tol, "turned")
+    val, tol = ref.attention(qkv[-tail:], [0, each, tail], nq, nkv, dh, True, d_o[-tail:])
+    for k, x in (("o", o), ("lse", lse), ("dqkv", dqkv)):
+        ref.check(x[-tail:], val[k], tol[k], k)
+
+
 def test_offsets_that_decrease_stay_in_bounds():
     b = Batch([40, 30, 30], 2, 1, 64, True, torch.bfloat16)
     b.on_gpu = torch.tensor([-5, 60, 20, 1000], dtype=torch.int32, device="cuda")      # taken as 0, 60, 60, 100
