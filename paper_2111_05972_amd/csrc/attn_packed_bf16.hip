@@ -58,24 +58,29 @@ template <int DH, int NT> struct FlatTile {
             col[i] = c * 8 < dh ? (unsigned)c * 16u : HEAD_OOB;
         }
     }
-    // flattened rows 64 qt ... of q (row stride ld) and d (ldo) into the LDS tiles at lds_q and lds_d
-    __device__ __forceinline__ void load(const Params& p, const BStrip& s, const bf16_t* d, int qt, unsigned lds_q, unsigned lds_d, int wave) const {
+    // flattened rows 64 qt ... of a tensor whose queries have row stride ld into the LDS tile at `lds`; zeros past the sequence
+    __device__ __forceinline__ void load(const Params& p, const BStrip& s, const bf16_t* base, int64_t ld, int qt, unsigned lds, int wave) const {
         const int r0 = qt * PACK_TILE, q0 = r0 / p.G, skip = r0 - q0 * p.G;          // uniform
         const int left = min(s.it.len - q0, (PACK_TILE - 1 + skip) / p.G + 1);       // queries of the tile
-        const unsigned tail = (unsigned)(p.G * p.dh * 2);
-        const i32x4 rq = make_rsrc(s.q + q0 * s.ld, (unsigned)((left - 1) * s.ld * 2) + tail);
-        const i32x4 rd = make_rsrc(d + q0 * s.ldo, (unsigned)((left - 1) * s.ldo * 2) + tail);
+        const i32x4 r = make_rsrc(base + q0 * ld, left > 0 ? (unsigned)((left - 1) * ld * 2) + (unsigned)(p.G * p.dh * 2) : 0u);
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if ((i + 1) * NT <= PACK_TILE * DH / 8 || i * NT + wave * 64 < PACK_TILE * DH / 8) {
                 const unsigned x = (unsigned)(row[i] + skip), q = x * p.div_g >> 16, g = x - q * (unsigned)p.G;
-                const unsigned head = g * (unsigned)(p.dh * 2) + col[i], dst = (unsigned)(i * NT + wave * 64) * 16u;
                 const bool in = (int)q < left && col[i] != HEAD_OOB;
-                buffer_load_lds_b128(rq, lds_q + dst, in ? q * (unsigned)(s.ld * 2) + head : HEAD_OOB);
-                buffer_load_lds_b128(rd, lds_d + dst, in ? q * (unsigned)(s.ldo * 2) + head : HEAD_OOB);
+                buffer_load_lds_b128(r, lds + (unsigned)(i * NT + wave * 64) * 16u, in ? q * (unsigned)(ld * 2) + g * (unsigned)(p.dh * 2) + col[i] : HEAD_OOB);
             }
     }
 };
+// The rows that a wavefront keeps in registers, 32 of a strip's 128, come through LDS too, two tiles at `strip`: loads of a lane's own row touch 32 lines of
+// 128 bytes each, and every line four times (16 sequences of 512, 16 / 2 heads of 128: dQ waited 5.3 us of 14 to a strip for Q and dO, so 3.2; backward
+// 145 -> 139 us, 120.8 -> 113.0 with 256 to a sequence; sequences of 16 tokens with heads of 64 take 9 % longer, the rest within 2 %).
+template <int DH> __device__ __forceinline__ void strip_frags(bf16x8 (&f)[DH / 16], unsigned strip, int quarter, int lane) {
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) f[ks] = lds_frag_k<0>(strip + (quarter >> 1) * tile_bytes<DH>() + frag_k_off<DH>((quarter & 1) * 32, ks, lane));
+#pragma unroll
+    for (int ks = 0; ks < DH / 16; ++ks) settle(f[ks]);
+}
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
 // Workgroup = (128 flattened rows, key head), four wavefronts of 32 rows each, two workgroups to a unit; K and V in tiles of 64 through two LDS
@@ -99,10 +104,6 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
     const int q_lo = (int)((unsigned)min(r0, s.rows - 1) / (unsigned)p.G), q_hi = (int)((unsigned)min(r0 + 31, s.rows - 1) / (unsigned)p.G);
     const float c2 = LOG2E * p.scale;
 
-    bf16x8 qf[NF];
-    const bf16_t* qrow = s.q + me.q * s.ld + me.g * p.dh;
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) qf[ks] = frag_k_global(qrow, 0, 0, valid ? 1 : 0, p.dh, ks, lane);
     f32x16 oacc[NT];
 #pragma unroll
     for (int dt = 0; dt < NT; ++dt) oacc[dt] = zero16();
@@ -124,10 +125,14 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
 #pragma unroll
         for (int g = 0; g < 2; ++g) { va[dt][g] = lds0 + TB + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(va[dt][g]); }
     fetch_tile(s.it.tile0, lds0);
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) settle(qf[ks]);
+    FlatTile<DH, WAVES4> ft;
+    ft.init(p.dh, t);
+    for (int j = 0; j < 2; ++j) ft.load(p, s, s.q, s.ld, s.it.first / PACK_TILE + j, lds0 + (2 + j) * TB, wave);
     dma_wait();
     __syncthreads();
+    bf16x8 qf[NF];
+    strip_frags<DH>(qf, lds0 + 2 * TB, wave, lane);
+    __syncthreads();                                              // the second stage is free
     auto step = [&](int kt, auto stg) __attribute__((always_inline)) {
         constexpr int SOFF = decltype(stg)::value * 2 * TB;
         if (kt + 1 < s.it.tile1) fetch_tile(kt + 1, lds0 + (1 - decltype(stg)::value) * 2 * TB);
@@ -405,9 +410,6 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
     const bf16_t* dobase = p.d_o + s.it.t0 * s.ldo + (int64_t)s.hk * G * p.dh;
     const float c2 = LOG2E * p.scale;
 
-    bf16x8 own[NF];                                        // K for the scores, V for dP
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) own[ks] = frag_k_global(DK_ROLE ? s.v : s.k, s.ld, kv, len, p.dh, ks, lane);
     f32x16 acc[NT];                                        // dK (DK_ROLE) or dV
 #pragma unroll
     for (int dt = 0; dt < NT; ++dt) acc[dt] = zero16();
@@ -418,7 +420,8 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
     ft.init(p.dh, t);
     float rl = 0.0f, rd = 0.0f;
     auto g2r = [&](int qt, int stage) {
-        ft.load(p, s, dobase, qt, lds0 + stage * TB, lds0 + (3 + ((qt - qt0) & 1)) * TB, wave);
+        ft.load(p, s, s.q, s.ld, qt, lds0 + stage * TB, wave);
+        ft.load(p, s, dobase, s.ldo, qt, lds0 + (3 + ((qt - qt0) & 1)) * TB, wave);
         if (t < PACK_TILE) {
             const int r = qt * PACK_TILE + t;
             const Row w = row_of(p, r);
@@ -449,10 +452,22 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
     char* pbuf = smem + PS + (wave & 3) * P_BYTES + lane * 16;
     g2r(qt0, 0);
     r2s(0);
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) settle(own[ks]);
+    // the strip's K into the second and third stage of Q, its V into the second of dO and where P will be
+    constexpr unsigned V1 = PS - 4 * TB;
+    static_assert(TB <= 2 * 4 * P_BYTES, "half a strip of V fits where P will be");
+    {
+        unsigned off[NCHUNKS<DH, WAVES8>];
+        dma_offsets<DH, WAVES8>(off, s.ld, p.dh, t);
+        for (int j = 0; j < 2; ++j) {
+            tile_dma<DH, WAVES8>(tile_rsrc(s.k, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + (1 + j) * TB, off, 0, wave);
+            tile_dma<DH, WAVES8>(tile_rsrc(s.v, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + 4 * TB + j * V1, off, 0, wave);
+        }
+    }
     dma_wait();
     __syncthreads();
+    bf16x8 own[NF];                                        // K for the scores, V for dP
+    strip_frags<DH>(own, DK_ROLE ? lds0 + 4 * TB + ((wave >> 1) & 1) * (V1 - TB) : lds0 + TB, wave & 3, lane);
+    __syncthreads();                                       // those stages are free
 
     // rows that see one of this wavefront's keys, in scalar registers: with the products in the loop it spilled
     const int see_lo = __builtin_amdgcn_readfirstlane(CAUSAL ? k0 * G - 31 : 0), see_hi = __builtin_amdgcn_readfirstlane(k0 < len ? rows : 0);
@@ -604,7 +619,7 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
 // Workgroup = (128 flattened rows, key head), 8 wavefronts: w takes 32 rows (w % 4) and one 32-key half (w / 4) of every tile; the
 // halves are added through LDS at the end.  Transposed score tile: lane = row.
-template <int DH> constexpr int dq_lds() { return std::max(4 * tile_bytes<DH>(), 4 * 64 * (DH / 2) * 4); }
+template <int DH> constexpr int dq_lds() { return std::max(6 * tile_bytes<DH>(), 4 * 64 * (DH / 2) * 4); }
 template <int DH, bool CAUSAL>
 __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStrip& s) {
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32;
@@ -620,12 +635,6 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
     const int64_t at = s.row0 + (int64_t)me.q * p.nq + me.g;
     const float l2 = valid ? p.lse[at] * LOG2E : 0.0f, dsum = valid ? p.dsum[at] : 0.0f;
     const bf16_t* dobase = p.d_o + s.it.t0 * s.ldo + (int64_t)s.hk * p.G * p.dh;
-    bf16x8 qf[NF], dof[NF];
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) {
-        qf[ks] = frag_k_global(s.q + me.q * s.ld + me.g * p.dh, 0, 0, valid ? 1 : 0, p.dh, ks, lane);
-        dof[ks] = frag_k_global(dobase + me.q * s.ldo + me.g * p.dh, 0, 0, valid ? 1 : 0, p.dh, ks, lane);
-    }
     f32x16 dq[NT];
 #pragma unroll
     for (int dt = 0; dt < NT; ++dt) dq[dt] = zero16();
@@ -640,12 +649,20 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
         tile_dma<DH, WAVES8>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
     };
     fetch_tile(tile0, lds0);
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) { settle(qf[ks]); settle(dof[ks]); }
+    FlatTile<DH, WAVES8> ft;
+    ft.init(p.dh, t);
+    for (int j = 0; j < 2; ++j) {
+        ft.load(p, s, s.q, s.ld, s.it.first / PACK_TILE + j, lds0 + (2 + j) * TB, wave);
+        ft.load(p, s, dobase, s.ldo, s.it.first / PACK_TILE + j, lds0 + (4 + j) * TB, wave);
+    }
     settle(l2);
     settle(dsum);
     dma_wait();
     __syncthreads();
+    bf16x8 qf[NF], dof[NF];
+    strip_frags<DH>(qf, lds0 + 2 * TB, qs, lane);
+    strip_frags<DH>(dof, lds0 + 4 * TB, qs, lane);
+    __syncthreads();                                       // the second stage is free
     unsigned ka[NF], ta[NT][2];
 #pragma unroll
     for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(kvh * 32, ks, lane); keep_in_register(ka[ks]); }
