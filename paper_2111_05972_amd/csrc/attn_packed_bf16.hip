@@ -84,7 +84,8 @@ template <int DH> __device__ __forceinline__ void strip_frags(bf16x8 (&f)[DH / 1
 
 // ---- forward ----------------------------------------------------------------------------------------------------------
 // Workgroup = (128 flattened rows, key head), four wavefronts of 32 rows each, two workgroups to a unit; K and V in tiles of 64 through two LDS
-// stages.  Eight wavefronts, two to 32 rows with half of each tile's keys, halve the chain of dependent steps but read K and V by rows twice:
+// stages.  Bound by what the products, the softmax and the LDS reads of a step take one after another: 16384 tokens in 3 documents, 12 / 4 heads of 128, causal
+// 389 us, 971 TFLOP/s (a library product of 8192^3 reaches 1370 to 1600); 12 documents of 8192 tokens, 16 / 2 heads 87 us.  Eight wavefronts, two to 32 rows with half of each tile's keys, halve the chain of dependent steps but read K and V by rows twice:
 // where a unit has one strip they took -5 to +10 % of the time, where it has two up to 38 % more (4096 tokens of 32 to 800, 16 / 2 heads of 128).
 constexpr int WAVES4 = 256;
 template <int DH> constexpr int fwd_lds() { return 4 * tile_bytes<DH>(); }
@@ -267,7 +268,8 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
 // D = rowsum(dO * O) where a row has many keys.  O has been rounded, by up to 2^-9 of itself, and where keys are few O is as large as V, so that
 // the difference dP - D loses half of its digits (error of dQ and dK against 64 bits with correctly rounded ones = 1: 2.3 for sequences of 2 tokens, 1.8 for 8,
 // 1.5 for 64, 1.43 for 512).  Rows of at most 64 keys, a tile, therefore get D = rowsum(P * dP), the same sum from unrounded terms: two of the three
-// products of dQ, for the strips that begin with such rows.  Workgroups [0, strips) walk those, the others the rows.
+// products of dQ, for the strips that begin with such rows.  Workgroups [0, strips) walk those, the others the rows.  Bound by memory: 18 us for the
+// 67 MB of O and dO of 8192 tokens of 16 heads of 128 in 12 documents, 25 us where all of 128 sequences have 64 tokens.
 template <int DH> constexpr int dsum_lds() { return 2 * tile_bytes<DH>(); }
 template <int DH, bool CAUSAL>
 __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, int strips) {
@@ -396,6 +398,8 @@ __device__ __forceinline__ void dq_rows_again(float* q_s, const Params& p, const
 // Workgroup = (128 keys, key head), 8 wavefronts: w and w + 4 share 32 keys.  w works out scores and probabilities and accumulates
 // dV; w + 4 works out dP and accumulates dK from the same probabilities, which it gets through LDS in float one sub-tile of 32 rows
 // later.  Tiles of 64 flattened rows: Q, LSE and D through three stages, as dK still reads the tile before, dO through two.
+// Bound by LDS: every 32 keys read the tile of Q and of dO twice, 256 KiB and 64 of P against four products of 64 x 128 x 128, and the three kinds of work
+// add up: 2.75 us a tile, 0.78 PFLOP/s over the chip.  12 documents of 8192 tokens, 16 / 2 heads of 128: 334 workgroups of 128 us, before those of dQ.
 constexpr int WAVES8 = 512;
 constexpr int P_BYTES = 32 * 32 * 4;
 template <int DH> constexpr int dkv_lds() { return 5 * tile_bytes<DH>() + 3 * 2 * PACK_TILE * 4 + 2 * 4 * P_BYTES; }
@@ -618,7 +622,8 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
 
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
 // Workgroup = (128 flattened rows, key head), 8 wavefronts: w takes 32 rows (w % 4) and one 32-key half (w / 4) of every tile; the
-// halves are added through LDS at the end.  Transposed score tile: lane = row.
+// halves are added through LDS at the end.  Transposed score tile: lane = row.  1.18 us a tile, 1.36 PFLOP/s over the chip, and about 6 us to begin and
+// end a strip (item 0.9, loads 2.6 to 3.2, end 2.2): 1038 workgroups of 22 us in the batch above, both lists in one launch of 276 us.
 template <int DH> constexpr int dq_lds() { return std::max(6 * tile_bytes<DH>(), 4 * 64 * (DH / 2) * 4); }
 template <int DH, bool CAUSAL>
 __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStrip& s) {

@@ -1,5 +1,7 @@
 // Rotary positions for gfx950: the first `rot` columns of every q and k head in rows of (q | k | v, head, dh) are turned, pair by
-// pair, by the angle position * frequency; backward turns back.  Bound by memory: every element is read and written once.
+// pair, by the angle position * frequency; backward turns back.  Bound by memory: every element is read and written once.  8192 tokens of
+// 12 + 2 x 12 heads of 128 in bf16, 151 MB: 24.5 us, 6.2 TB/s (some of it out of the infinity cache; a copy of 512 MiB reaches 5.4); 3001 tokens of
+// 32 + 2 x 8 heads of 80 in float, 92 MB: 16 us, 5.8 TB/s; 64 tokens 3.3 us, a launch.
 //
 // Angles are worked out here and not read from a table: one per (token, pair), shared by all heads through LDS.  position *
 // frequency is a product of 64 bits whose whole turns are taken off before it is rounded to 32 (at position 1e6 a 32-bit angle
