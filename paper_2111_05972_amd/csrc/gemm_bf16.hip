@@ -2086,7 +2086,8 @@ bool takes_wide_tile(const GemmArgs* g, int n, const GroupPlan& wide, const Grou
 
 bool any_acc(const GemmArgs* g, int n) { return std::any_of(g, g + n, [](const GemmArgs& a) { return a.acc != nullptr; }); }
 GroupPlan make_group_plan(const GemmArgs* g, int n) {
-    const int forced = n == 1 ? 256 : any_acc(g, n) ? 0 : options().gemm_group;       // one GEMM: see by_turns
+    // one GEMM: see by_turns; scaled ones have no kernel of 128 x 256, and the option is for those of a layer
+    const int forced = n == 1 ? 256 : g[0].epi == EPI_SCALE ? -1 : options().gemm_group;
     double us = INFINITY;
     GroupPlan best{};
     if (!any_acc(g, n)) best = make_small_plan(g, n, forced, &us);    // running sums: the tiles by turns only, which have the epilogue

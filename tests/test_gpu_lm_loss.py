@@ -152,6 +152,17 @@ def test_large_logits(dtype):
     assert torch.isfinite(s.loss).all()
 
 
+# The options that force the tiles of a layer's products leave the loss right, whatever they are set to.
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("name,value", [("gemm_group", g) for g in ("0", "64", "128", "192", "256", "384", "512")] + [("gemm_tile", "8"), ("gemm_shares", "3"), ("gemm_band", "2")])
+def test_options(tune, name, value, dtype):
+    tune.set(name, value)
+    s = Shards(300, 520, 2055, 1, dtype)
+    s.run()
+    torch.cuda.synchronize()
+    s.check()
+
+
 def test_captured_and_replayed():
     s = Shards(150, 128, 1003, 1, torch.bfloat16)
     s.run()
