@@ -83,17 +83,29 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     int* const before[2] = {fits ? near[0] : p.plan + p.L.pre[0], fits ? near[1] : p.plan + p.L.pre[1]};   // strips before each sequence
     auto offset = [&](int i) { return min(max(p.offsets[i], 0), p.M); };
     if (blockIdx.x > 0) {
-        // This workgroup's tokens, each looking for its sequence among the offsets.  Where these decrease, their running maximum would be
-        // needed: the lists do not come from here, so what is wrong then is a position, or how exactly a row's D is summed.
-        for (int64_t m = (int64_t)(blockIdx.x - 1) * PLAN_THREADS + t; m < p.M; m += (int64_t)(gridDim.x - 1) * PLAN_THREADS) {
-            int lo = 0, hi = p.n;                                  // the last i with offset(i) <= m
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (offset(mid) <= m) lo = mid; else hi = mid - 1;
+        // This workgroup's tokens, each looking for its sequence among the running maxima of the offsets, 1024 sequences at a time.
+        const int64_t step = (int64_t)(gridDim.x - 1) * PLAN_THREADS, m0 = (int64_t)(blockIdx.x - 1) * PLAN_THREADS + t;
+        for (int64_t m = m0; m < p.M; m += step) p.plan[m] = p.plan[p.L.seen + m] = 0;
+        int* begin = near[0];                                      // of these sequences, and the end of the last
+        int carry = 0;
+        for (int base = 0; base < p.n; base += PLAN_THREADS) {
+            const int i = base + t, count = min(p.n - base, PLAN_THREADS);
+            int all;
+            begin[t] = max(block_scan<true>(i <= p.n ? offset(i) : 0, tmp, all), carry);
+            carry = max(carry, all);
+            if (t == 0) begin[PLAN_THREADS] = max(carry, base + PLAN_THREADS <= p.n ? offset(base + PLAN_THREADS) : 0);
+            __syncthreads();
+            for (int64_t m = m0; m < p.M; m += step) {
+                if (m < begin[0] || m >= begin[count]) continue;
+                int lo = 0, hi = count - 1;                        // the last with begin <= m
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (begin[mid] <= m) lo = mid; else hi = mid - 1;
+                }
+                p.plan[m] = (int)m - begin[lo];
+                p.plan[p.L.seen + m] = p.causal ? (int)m - begin[lo] + 1 : begin[lo + 1] - begin[lo];
             }
-            const bool in = lo < p.n && offset(lo) <= m;
-            p.plan[m] = in ? (int)m - offset(lo) : 0;
-            p.plan[p.L.seen + m] = !in ? 0 : p.causal ? (int)m - offset(lo) + 1 : offset(lo + 1) - offset(lo);
+            __syncthreads();
         }
         return;
     }
@@ -218,7 +230,7 @@ hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, i
     p.shares = pack_shares(M, nq, nkv, compute_units());
     p.offsets = offsets; p.plan = plan;
     p.L = pack_layout(sequences, M, nq, nkv, p.shares);
-    static_assert(BUCKETS == PLAN_THREADS, "a thread to a bucket");
+    static_assert(BUCKETS == PLAN_THREADS && NEAR > PLAN_THREADS, "a thread to a bucket, 1024 sequences and an end in LDS");
     const int64_t groups = std::min<int64_t>((M + PLAN_THREADS - 1) / PLAN_THREADS, 1024);
     hipLaunchKernelGGL(pack_plan_kernel, dim3((unsigned)(1 + groups)), dim3(PLAN_THREADS), 0, s, p);
     return hipGetLastError();

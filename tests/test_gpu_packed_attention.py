@@ -222,6 +222,33 @@ def test_offsets_that_decrease_stay_in_bounds():
     b.check()
 
 
+@pytest.mark.parametrize("causal", [True, False])
+def test_offsets_that_decrease_are_their_running_maximum(causal):
+    b = Batch([200, 0, 100, 50], 2, 1, 64, causal, torch.bfloat16, behind=3)
+    b.on_gpu = torch.tensor([0, 200, 90, 300, 350], dtype=torch.int32, device="cuda")          # 0, 200, 200, 300, 350
+    b.dsum.fill_(math.nan)
+    b.make_plan()
+    assert b.plan.view(torch.int32)[:b.M].tolist() == list(range(200)) + list(range(100)) + list(range(50)) + [0] * 3
+    b.run()
+    b.check()
+
+
+# More sequences than a workgroup of the plan has threads, and than it keeps in LDS; empty ones and a decrease among them
+@pytest.mark.parametrize("n", [1023, 1024, 1025, 2047, 2048, 2500])
+def test_many_sequences(n):
+    g = torch.Generator().manual_seed(n)
+    lengths = torch.randint(0, 5, (n,), generator=g).tolist()
+    lengths[n // 2], lengths[n - 1] = 150, 3
+    b = Batch(lengths, 2, 1, 32, True, torch.bfloat16, behind=2)
+    b.on_gpu[n // 3] = 1                                            # before it all is larger: the sequence before ends where this one did not
+    b.offsets = torch.tensor(b.on_gpu.tolist()).cummax(0)[0].tolist()
+    b.make_plan()
+    want = [i for a, z in zip(b.offsets[:-1], b.offsets[1:]) for i in range(z - a)] + [0] * 2
+    assert b.plan.view(torch.int32)[:b.M].tolist() == want
+    b.run()
+    b.check()
+
+
 def test_another_plan_writes_nothing():
     b = Batch([40, 30], 2, 1, 64, True, torch.bfloat16)
     other = Batch([40, 30], 2, 1, 64, False, torch.bfloat16)
