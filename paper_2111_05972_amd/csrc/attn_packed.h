@@ -35,8 +35,8 @@ struct PackHeader {
     int sequences, tokens, nq, nkv, causal;
     int items[2];          // [0]: forward and dQ, [1]: dK, dV
     int joins[2];          // strips that were cut
-    int first_short;       // strips of one or two tiles of list 0 are items from here on (longer ones may be among them)
-    int pad[6];
+    int first_short[2];    // strips of one or two tiles are items from here on (longer ones may be among them)
+    int pad[5];
 };
 // Word offsets of the plan's parts; a function of what the host knows, so host and device agree without a copy.
 struct PackLayout {

@@ -22,7 +22,7 @@ struct PackParams {
     const T* qkv; T* o; float* lse;
     const T* d_o; T* dqkv; float* dsum;
     float* part[2];               // sums of chunks: forward or dQ, dK and dV
-    int kv_wgs;                   // backward: workgroups of dK/dV, before those of dQ
+    int kv_items;                 // bf16 backward: items of list 1 at most
     float scale;
 };
 // What a workgroup works on.
@@ -52,10 +52,17 @@ template <typename T>
 __device__ __forceinline__ bool take_strip(const PackParams<T>& p, int side, int wg, Strip<T>& s) {
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
     const int i = wg / p.nkv;
-    s.it = pack_items(p.plan, p.items[side])[i];                  // within the list's capacity; requested beside the header, not after it
+    s.it = pack_items(p.plan, p.items[side])[i];                  // within the plan: requested beside the header, not after it
     if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal) || i >= h->items[side]) return false;
     set_strip(p, wg - i * p.nkv, s);
     return true;
+}
+// Item `i` of list `side`, counted with the key heads as above.
+template <typename T>
+__device__ __forceinline__ void strip_at(const PackParams<T>& p, int side, int i, Strip<T>& s) {
+    const int n = i / p.nkv;
+    s.it = pack_items(p.plan, p.items[side])[n];
+    set_strip(p, i - n * p.nkv, s);
 }
 // A flattened row: its query and its head in the group.
 struct Row { int q, g; };

@@ -45,13 +45,40 @@ __device__ __forceinline__ void xfetch_flat(const FParams& p, const FStrip& s, c
     }
 }
 
+// Workgroup `u` of a launch: a quarter of a strip of list 0 (forward), of list 1 or 0 (backward).  Long strips by lists, their four quarters one after
+// another, longest first; then the short ones (first_short), all first quarters, all second ones and so on, as those of short sequences have no more
+// than one: workgroups without work among the others made these wait (52 sequences of 117 tokens together, 8 heads of 128: forward 66 us, so 21, backward
+// 193, so 59; all strips that way: 29 sequences of 9224 tokens, 8 heads of 32, forward 62 -> 74).  False: there is no such quarter.
+__device__ __forceinline__ bool take_quarter(const FParams& p, bool bwd, int u, FStrip& s, int& side, int& sub) {
+    const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
+    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return false;
+    const int first[2] = {h->first_short[0] * p.nkv, bwd ? h->first_short[1] * p.nkv : 0};
+    const int after[2] = {h->items[0] * p.nkv - first[0], bwd ? h->items[1] * p.nkv - first[1] : 0};        // short ones
+    for (side = 1; side >= 0; --side) {
+        if (u < QUARTERS * first[side]) {
+            sub = u % QUARTERS;
+            strip_at(p, side, u / QUARTERS, s);
+            return true;
+        }
+        u -= QUARTERS * first[side];
+    }
+    const int all = after[0] + after[1];
+    if (u >= QUARTERS * all) return false;
+    sub = u / all;
+    u -= sub * all;
+    side = u < after[1];
+    strip_at(p, side, side ? first[1] + u : first[0] + u - after[1], s);
+    return true;
+}
+
 template <int DH>
 __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TB = xtile_bytes<DH>(), NL = xloads<DH>();
     FStrip s;
-    if (!take_strip(p, 0, blockIdx.x / QUARTERS, s)) return;
-    const int sub = blockIdx.x % QUARTERS, r0 = s.it.first + sub * XT, len = s.it.len;
+    int side, sub;
+    if (!take_quarter(p, false, blockIdx.x, s, side, sub)) return;
+    const int r0 = s.it.first + sub * XT, len = s.it.len;
     if (r0 >= s.rows) return;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = r0 + (lane & 31);
@@ -363,12 +390,10 @@ template <int DH>
 __global__ __launch_bounds__(256, DH <= 64 ? 2 : 1) void attn_packed_f32_bwd_kernel(FParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     FStrip s;
-    const int wg = blockIdx.x / QUARTERS, sub = blockIdx.x % QUARTERS;
-    if (wg >= p.kv_wgs) {
-        if (take_strip(p, 0, wg - p.kv_wgs, s)) f32_dq<DH>(smem, p, s, sub);
-    } else if (take_strip(p, 1, wg, s)) {
-        f32_dkv<DH>(smem, p, s, sub);
-    }
+    int side, sub;
+    if (!take_quarter(p, true, blockIdx.x, s, side, sub)) return;
+    if (side) f32_dkv<DH>(smem, p, s, sub);
+    else f32_dq<DH>(smem, p, s, sub);
 }
 
 template <int DH>
@@ -392,7 +417,6 @@ hipError_t run(const PackAttnArgs& a, bool bwd) {
     p.part[1] = (float*)((char*)a.ws + ws_of(a, true).part[0]);
     hipLaunchKernelGGL(attn_packed_f32_dsum_kernel, dim3((unsigned)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units())), dim3(256), 0, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    p.kv_wgs = (int)(L.cap[1] * a.nkv);
     hipLaunchKernelGGL(attn_packed_f32_bwd_kernel<DH>, dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);

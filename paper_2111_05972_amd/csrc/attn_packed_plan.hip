@@ -74,7 +74,7 @@ __device__ __forceinline__ int bucket_of(int tiles, int top) {
 __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     __shared__ int tmp[PLAN_THREADS / 64];
     __shared__ int hist[2][BUCKETS];
-    __shared__ int longest[2], slots[2], joins[2], first_short;
+    __shared__ int longest[2], slots[2], joins[2], first_short[2];
     __shared__ unsigned long long tiles[2];
     __shared__ int near[3][NEAR];                                  // what the searches read, where it fits
     const int t = threadIdx.x, G = p.nq / p.nkv;
@@ -109,8 +109,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         }
         return;
     }
-    if (t == 0) first_short = 0;
-    if (t < 2) { longest[t] = 0; slots[t] = 0; joins[t] = 0; tiles[t] = 0; }
+    if (t < 2) { first_short[t] = 0; longest[t] = 0; slots[t] = 0; joins[t] = 0; tiles[t] = 0; }
     hist[0][t] = hist[1][t] = 0;
     __syncthreads();
     // offsets as running maxima, and the strips before each sequence
@@ -207,7 +206,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                 int all;
                 const int v = hist[side][t], at = block_scan<false>(v, tmp, all) - v;
                 hist[side][t] = at;
-                if (side == 0 && t == bucket_of(2, top)) first_short = at;
+                if (t == bucket_of(2, top)) first_short[side] = at;
                 __syncthreads();
             }
         }
@@ -215,7 +214,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
             PackHeader* h = reinterpret_cast<PackHeader*>(p.plan + p.L.header);
             h->items[side] = min(hist[side][BUCKETS - 1], (int)p.L.cap[side]);   // the end of the last bucket
             h->joins[side] = min(joins[side], (int)p.L.join_cap[side]);
-            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->causal = p.causal; h->first_short = first_short; }
+            h->first_short[side] = min(first_short[side], h->items[side]);
+            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->causal = p.causal; }
         }
     }
 }
