@@ -40,7 +40,8 @@ struct LossParams {
     float* target;             // [M], written by the tile that holds a row's label
     int part0;                 // tiles of columns before this piece
     // backward
-    const float* lse; const float* dloss; const float* alpha;
+    const float* lse; const float* dloss; float* alpha;
+    int own_alpha;             // alpha is worked out by the workgroups that use it, and left for the launches behind
     int vocab;                 // labels outside [0, vocab) are ignored
     bf16_t* dz; int ldz;       // [M, ldz], columns past the piece zero
 };
@@ -124,9 +125,9 @@ __device__ __forceinline__ void stats_epilogue(const LossParams& lp, const PPAcc
 
 // A block of 16 rows of dz.
 struct RowTerms { int label; float lse2, d; };
-__device__ __forceinline__ RowTerms row_terms(const LossParams& lp, int row) {
+__device__ __forceinline__ RowTerms row_terms(const LossParams& lp, int row, float alpha) {
     const int at = row < lp.g.M ? row : 0;
-    return RowTerms{lp.labels[at], lp.lse[at] * LOG2E, lp.dloss[at] / *lp.alpha};
+    return RowTerms{lp.labels[at], lp.lse[at] * LOG2E, lp.dloss[at] / alpha};
 }
 __device__ __forceinline__ void grad_block(const LossParams& lp, const PPLane& el, const f32x4 (&x)[4], int row, const RowTerms& r) {
     const GemmParams& p = lp.g;
@@ -147,28 +148,52 @@ __device__ __forceinline__ void grad_block(const LossParams& lp, const PPLane& e
     }
 }
 template <typename TL>
-__device__ __forceinline__ void grad_epilogue(const LossParams& lp, const PPAcc<TL>& acc, const PPWork& w) {
+__device__ __forceinline__ void grad_epilogue(const LossParams& lp, const PPAcc<TL>& acc, const PPWork& w, float alpha) {
     const PPLane el = pp_lane<TL>(lp.g, w.m0, w.n0);
 #pragma unroll
     for (int h = 0; h < TL::UA; ++h) {
         RowTerms r[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r[i] = row_terms(lp, el.row + h * TL::A_ROWS + 16 * i);
+        for (int i = 0; i < 4; ++i) r[i] = row_terms(lp, el.row + h * TL::A_ROWS + 16 * i, alpha);
 #pragma unroll
         for (int i = 0; i < 4; ++i) grad_block(lp, el, acc[h][i], el.row + h * TL::A_ROWS + 16 * i, r[i]);
     }
 }
 
+// alpha = the largest |dloss| of a token that counts (1 where there is none or it is 0), by all N threads of a workgroup.
+template <int N>
+__device__ __forceinline__ float largest_dloss(const float* dloss, const int* labels, int64_t vocab, int64_t M, float* tmp) {
+    float m = 0.0f;
+#pragma unroll 4
+    for (int64_t i = threadIdx.x; i < M; i += N) m = fmaxf(m, labels[i] >= 0 && labels[i] < vocab ? fabsf(dloss[i]) : 0.0f);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
+    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = m;
+    __syncthreads();
+    m = tmp[0];
+    for (int w = 1; w < N / 64; ++w) m = fmaxf(m, tmp[w]);
+    return m > 0.0f && m < INFINITY ? m : 1.0f;
+}
+
 template <typename TL, bool GRAD>
 __global__ __launch_bounds__(512, 2) void lm_loss_kernel(LossParams lp) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    __shared__ float own;
+    if (GRAD && lp.own_alpha) {
+        const float alpha = largest_dloss<512>(lp.dloss, lp.labels, lp.vocab, lp.g.M, reinterpret_cast<float*>(smem));
+        if (threadIdx.x == 0) {
+            own = alpha;
+            if (blockIdx.x == 0) *lp.alpha = alpha;
+        }
+        __syncthreads();                                           // the rest of LDS is free
+    }
     const int whole = lp.run[0].count, bid = blockIdx.x;
     const PPRun& run = lp.run[bid < whole ? 0 : 1];               // whole tiles first, then the K shares of the others
     const PPWork w = bid < whole ? pp_work<TL>(lp.g, run, share_of_block(bid, whole)) : pp_work<TL>(lp.g, run, share_of_block(bid - whole, gridDim.x - whole));
     PPAcc<TL> acc;
     pp_products<TL, true, true, false>(lp.g, w, smem, acc);
     if (w.partial) pp_store_partial<TL, 0>(lp.g, acc, w.m0 + pp_wave() / TL::WN * 64, w.partial);
-    else if constexpr (GRAD) grad_epilogue<TL>(lp, acc, w);
+    else if constexpr (GRAD) grad_epilogue<TL>(lp, acc, w, lp.own_alpha ? own : *lp.alpha);
     else stats_epilogue<TL>(lp, acc, w, smem);
 }
 // The tiles whose K was cut: the shares' sums in share order, then the epilogue.  A workgroup per block of 16 rows of a wavefront.
@@ -198,7 +223,7 @@ __global__ __launch_bounds__(512) void lm_loss_sum_kernel(LossParams lp, int sha
             }
         }
     if constexpr (GRAD) {
-        grad_block(lp, el, x, row, row_terms(lp, row));
+        grad_block(lp, el, x, row, row_terms(lp, row, *lp.alpha));
     } else {
         stats_block<TL>(lp, el, x, row, label_of(lp, row), n0 + TL::BN > lp.g.N, m0, red);
         __syncthreads();
@@ -207,19 +232,10 @@ __global__ __launch_bounds__(512) void lm_loss_sum_kernel(LossParams lp, int sha
     }
 }
 
-// alpha = the largest |dloss| of a token that counts (1 where there is none or it is 0).
 __global__ __launch_bounds__(1024) void lm_alpha_kernel(const float* __restrict__ dloss, const int* __restrict__ labels, int64_t vocab, int64_t M, float* __restrict__ alpha) {
     __shared__ float tmp[16];
-    float m = 0.0f;
-#pragma unroll 4
-    for (int64_t i = threadIdx.x; i < M; i += 1024) m = fmaxf(m, labels[i] >= 0 && labels[i] < vocab ? fabsf(dloss[i]) : 0.0f);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o, 64));
-    if ((threadIdx.x & 63) == 0) tmp[threadIdx.x >> 6] = m;
-    __syncthreads();
-    if (threadIdx.x) return;
-    for (int w = 1; w < 16; ++w) m = fmaxf(m, tmp[w]);
-    alpha[0] = m > 0.0f && m < INFINITY ? m : 1.0f;
+    const float m = largest_dloss<1024>(dloss, labels, vocab, M, tmp);
+    if (threadIdx.x == 0) alpha[0] = m;
 }
 
 // (log-sum-exp, target logit) of every token from its tiles' (maximum, sum), in tile order by 16 lanes.
@@ -391,6 +407,10 @@ hipError_t launch_logits(const LossParams& lp, const LossPlan& pl, void* partial
            : pl.tile == 1 ? launch_tile<PPTile<4, 1>, GRAD>(lp, pl, q, s)
                           : launch_tile<PPTile<2, 2>, GRAD>(lp, pl, q, s);
 }
+// Whether the workgroups of dz work alpha out themselves, which costs each about a microsecond, or a kernel before them, which costs 1.5 to 2 and reads
+// the tokens with one workgroup: few tokens and at most two rounds of tiles (3 x 288 x 434 backward 18.5 -> 17.0 us, 55 x 3888 x 1423 36.1 -> 34.4, 500 x 11368 x 269
+// 49.3 -> 47.0; with 4.5 rounds of two pieces 523 -> 534).
+bool own_alpha(const LmLossArgs& a, int64_t piece) { return a.M <= 1024 && piece >= a.V && loss_plan(a.M, a.V, a.H).tiles <= 2 * compute_units(); }
 LossParams loss_params(const LmLossArgs& a, int64_t v0, int64_t n) {
     LossParams lp{};
     lp.g.A = (const bf16_t*)a.x;
@@ -503,7 +523,8 @@ hipError_t lm_loss_bwd(const LmLossArgs& a) {
     const LossWs w = layout(a.dtype, a.M, a.H, a.V, true);
     char* ws = (char*)a.ws;
     hipError_t e = hipSuccess;
-    if (a.dtype == BF16) {
+    const bool own = a.dtype == BF16 && own_alpha(a, w.piece);
+    if (a.dtype == BF16 && !own) {
         hipLaunchKernelGGL(lm_alpha_kernel, dim3(1), dim3(1024), 0, a.stream, a.dloss, a.labels, a.vocab, a.M, (float*)(ws + w.alpha));
         if ((e = hipGetLastError()) != hipSuccess) return e;
     }
@@ -517,7 +538,7 @@ hipError_t lm_loss_bwd(const LmLossArgs& a) {
             e = hipGetLastError();
         } else {
             LossParams lp = loss_params(a, v0, n);
-            lp.dz = (bf16_t*)ws; lp.ldz = (int)row_stride(BF16, n); lp.alpha = (const float*)(ws + w.alpha);
+            lp.dz = (bf16_t*)ws; lp.ldz = (int)row_stride(BF16, n); lp.alpha = (float*)(ws + w.alpha); lp.own_alpha = own;
             e = launch_logits<true>(lp, loss_plan(a.M, n, a.H), ws + w.gemm, a.stream);
         }
         if (e != hipSuccess) return e;
