@@ -23,6 +23,7 @@ struct PackParams {
     const T* d_o; T* dqkv; float* dsum;
     float* part[2];               // sums of chunks: forward or dQ, dK and dV
     int kv_items;                 // bf16 backward: items of list 1 at most
+    int many;                     // float: short strips above which a wavefront has a quarter to itself
     float scale;
 };
 // What a workgroup works on.

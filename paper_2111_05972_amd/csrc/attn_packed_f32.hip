@@ -46,41 +46,62 @@ __device__ __forceinline__ void xfetch_flat(const FParams& p, const FStrip& s, c
 }
 
 // Workgroup `u` of a launch: a quarter of a strip of list 0 (forward), of list 1 or 0 (backward).  Long strips by lists, their four quarters one after
-// another, longest first; then the short ones (first_short), all first quarters, all second ones and so on, as those of short sequences have no more
-// than one: workgroups without work among the others made these wait (52 sequences of 117 tokens together, 8 heads of 128: forward 66 us, so 21, backward
-// 193, so 59; all strips that way: 29 sequences of 9224 tokens, 8 heads of 32, forward 62 -> 74).  False: there is no such quarter.
-__device__ __forceinline__ bool take_quarter(const FParams& p, bool bwd, int u, FStrip& s, int& side, int& sub) {
+// another, longest first; then the short ones (first_short).  Where these are many, a workgroup has all of one, a wavefront to a quarter (ALONE);
+// otherwise all first quarters, all second ones and so on, as those of short sequences have no more than one.  Workgroups that find none of their
+// own come last: among the others they made these wait.  52 sequences of 117 tokens together, 8 heads of 128, forward and backward: 66 and 193 us with four
+// workgroups to a strip one after another, so 21 and 61; all strips as the short ones: 29 sequences of 9224 tokens, 8 heads of 32, forward 62 -> 74.
+// Returns the list, -1: there is no such quarter.
+constexpr int ALONE = -1;
+template <bool MANY> __device__ __forceinline__ int take_quarter(const FParams& p, bool bwd, int u, FStrip& s, int& sub) {
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
-    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return false;
+    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return -1;
     const int first[2] = {h->first_short[0] * p.nkv, bwd ? h->first_short[1] * p.nkv : 0};
     const int after[2] = {h->items[0] * p.nkv - first[0], bwd ? h->items[1] * p.nkv - first[1] : 0};        // short ones
-    for (side = 1; side >= 0; --side) {
+    for (int side = 1; side >= 0; --side) {
         if (u < QUARTERS * first[side]) {
             sub = u % QUARTERS;
             strip_at(p, side, u / QUARTERS, s);
-            return true;
+            return side;
         }
         u -= QUARTERS * first[side];
     }
     const int all = after[0] + after[1];
-    if (u >= QUARTERS * all) return false;
-    sub = u / all;
-    u -= sub * all;
-    side = u < after[1];
+    const bool alone = MANY && all > p.many;
+    if (u >= (alone ? 1 : QUARTERS) * all) return -1;
+    sub = alone ? ALONE : u / all;
+    u %= all;
+    const int side = u < after[1];
     strip_at(p, side, side ? first[1] + u : first[0] + u - after[1], s);
-    return true;
+    return side;
+}
+// The result of a wavefront that had all tiles: every accumulator times f to put(d block, i, four rows' values); returns as xcombine.
+template <int DH, typename Put>
+__device__ __forceinline__ float xalone(const f32x16 (&acc)[DH / 32], float f, Put put) {
+    float z = 0.0f;
+#pragma unroll
+    for (int d = 0; d < DH / 32; ++d)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            float r[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { r[j] = acc[d][4 * i + j] * f; z = fmaf(r[j], 0.0f, z); }
+            put(d, i, r);
+        }
+    return z;
 }
 
-template <int DH>
+template <int DH, bool MANY>
 __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TB = xtile_bytes<DH>(), NL = xloads<DH>();
     FStrip s;
-    int side, sub;
-    if (!take_quarter(p, false, blockIdx.x, s, side, sub)) return;
-    const int r0 = s.it.first + sub * XT, len = s.it.len;
-    if (r0 >= s.rows) return;
+    int sub;
+    if (take_quarter<MANY>(p, false, blockIdx.x, s, sub) < 0) return;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool alone = MANY && sub == ALONE;                      // this wavefront has its quarter to itself, and meets no barrier
+    if (alone) sub = wave;
+    const int r0 = s.it.first + sub * XT, len = s.it.len, mine = alone ? 0 : wave, step = alone ? 1 : 4;
+    if (r0 >= s.rows) return;
     const int r = r0 + (lane & 31);
     const bool valid = r < s.rows;
     const Row me = row_of(p, valid ? r : s.rows - 1);
@@ -99,12 +120,12 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
     unsigned off[NL];
     xoffsets<DH>(off, s.ld, p.dh, lane);
     auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? t * XT : len, len, p.dh), lds, off, 0, s.ld); };
-    if (t0 + wave < nt) { fetch(s.k, lk, t0 + wave); fetch(s.v, lv, t0 + wave); }
-    for (int t = t0 + wave; t < nt; t += 4) {
+    if (t0 + mine < nt) { fetch(s.k, lk, t0 + mine); fetch(s.v, lv, t0 + mine); }
+    for (int t = t0 + mine; t < nt; t += step) {
         xwait<NL>();                                              // K of this tile (V is younger)
         f32x16 x = xscores<DH>(kt_, qr, lane);
         xreads_done();
-        fetch(s.k, lk, t + 4);                                    // past the last tile: zeros, so that the count of loads in flight stays
+        fetch(s.k, lk, t + step);                                    // past the last tile: zeros, so that the count of loads in flight stays
         const int k0 = t * XT;
         const bool edge = k0 + XT > len || (p.causal && k0 + XT - 1 > q_lo);
 #pragma unroll
@@ -132,37 +153,44 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
         xwait<NL>();                                              // V of this tile (the next K is younger)
         xaccumulate<DH>(acc, kt_ + TB, x, lane);
         xreads_done();
-        fetch(s.v, lv, t + 4);
+        fetch(s.v, lv, t + step);
     }
     xwait<0>();
     l += xother(l);
-    float* st = reinterpret_cast<float*>(smem + 8 * TB);          // [wavefront][m, l][row]
-    if (half == 0) { st[wave * 64 + lane] = m; st[wave * 64 + 32 + lane] = l; }
-    __syncthreads();
-    float mt = -INFINITY, f[4], lt = 0.0f;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) mt = fmaxf(mt, st[w * 64 + (lane & 31)]);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        f[w] = expf(st[w * 64 + (lane & 31)] - (mt == -INFINITY ? 0.0f : mt));
-        lt = fmaf(st[w * 64 + 32 + (lane & 31)], f[w], lt);
-    }
     const bool whole = s.it.slot < 0;
     float* part = whole ? nullptr : p.part[0] + ((int64_t)s.it.slot * p.nkv + s.hk) * (PACK_BLK * (DH + 2));
     const int rl = sub * XT + (lane & 31);
-    if (whole) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) f[w] /= lt;
-    }
     const int64_t head = (int64_t)s.hk * p.G;
     float* op = whole ? p.o + (s.it.t0 + me.q) * s.ldo + (head + me.g) * p.dh : part + rl * DH;
-    const float z = xcombine<DH>(smem, acc, f, wave, lane, [&](int d, int i, const float (&v)[4]) {
+    auto put = [&](int d, int i, const float (&v)[4]) {
         const int c = d * 32 + 8 * i + 4 * half;
         if (!whole || (valid && c < p.dh)) *reinterpret_cast<float4*>(op + c) = make_float4(v[0], v[1], v[2], v[3]);
-    });
-    if (wave == 0 && half == 0) {
-        if (!whole) { part[PACK_BLK * DH + rl] = mt; part[PACK_BLK * DH + PACK_BLK + rl] = lt; }
-        else if (valid) p.lse[s.row0 + (int64_t)me.q * p.nq + me.g] = mt + logf(lt);
+    };
+    float z;
+    if (alone) {
+        z = xalone<DH>(acc, 1.0f / l, put);
+        if (half == 0 && valid) p.lse[s.row0 + (int64_t)me.q * p.nq + me.g] = m + logf(l);
+    } else {
+        float* st = reinterpret_cast<float*>(smem + 8 * TB);      // [wavefront][m, l][row]
+        if (half == 0) { st[wave * 64 + lane] = m; st[wave * 64 + 32 + lane] = l; }
+        __syncthreads();
+        float mt = -INFINITY, f[4], lt = 0.0f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) mt = fmaxf(mt, st[w * 64 + (lane & 31)]);
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            f[w] = expf(st[w * 64 + (lane & 31)] - (mt == -INFINITY ? 0.0f : mt));
+            lt = fmaf(st[w * 64 + 32 + (lane & 31)], f[w], lt);
+        }
+        if (whole) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) f[w] /= lt;
+        }
+        z = xcombine<DH>(smem, acc, f, wave, lane, put);
+        if (wave == 0 && half == 0) {
+            if (!whole) { part[PACK_BLK * DH + rl] = mt; part[PACK_BLK * DH + PACK_BLK + rl] = lt; }
+            else if (valid) p.lse[s.row0 + (int64_t)me.q * p.nq + me.g] = mt + logf(lt);
+        }
     }
     if (!p.causal || !__any(z != 0.0f)) return;
     rows_stored();
@@ -174,8 +202,8 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
         float* oi = whole ? p.o + (s.it.t0 + w.q) * s.ldo + (head + w.g) * p.dh : part + (i - s.it.first) * DH;
         float mr, lr;
         attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, s.it.tile0 * PACK_TILE, min(w.q + 1, s.it.tile1 * PACK_TILE), p.scale, whole, lane, mr, lr,
-                                     [&](int d, float v) { if (xmine(d, wave)) oi[d] = v; });
-        if (lane == 0 && wave == 0) {
+                                     [&](int d, float v) { if (alone || xmine(d, wave)) oi[d] = v; });
+        if (lane == 0 && (alone || wave == 0)) {
             if (whole) p.lse[s.row0 + (int64_t)w.q * p.nq + w.g] = mr + logf(lr);
             else { part[PACK_BLK * DH + i - s.it.first] = mr; part[PACK_BLK * DH + PACK_BLK + i - s.it.first] = lr; }
         }
@@ -183,12 +211,14 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
     }
 }
 
-template <int DH>
+template <int DH, bool MANY>
 __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStrip& s, int sub) {
     constexpr int TB = xtile_bytes<DH>(), NL = xloads<DH>();
-    const int r0 = s.it.first + sub * XT, len = s.it.len;
-    if (r0 >= s.rows) return;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool alone = MANY && sub == ALONE;
+    if (alone) sub = wave;
+    const int r0 = s.it.first + sub * XT, len = s.it.len, mine = alone ? 0 : wave, step = alone ? 1 : 4;
+    if (r0 >= s.rows) return;
     const int r = r0 + (lane & 31);
     const bool valid = r < s.rows;
     const Row me = row_of(p, valid ? r : s.rows - 1);
@@ -211,12 +241,12 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
     unsigned off[NL];
     xoffsets<DH>(off, s.ld, p.dh, lane);
     auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? t * XT : len, len, p.dh), lds, off, 0, s.ld); };
-    if (t0 + wave < nt) { fetch(s.v, lv, t0 + wave); fetch(s.k, lk, t0 + wave); }   // V is read first
-    for (int t = t0 + wave; t < nt; t += 4) {
+    if (t0 + mine < nt) { fetch(s.v, lv, t0 + mine); fetch(s.k, lk, t0 + mine); }   // V is read first
+    for (int t = t0 + mine; t < nt; t += step) {
         xwait<NL>();
         f32x16 dp = xscores<DH>(kt_ + TB, gr, lane);              // dP^T = V dO^T
         xreads_done();
-        fetch(s.v, lv, t + 4);
+        fetch(s.v, lv, t + step);
         xwait<NL>();
         const f32x16 x = xscores<DH>(kt_, qr, lane);
         const int k0 = t * XT;
@@ -233,17 +263,18 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
         }
         xaccumulate<DH>(acc, kt_, dp, lane);                      // dQ^T += K^T dS
         xreads_done();
-        fetch(s.k, lk, t + 4);
+        fetch(s.k, lk, t + step);
     }
     xwait<0>();
     const bool whole = s.it.slot < 0;
     const float f1 = whole ? p.scale : 1.0f, f[4] = {f1, f1, f1, f1};
     float* part = whole ? nullptr : p.part[0] + ((int64_t)s.it.slot * p.nkv + s.hk) * (PACK_BLK * DH);
     float* dqp = whole ? p.dqkv + (s.it.t0 + me.q) * s.ld + (head + me.g) * p.dh : part + (sub * XT + (lane & 31)) * DH;
-    const float z = xcombine<DH>(smem, acc, f, wave, lane, [&](int d, int i, const float (&v)[4]) {
+    auto put = [&](int d, int i, const float (&v)[4]) {
         const int c = d * 32 + 8 * i + 4 * half;
         if (!whole || (valid && c < p.dh)) *reinterpret_cast<float4*>(dqp + c) = make_float4(v[0], v[1], v[2], v[3]);
-    });
+    };
+    const float z = alone ? xalone<DH>(acc, f1, put) : xcombine<DH>(smem, acc, f, wave, lane, put);
     if (!p.causal || !__any(z != 0.0f)) return;
     rows_stored();
     float* q_s = xrows<DH>(smem, wave);
@@ -255,17 +286,19 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
         float* dqi = whole ? p.dqkv + (s.it.t0 + w.q) * s.ld + (head + w.g) * p.dh : part + (i - s.it.first) * DH;
         const int64_t a = s.row0 + (int64_t)w.q * p.nq + w.g;
         attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, s.it.tile0 * PACK_TILE, min(w.q + 1, s.it.tile1 * PACK_TILE), p.scale, p.lse[a], p.dsum[a],
-                                    lane, [&](int d, float v) { if (xmine(d, wave)) dqi[d] = v * f1; });
+                                    lane, [&](int d, float v) { if (alone || xmine(d, wave)) dqi[d] = v * f1; });
         row_loaded();
     }
 }
 
-template <int DH>
+template <int DH, bool MANY>
 __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStrip& s, int sub) {
     constexpr int TB = xtile_bytes<DH>();
-    const int k0 = s.it.first + sub * XT, len = s.it.len;
-    if (k0 >= len) return;
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const bool alone = MANY && sub == ALONE;
+    if (alone) sub = wave;
+    const int k0 = s.it.first + sub * XT, len = s.it.len, mine = alone ? 0 : wave, step = alone ? 1 : 4;
+    if (k0 >= len) return;
     const int k = k0 + (lane & 31);
     const bool valid = k < len;
     const int64_t head = (int64_t)s.hk * p.G;
@@ -290,14 +323,14 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
     auto fetch_q = [&](int t) { xfetch_flat<DH>(p, s, s.q, s.ld, t < nt ? t * XT : s.rows, lq, lane); };
     auto fetch_g = [&](int t) { xfetch_flat<DH>(p, s, dobase, s.ldo, t < nt ? t * XT : s.rows, lg, lane); };
     float tn = 0.0f;
-    if (t0 + wave < nt) {
-        tn = term(t0 + wave);
-        fetch_q(t0 + wave);
-        fetch_g(t0 + wave);
+    if (t0 + mine < nt) {
+        tn = term(t0 + mine);
+        fetch_q(t0 + mine);
+        fetch_g(t0 + mine);
     }
     const int from = p.causal ? k * p.G : 0;                      // the first row that sees this lane's key
-    for (int t = t0 + wave; t < nt; t += 4) {
-        const int nx = t + 4;
+    for (int t = t0 + mine; t < nt; t += step) {
+        const int nx = t + step;
         terms[lane] = tn;
         xwait<0>();
         if (nx < nt) tn = term(nx);
@@ -339,8 +372,14 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
             if (!whole || (valid && c < p.dh)) *reinterpret_cast<float4*>(to + c) = make_float4(v[0], v[1], v[2], v[3]);
         };
     };
-    float z = xcombine<DH>(smem, dk, fk, wave, lane, put(kp));
-    z += xcombine<DH>(smem, dv, fv, wave, lane, put(vp));
+    float z;
+    if (alone) {
+        z = xalone<DH>(dk, f1, put(kp));
+        z += xalone<DH>(dv, 1.0f, put(vp));
+    } else {
+        z = xcombine<DH>(smem, dk, fk, wave, lane, put(kp));
+        z += xcombine<DH>(smem, dv, fv, wave, lane, put(vp));
+    }
     if (!p.causal || !__any(z != 0.0f)) return;
     rows_stored();
     constexpr int NA = (DH + 63) / 64;
@@ -372,7 +411,7 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
 #pragma unroll
         for (int n = 0; n < NA; ++n) {
             const int d = lane + 64 * n;
-            if (d >= p.dh || !xmine(d, wave)) continue;
+            if (d >= p.dh || !(alone || xmine(d, wave))) continue;
             if (whole) { p.dqkv[row + d] = dks[n] * p.scale; p.dqkv[row + (int64_t)p.nkv * p.dh + d] = dvs[n]; }
             else { part[(j - s.it.first) * DH + d] = dks[n]; part[PACK_BLK * DH + (j - s.it.first) * DH + d] = dvs[n]; }
         }
@@ -386,30 +425,36 @@ __global__ __launch_bounds__(256) void attn_packed_f32_dsum_kernel(FParams p) {
 }
 
 // Two workgroups share a compute unit up to head size 64 (see attn_f32.hip); wider heads need more than 256 registers.
-template <int DH>
+template <int DH, bool MANY>
 __global__ __launch_bounds__(256, DH <= 64 ? 2 : 1) void attn_packed_f32_bwd_kernel(FParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     FStrip s;
-    int side, sub;
-    if (!take_quarter(p, true, blockIdx.x, s, side, sub)) return;
-    if (side) f32_dkv<DH>(smem, p, s, sub);
-    else f32_dq<DH>(smem, p, s, sub);
+    int sub;
+    const int side = take_quarter<MANY>(p, true, blockIdx.x, s, sub);
+    if (side < 0) return;
+    if (side) f32_dkv<DH, MANY>(smem, p, s, sub);
+    else f32_dq<DH, MANY>(smem, p, s, sub);
 }
 
-template <int DH>
-hipError_t run(const PackAttnArgs& a, bool bwd) {
+// Short strips above which a wavefront has a quarter to itself: three quarters of the workgroups that run at once.  48 sequences of 918 tokens together,
+// 32 / 8 heads of 96, forward and backward 55 and 117 us, so 33 and 98; 60 of 600, 8 heads of 64, 14.7 and 32.4, so 11.2 and 28.5; but 30 of 1489, 2 heads of 64,
+// 25 us backward, so 51: each wavefront then has up to six tiles in a row.
+int many_strips(int DH) { return compute_units() * (DH <= 32 ? 4 : DH <= 64 ? 2 : 1) * 3 / 4; }
+template <int DH, bool MANY>
+hipError_t launch(const PackAttnArgs& a, bool bwd) {
     constexpr int lds = xlds_bytes<DH>();
-    static const hipError_t attr_f = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_fwd_kernel<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    static const hipError_t attr_b = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_bwd_kernel<DH>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr_f = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_fwd_kernel<DH, MANY>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr_b = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_bwd_kernel<DH, MANY>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr_f != hipSuccess || attr_b != hipSuccess) return attr_f != hipSuccess ? attr_f : attr_b;
     const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
     const PackLayout L = pack_layout(a.sequences, a.M, a.nq, a.nkv, shares);
     FParams p = make_params<float>(a, L);
     p.part[0] = (float*)a.ws;
+    p.many = many_strips(DH);
     const dim3 join(join_wgs(L, a.nkv));
     hipError_t e;
     if (!bwd) {
-        hipLaunchKernelGGL(attn_packed_f32_fwd_kernel<DH>, dim3((unsigned)(L.cap[0] * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
+        hipLaunchKernelGGL((attn_packed_f32_fwd_kernel<DH, MANY>), dim3((unsigned)(L.cap[0] * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
         if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
         hipLaunchKernelGGL((attn_packed_fwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
         return hipGetLastError();
@@ -417,11 +462,14 @@ hipError_t run(const PackAttnArgs& a, bool bwd) {
     p.part[1] = (float*)((char*)a.ws + ws_of(a, true).part[0]);
     hipLaunchKernelGGL(attn_packed_f32_dsum_kernel, dim3((unsigned)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units())), dim3(256), 0, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(attn_packed_f32_bwd_kernel<DH>, dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
+    hipLaunchKernelGGL((attn_packed_f32_bwd_kernel<DH, MANY>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
+// MANY: the kernels that can give a wavefront a quarter of its own, 3 % slower in backward where they do not, only where there are sequences enough for it.
+template <int DH>
+hipError_t run(const PackAttnArgs& a, bool bwd) { return a.sequences * a.nkv > many_strips(DH) ? launch<DH, true>(a, bwd) : launch<DH, false>(a, bwd); }
 }  // namespace
 
 hipError_t attn_packed_f32(const PackAttnArgs& a, bool bwd) {

@@ -213,6 +213,32 @@ def test_a_long_batch():
         ref.check(x[-tail:], val[k], tol[k], k)
 
 
+# Many short sequences in float, which a wavefront has to itself, beside longer ones; and what a mask hides among them
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("dh,nq,nkv", [(64, 16, 8), (128, 4, 4), (32, 6, 2), (32, 12, 12), (96, 16, 4)])
+def test_many_short_sequences_in_float(dh, nq, nkv, causal):
+    _run(list(range(0, 60)) + [0, 1, 31, 32, 33, 64, 65, 150, 193] * 2, nq, nkv, dh, causal, torch.float32, behind=1)
+
+
+def test_hidden_values_among_many_short_sequences():
+    nq, nkv, dh, n, cut = 4, 4, 128, 70, 20
+    b = Batch([30] * n, nq, nkv, dh, True, torch.float32)
+    val, tol = ref.attention(b.qkv, b.offsets, nq, nkv, dh, True, b.d_o)
+    rows = b.qkv.view(n, 30, nq + 2 * nkv, dh)
+    rows[::2, cut:, nq:] = math.inf                                  # K and V of the later tokens of every other sequence
+    b.d_o.view(n, 30, nq, dh)[1::4, :cut] = math.nan                 # dO of the earlier ones of some of the others
+    b.make_plan()
+    b.run()
+    shape = lambda x: x.reshape(n, 30, -1)                           # noqa: E731
+    for k in ("o", "lse"):
+        ref.check(shape(b.outputs()[k])[::2, :cut], shape(val[k])[::2, :cut], shape(tol[k])[::2, :cut], k)
+        ref.check(shape(b.outputs()[k])[1::2], shape(val[k])[1::2], shape(tol[k])[1::2], k)
+    got, want, off = shape(b.dqkv), shape(val["dqkv"]), shape(tol["dqkv"])
+    ref.check(got[::2, :cut, :nq * dh], want[::2, :cut, :nq * dh], off[::2, :cut, :nq * dh], "dq")
+    ref.check(got[1::4, cut:], want[1::4, cut:], off[1::4, cut:], "dqkv")
+    ref.check(got[3::4], want[3::4], off[3::4], "dqkv")
+
+
 def test_offsets_that_decrease_stay_in_bounds():
     b = Batch([40, 30, 30], 2, 1, 64, True, torch.bfloat16)
     b.on_gpu = torch.tensor([-5, 60, 20, 1000], dtype=torch.int32, device="cuda")      # taken as 0, 60, 60, 100
