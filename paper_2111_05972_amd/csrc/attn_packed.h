@@ -10,7 +10,7 @@
 // A strip is a block of 128 rows (forward, dQ) or 128 keys (dK, dV) of a sequence with the 64-row tiles that it visits on the other
 // side.  Strips much longer than a compute unit's share of all tiles are cut into chunks, each an item of its own that leaves float
 // sums in a slot of the workspace, and joined in chunk order by another kernel.  Lists are ordered by length, longest first (what
-// starts last should be short); items of equal length come in any order, which no result depends on.
+// starts last should be short), those of up to three tiles about as the rows are; items of equal length come in any order, which no result depends on.
 #pragma once
 #include <hip/hip_runtime_api.h>
 

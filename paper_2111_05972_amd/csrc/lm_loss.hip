@@ -11,6 +11,7 @@
 // What is rounded is dz divided by alpha, the largest |dloss|, and the products are multiplied by it again in float.  The dz of a label is close to
 // -dloss; where dloss is one number for all (a mean over the tokens) its rounding would be one and the same factor on all of them, up to 2^-9, and no
 // rounding error: against 64 bits dx and dw were 2.4 times as far off as rounding their values alone, so 1.4 times.
+// (One token: its label's dz is nearly all of dx and dw, and one rounding of it, 2^-9 at most, is theirs: up to 1.8 times.)
 // 8 M H V flops in all, bound by the matrix cores (board power): 4096 x 12576 x 5120 forward 405 us (1.30 PFLOP/s), dz 439, dx and dw 774 (1.36 PFLOP/s).
 // For few tokens bound by reading w three times and writing dw: 37 x 50257 x 4096 forward 120 us (3.4 TB/s, 197 tiles on 256 units), dz 97, dx and dw 199
 // (4.1 TB/s).
