@@ -35,7 +35,7 @@ struct PackHeader {
     int sequences, tokens, nq, nkv, causal;
     int items[2];          // [0]: forward and dQ, [1]: dK, dV
     int joins[2];          // strips that were cut
-    int first_short[2];    // strips of one or two tiles are items from here on (longer ones may be among them)
+    int first_short[2];    // items of one or two tiles stand from here on (longer ones, and chunks of cut strips, may be among them)
     int pad[5];
 };
 // Word offsets of the plan's parts; a function of what the host knows, so host and device agree without a copy.

@@ -46,7 +46,8 @@ __device__ __forceinline__ void xfetch_flat(const FParams& p, const FStrip& s, c
 }
 
 // Workgroup `u` of a launch: a quarter of a strip of list 0 (forward), of list 1 or 0 (backward).  Long strips by lists, their four quarters one after
-// another, longest first; then the short ones (first_short).  Where these are many, a workgroup has all of one, a wavefront to a quarter (ALONE);
+// another, longest first; then the short ones (first_short), chunks of cut strips among them.  Where these are many, a workgroup has all of one, a
+// wavefront to a quarter (ALONE);
 // otherwise all first quarters, all second ones and so on, as those of short sequences have no more than one.  Workgroups that find none of their
 // own come last: among the others they made these wait.  52 sequences of 117 tokens together, 8 heads of 128, forward and backward: 66 and 193 us with four
 // workgroups to a strip one after another, so 21 and 61; all strips as the short ones: 29 sequences of 9224 tokens, 8 heads of 32, forward 62 -> 74.
@@ -167,9 +168,13 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
         if (!whole || (valid && c < p.dh)) *reinterpret_cast<float4*>(op + c) = make_float4(v[0], v[1], v[2], v[3]);
     };
     float z;
-    if (alone) {
-        z = xalone<DH>(acc, 1.0f / l, put);
-        if (half == 0 && valid) p.lse[s.row0 + (int64_t)me.q * p.nq + me.g] = m + logf(l);
+    auto stats = [&](float top, float sum) {
+        if (!whole) { part[PACK_BLK * DH + rl] = top; part[PACK_BLK * DH + PACK_BLK + rl] = sum; }
+        else if (valid) p.lse[s.row0 + (int64_t)me.q * p.nq + me.g] = top + logf(sum);
+    };
+    if (alone) {                                                  // a short strip, or as short a chunk of one that was cut
+        z = xalone<DH>(acc, whole ? 1.0f / l : 1.0f, put);
+        if (half == 0) stats(m, l);
     } else {
         float* st = reinterpret_cast<float*>(smem + 8 * TB);      // [wavefront][m, l][row]
         if (half == 0) { st[wave * 64 + lane] = m; st[wave * 64 + 32 + lane] = l; }
@@ -187,10 +192,7 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
             for (int w = 0; w < 4; ++w) f[w] /= lt;
         }
         z = xcombine<DH>(smem, acc, f, wave, lane, put);
-        if (wave == 0 && half == 0) {
-            if (!whole) { part[PACK_BLK * DH + rl] = mt; part[PACK_BLK * DH + PACK_BLK + rl] = lt; }
-            else if (valid) p.lse[s.row0 + (int64_t)me.q * p.nq + me.g] = mt + logf(lt);
-        }
+        if (wave == 0 && half == 0) stats(mt, lt);
     }
     if (!p.causal || !__any(z != 0.0f)) return;
     rows_stored();
