@@ -114,7 +114,7 @@ __global__ __launch_bounds__(32 * JOIN_ROWS) void attn_packed_fwd_join_kernel(Pa
             const float* pc = p0 + c * next;
             const float f = pack_exp<T>(pc[PACK_BLK * DH + rl] - mu), l = pc[PACK_BLK * DH + PACK_BLK + rl];
             const float4 x = *reinterpret_cast<const float4*>(pc + rl * DH + col);
-            if (f == 0.0f) continue;                              // a chunk of masked keys: what it holds does not count
+            if (l == 0.0f) continue;                              // a chunk of masked keys: what it holds does not count (of NaN keys: l is NaN)
             total = fmaf(l, f, total);
             v[0] = fmaf(x.x, f, v[0]); v[1] = fmaf(x.y, f, v[1]); v[2] = fmaf(x.z, f, v[2]); v[3] = fmaf(x.w, f, v[3]);
         }
