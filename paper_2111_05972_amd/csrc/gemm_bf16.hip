@@ -2143,12 +2143,13 @@ size_t gemm_bf16_group_workspace_bytes(const GemmArgs* g, int n) {
     return need;
 }
 
-template <typename TL, typename Params>
-static hipError_t launch_group(void (*kernel)(Params), int threads, const Params& gp, hipStream_t s) {
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel),
+// A static of each kernel's own says that its LDS size is set.
+template <typename TL, auto KERNEL, typename Params>
+static hipError_t launch_group(int threads, const Params& gp, hipStream_t s) {
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(KERNEL),
                                                        hipFuncAttributeMaxDynamicSharedMemorySize, TL::LDS_BYTES);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL(kernel, dim3((unsigned)gp.first[gp.n]), dim3(threads), TL::LDS_BYTES, s, gp);
+    hipLaunchKernelGGL(KERNEL, dim3((unsigned)gp.first[gp.n]), dim3(threads), TL::LDS_BYTES, s, gp);
     return hipGetLastError();
 }
 
@@ -2182,7 +2183,7 @@ static hipError_t launch_pp_jobs(const GroupPlan& pl, const GemmArgs* g, int n, 
         sp.first[sp.n + 1] = sp.first[sp.n] + job.count * 4 * TL::UA;
         ++sp.n;
     }
-    const hipError_t e = launch_group<TL>(&gemm_bf16_group_pp_kernel<TL, ACC>, 512, gp, stream);
+    const hipError_t e = launch_group<TL, &gemm_bf16_group_pp_kernel<TL, ACC>>(512, gp, stream);
     if (e != hipSuccess || sp.n == 0) return e;
     hipLaunchKernelGGL((gemm_group_pp_sum_kernel<TL, ACC>), dim3((unsigned)sp.first[sp.n]), dim3(512), 0, stream, sp);
     return hipGetLastError();
@@ -2234,9 +2235,9 @@ hipError_t gemm_bf16_group(const GemmArgs* g, int n, void* ws, size_t ws_bytes, 
         gp.layout[q] = a.trans_a ? 2 : a.trans_b ? 1 : 0;
         gp.first[q + 1] = gp.first[q] + p.tiles_m * p.tiles_n * shares;
     }
-    hipError_t e = bm == 192   ? launch_group<Tile<3, 3, 3>>(&gemm_bf16_group_kernel<Tile<3, 3, 3>>, 256, gp, stream)
-                   : bm == 128 ? launch_group<Tile<2, 2, 4>>(&gemm_bf16_group_kernel<Tile<2, 2, 4>>, 256, gp, stream)
-                               : launch_group<Tile<1, 1, 6>>(&gemm_bf16_group_kernel<Tile<1, 1, 6>>, 256, gp, stream);
+    hipError_t e = bm == 192   ? launch_group<Tile<3, 3, 3>, &gemm_bf16_group_kernel<Tile<3, 3, 3>>>(256, gp, stream)
+                   : bm == 128 ? launch_group<Tile<2, 2, 4>, &gemm_bf16_group_kernel<Tile<2, 2, 4>>>(256, gp, stream)
+                               : launch_group<Tile<1, 1, 6>, &gemm_bf16_group_kernel<Tile<1, 1, 6>>>(256, gp, stream);
     if (e != hipSuccess || sp.n == 0) return e;
     hipLaunchKernelGGL(gemm_group_sum_kernel, dim3((unsigned)sp.first[sp.n]), dim3(256), 0, stream, sp);
     return hipGetLastError();
