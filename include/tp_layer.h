@@ -306,7 +306,8 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal,
  *   TPL_ROPE_LINEAR  every frequency divided by stretch
  *   TPL_ROPE_BASE    base * stretch^(rot / (rot - 2)), which leaves pair 0 as it is and divides the last one
  *   TPL_ROPE_PARTS   pairs that turn 32 times or more over `context` positions as they are, once or less divided by stretch, a linear
- *                    ramp between, and factor = 0.1 ln(stretch) + 1 (Peng et al. 2023, arXiv 2309.00071); otherwise factor = 1. */
+ *                    ramp between, and factor = 0.1 ln(stretch) + 1 (Peng et al. 2023, arXiv 2309.00071); otherwise factor = 1.
+ * TPL_EINVAL also where a stretched base or a frequency would leave the range of double. */
 enum { TPL_ROPE_HALF = 0, TPL_ROPE_ADJACENT = 1 };
 enum { TPL_ROPE_PLAIN = 0, TPL_ROPE_LINEAR = 1, TPL_ROPE_BASE = 2, TPL_ROPE_PARTS = 3 };
 int tp_layer_rope_frequencies(int rot, double base, int scaling, double stretch, double context, double* freq, float* factor);

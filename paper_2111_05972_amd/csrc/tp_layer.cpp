@@ -893,6 +893,7 @@ int tp_layer_rope_frequencies(int rot, double base, int scaling, double stretch,
     if (scaling == TPL_ROPE_PARTS && (!(context > 0.0) || !std::isfinite(context))) return TPL_EINVAL;
     const double circle = 6.28318530717958647692;
     if (scaling == TPL_ROPE_BASE && rot > 2) base *= std::pow(stretch, (double)rot / (rot - 2));
+    if (!(base > 0.0) || !std::isfinite(base)) return TPL_EINVAL;
     for (int i = 0; i < rot / 2; ++i) {
         double f = std::pow(base, -2.0 * i / rot);
         if (scaling == TPL_ROPE_LINEAR) f /= stretch;
@@ -900,6 +901,7 @@ int tp_layer_rope_frequencies(int rot, double base, int scaling, double stretch,
             const double turns = context * f / circle, keep = std::min(1.0, std::max(0.0, (turns - 1.0) / (32.0 - 1.0)));
             f = keep * f + (1.0 - keep) * f / stretch;
         }
+        if (!std::isfinite(f)) return TPL_EINVAL;
         freq[i] = f;
     }
     *factor = scaling == TPL_ROPE_PARTS && stretch > 1.0 ? (float)(0.1 * std::log(stretch) + 1.0) : 1.0f;
