@@ -300,8 +300,9 @@ int tp_layer_attn_bwd(int dtype, int B, int S, int nl, int dh, int causal,
  * backward: the transpose of that, (x, y) -> factor * (x cos a + y sin a, y cos a - x sin a).  The other columns and v are copied.
  * freq: double [rot / 2] in device memory, radians per position.  positions: int32 [M] (16-byte aligned; the front of a pack plan is such
  * an array), or NULL: row m has position m % seq (seq > 0; not looked at where there are positions).  Any int32 is a position; the angle is
- * worked out in 64 bits.  qkv and out are [M, (nq + 2 nkv) dh], M < 2^24, whole 16-byte rows; out may be qkv itself (then only what is turned is
- * touched), but may not overlap it otherwise (TPL_EINVAL).
+ * worked out in 64 bits.  qkv and out are [M, (nq + 2 nkv) dh], M < 2^24, whole 16-byte rows (TPL_EUNSUPPORTED: others, over 65536 heads of a
+ * kind, dh over 8192, (nq + 2 nkv) dh^2 from 2^31 on); out may be qkv itself (then only what is turned is touched), but may not overlap it
+ * otherwise (TPL_EINVAL).
  * tp_layer_rope_frequencies fills freq and factor in HOST memory: base^(-2 i / rot), for a context stretched `stretch` times
  *   TPL_ROPE_LINEAR  every frequency divided by stretch
  *   TPL_ROPE_BASE    base * stretch^(rot / (rot - 2)), which leaves pair 0 as it is and divides the last one
@@ -323,8 +324,9 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
  * Rows that belong to no sequence (behind the last one) are neither read nor written: what the caller's products make of whole tensors
  * (dW of a projection) reads what they held, so o and dqkv are best zeroed once where a batch may end before M.  A masked value is as if it
  * were not there, infinities and NaN among them.  dh: a multiple of 8 up to 128; at most 128 query heads to a key head.
- * TPL_EUNSUPPORTED: over 2^24 rows, 2^20 sequences, 2^31 (row, head) pairs, or 2^22 strips (of 128 (row, head) pairs or keys of one sequence
- * and key head, those that may be cut counted twice).
+ * bf16: weights and dS are rounded to bf16 as operands of the products at every head size (tp_layer_attn_* keeps them float at head sizes other than 64 and 128).
+ * TPL_EUNSUPPORTED: over 2^24 rows, 2^20 sequences or 4096 query heads, from 2^31 (row, head) pairs on, from 2^30 of (M + 256) nq / nkv on, from 2^22 strips
+ * on (of 128 (row, head) pairs or keys of one sequence and key head, those that may be cut counted twice).
  *
  * The plan: tp_layer_pack_plan_bytes() of device memory that tp_layer_pack_plan fills on the stream from offsets (int32
  * [sequences + 1], device memory, offsets[0] = 0, not decreasing, the last at most M), once for a batch; every layer's calls with the same
@@ -352,7 +354,9 @@ int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, in
  *   3. tp_layer_lm_loss_bwd : dz = (exp(z - lse) - onehot(label)) * dloss[m], worked out again piece by piece;
  *      dx_partial [M, H] = dz w, which the ranks would all-reduce; dw [V, H] = dz^T x
  * (x of an ignored token is multiplied by zero in dw: it has to be finite).  stats, loss, lse, dloss: float, natural logarithms.
- * H whole 16-byte rows; V up to 2^24, M up to 2^20, M V up to 2^37; x below 2 GiB.  ws_bytes >= tp_layer_lm_loss_workspace_bytes(..., bwd). */
+ * H whole 16-byte rows up to 2^20; V up to 2^24, M up to 2^20, M V up to 2^37, first and vocab up to 2^30; x below 2 GiB (join: M up to 2^24, ranks up to
+ * 65536).  stats 8-byte aligned; labels, loss, lse, dloss 4.  bf16: dz / max |dloss| is rounded to bf16 as an operand of both products.
+ * ws_bytes >= tp_layer_lm_loss_workspace_bytes(..., bwd). */
 size_t tp_layer_lm_loss_workspace_bytes(int dtype, int64_t M, int64_t H, int64_t V, int bwd);
 int tp_layer_lm_loss_fwd(int dtype, int64_t M, int64_t H, int64_t V, int64_t first, const void* x, const void* w, const int32_t* labels,
                          float* stats, void* ws, size_t ws_bytes, void* hip_stream);

@@ -11,8 +11,9 @@
 // grows with the length, so the rows of a batch may be any number of bytes.  A tile of Q and dO holds flattened rows; their
 // addresses come from a division by G of a number below 64 + G, one multiplication.
 //
-// Precision.  Probabilities and dS are rounded to bf16 as matrix operands (each product's rounding is off by at most 2^-9 of it and
-// they have no common sign; sums, statistics and D are float).
+// Precision.  Probabilities and dS are rounded to bf16 as matrix operands, at every head size (attn_bf16.hip keeps them float at head sizes other than 64
+// and 128): each is off by at most 2^-8 of itself, and these roundings have no common sign.  Sums, statistics and D are float.
+// Against 64 bits o and dqkv are 1.4 times as far off as their rounding alone.
 //
 // Infinities and NaN in masked places.  Zero times infinity is NaN, so a masked row of V (K; Q, dO) in the tile that the diagonal
 // crosses would reach rows that do not see it.  A wavefront that ends with a value that is not finite computes its rows again, row by
@@ -265,7 +266,7 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
 }
 
 // ---- D ----------------------------------------------------------------------------------------------------------------
-// D = rowsum(dO * O) where a row has many keys.  O has been rounded, by up to 2^-9 of itself, and where keys are few O is as large as V, so that
+// D = rowsum(dO * O) where a row has many keys.  O has been rounded, by up to 2^-8 of itself, and where keys are few O is as large as V, so that
 // the difference dP - D loses half of its digits (error of dQ and dK against 64 bits with correctly rounded ones = 1: 2.3 for sequences of 2 tokens, 1.8 for 8,
 // 1.5 for 64, 1.43 for 512).  Rows of at most 64 keys, a tile, therefore get D = rowsum(P * dP), the same sum from unrounded terms: two of the three
 // products of dQ, for the strips that begin with such rows.  Workgroups [0, strips) walk those, the others the rows.  Bound by memory: 18 us for the

@@ -9,9 +9,10 @@
 // rounded to bf16 as an operand of the two products that follow, which go out as one group.  A piece of dz is at most 128 MiB, so
 // that both products find it in the infinity cache; where there are several, dx is added up in float.
 // What is rounded is dz divided by alpha, the largest |dloss|, and the products are multiplied by it again in float.  The dz of a label is close to
-// -dloss; where dloss is one number for all (a mean over the tokens) its rounding would be one and the same factor on all of them, up to 2^-9, and no
+// -dloss; where dloss is one number for all (a mean over the tokens) its rounding would be one and the same factor on all of them, up to 2^-8, and no
 // rounding error: against 64 bits dx and dw were 2.4 times as far off as rounding their values alone, so 1.4 times.
-// (One token: its label's dz is nearly all of dx and dw, and one rounding of it, 2^-9 at most, is theirs: up to 1.8 times.)
+// (Of few tokens the labels' dz are nearly all of dx and dw, and their roundings, 2^-8 at most, do not average out: up to 1.8 times as far off at one to eight
+// tokens.)
 // 8 M H V flops in all, bound by the matrix cores (board power): 4096 x 12576 x 5120 forward 405 us (1.30 PFLOP/s), dz 439, dx and dw 774 (1.36 PFLOP/s).
 // For few tokens bound by reading w three times and writing dw: 37 x 50257 x 4096 forward 120 us (3.4 TB/s, 197 tiles on 256 units), dz 97, dx and dw 199
 // (4.1 TB/s).

@@ -1,11 +1,14 @@
 // Rotary positions for gfx950: the first `rot` columns of every q and k head in rows of (q | k | v, head, dh) are turned, pair by
 // pair, by the angle position * frequency; backward turns back.  Bound by memory: every element is read and written once.  8192 tokens of
 // 12 + 2 x 12 heads of 128 in bf16, 151 MB: 24.5 us, 6.2 TB/s (some of it out of the infinity cache; a copy of 512 MiB reaches 5.4); 3001 tokens of
-// 32 + 2 x 8 heads of 80 in float, 92 MB: 16 us, 5.8 TB/s; 64 tokens 3.3 us, a launch.
+// 32 + 2 x 8 heads of 80 in float, 92 MB: 16 us, 5.8 TB/s; 64 tokens 3.3 us, a launch.  That is where the two halves of a rotation (neighbouring pairs: the
+// rotation) are whole 16-byte units; otherwise every element of the row moves alone: bf16, 8192 tokens, 32 + 2 x 8 heads of 104 turned whole 40.5 us (4.0 TB/s;
+// neighbouring pairs 25.8), 64 + 2 x 8 of 96 turned by 24 85 us (3.0; 38.7), 32 + 2 x 8 of 80 turned by 20 47 us (2.7).
 //
 // Angles are worked out here and not read from a table: one per (token, pair), shared by all heads through LDS.  position *
 // frequency is a product of 64 bits whose whole turns are taken off before it is rounded to 32 (at position 1e6 a 32-bit angle
-// would be off by 0.03), so there is no largest position and nothing to keep.
+// would be off by 0.03), so there is no largest position and nothing to keep.  What is left, half a circle at most, is an angle of 32 bits, off by 2^-24 of
+// itself: rows of float are 1.5 times as far from 64 bits as with sine and cosine rounded once.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
