@@ -345,6 +345,21 @@ int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, in
                              const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, float* d_scratch,
                              void* ws, size_t ws_bytes, void* hip_stream);
 
+/* The same with a sliding window and first tokens that stay visible ("sinks"): query i of a sequence sees its keys j <= i with i - j < window
+ * or j < sinks, so itself at least.  window from 1 on, sinks from 0 on (TPL_EINVAL: others); either may be longer than a sequence, and a window as long as
+ * the longest sequence is the causal mask.  Everything else, the limits, the rows that are left alone and the masked values that do not matter included, as above; lse is over the
+ * keys that a query sees.  The plan is of the window and the sinks too: a call with a plan of others writes nothing, nor does one of
+ * tp_layer_attn_packed_* with such a plan.  It begins with the positions as well, and may be captured. */
+size_t tp_layer_window_plan_bytes(int64_t sequences, int64_t M, int nq, int nkv);
+int tp_layer_window_plan(int64_t sequences, int64_t M, const int32_t* offsets, int nq, int nkv, int64_t window, int64_t sinks, void* plan,
+                         size_t plan_bytes, void* hip_stream);
+size_t tp_layer_attn_window_workspace_bytes(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks, int bwd);
+int tp_layer_attn_window_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks, const void* plan,
+                             size_t plan_bytes, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream);
+int tp_layer_attn_window_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks, const void* plan,
+                             size_t plan_bytes, const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, float* d_scratch,
+                             void* ws, size_t ws_bytes, void* hip_stream);
+
 /* Softmax cross entropy over a vocabulary split over the ranks, without keeping the logits z = x w^T.  x [M, H] is replicated, w [V, H]
  * (dtype, a row per token of the vocabulary) holds rows first .. first + V - 1 of the whole one; labels int32 [M], numbers in the whole
  * vocabulary; a label outside [0, vocab) is ignored (loss 0, no gradient).

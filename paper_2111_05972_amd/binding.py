@@ -108,6 +108,11 @@ def load_library():
         "tp_layer_attn_packed_workspace_bytes": (sz, [ci, i64, i64, ci, ci, ci, ci, ci]),
         "tp_layer_attn_packed_fwd": (ci, [ci, i64, i64, ci, ci, ci, ci, _vp, sz, _vp, _vp, _vp, _vp, sz, _vp]),
         "tp_layer_attn_packed_bwd": (ci, [ci, i64, i64, ci, ci, ci, ci, _vp, sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
+        "tp_layer_window_plan_bytes": (sz, [i64, i64, ci, ci]),
+        "tp_layer_window_plan": (ci, [i64, i64, _vp, ci, ci, i64, i64, _vp, sz, _vp]),
+        "tp_layer_attn_window_workspace_bytes": (sz, [ci, i64, i64, ci, ci, ci, i64, i64, ci]),
+        "tp_layer_attn_window_fwd": (ci, [ci, i64, i64, ci, ci, ci, i64, i64, _vp, sz, _vp, _vp, _vp, _vp, sz, _vp]),
+        "tp_layer_attn_window_bwd": (ci, [ci, i64, i64, ci, ci, ci, i64, i64, _vp, sz, _vp, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
         "tp_layer_lm_loss_workspace_bytes": (sz, [ci, i64, i64, i64, ci]),
         "tp_layer_lm_loss_fwd": (ci, [ci, i64, i64, i64, i64, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
         "tp_layer_lm_loss_join": (ci, [i64, i64, i64, _vp, _vp, _vp, _vp, _vp]),
@@ -447,6 +452,37 @@ def tp_layer_attn_packed_bwd(dtype, sequences, M, nq, nkv, dh, causal, plan, qkv
                                                  _ptr(d_o), _ptr(dqkv), _ptr(d_scratch), _ptr(ws),
                                                  (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
     return _checked(rc, "tp_layer_attn_packed_bwd", check)
+
+
+def tp_layer_window_plan_bytes(sequences, M, nq, nkv):
+    return load_library().tp_layer_window_plan_bytes(sequences, M, nq, nkv)
+
+
+def tp_layer_window_plan(sequences, M, offsets, nq, nkv, window, sinks, plan, plan_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_window_plan(sequences, M, _ptr(offsets), nq, nkv, window, sinks, _ptr(plan),
+                                             (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_window_plan", check)
+
+
+def tp_layer_attn_window_workspace_bytes(dtype, sequences, M, nq, nkv, dh, window, sinks, bwd):
+    return load_library().tp_layer_attn_window_workspace_bytes(dtype, sequences, M, nq, nkv, dh, window, sinks, int(bool(bwd)))
+
+
+def tp_layer_attn_window_fwd(dtype, sequences, M, nq, nkv, dh, window, sinks, plan, qkv, o, lse, ws, ws_bytes=None, plan_bytes=None, stream=None,
+                             check=True):
+    rc = load_library().tp_layer_attn_window_fwd(dtype, sequences, M, nq, nkv, dh, window, sinks, _ptr(plan),
+                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _ptr(qkv), _ptr(o), _ptr(lse),
+                                                 _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_attn_window_fwd", check)
+
+
+def tp_layer_attn_window_bwd(dtype, sequences, M, nq, nkv, dh, window, sinks, plan, qkv, o, lse, d_o, dqkv, d_scratch, ws, ws_bytes=None,
+                             plan_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_attn_window_bwd(dtype, sequences, M, nq, nkv, dh, window, sinks, _ptr(plan),
+                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _ptr(qkv), _ptr(o), _ptr(lse),
+                                                 _ptr(d_o), _ptr(dqkv), _ptr(d_scratch), _ptr(ws),
+                                                 (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_attn_window_bwd", check)
 
 
 def tp_layer_lm_loss_workspace_bytes(dtype, M, H, V, bwd):

@@ -3,13 +3,14 @@
 //
 // Flattened rows.  The G = nq / nkv query heads of a key head read the same keys, so to that key head they are one sequence of
 // len * G query rows: row r is head r % G of query r / G.  Its keys are 0 .. r / G under the causal mask, that is, key j is seen
-// by the rows r >= j G.  A block of 128 rows is then full where there are short sequences and many heads to a key head, crosses a
+// by the rows r >= j G (with a window: and r < (j + window) G, unless j is among the first keys that stay visible).  A block of 128 rows is then full where there are short sequences and many heads to a key head, crosses a
 // short piece of the diagonal, and dK, dV of a key head need no sum over heads besides the one over rows.
 //
 // Plan (device memory, 32-bit words): positions [M], keys that a token sees [M] (0: it is in no sequence), a header, offsets of the sequences, block counts, and lists of work items.
 // A strip is a block of 128 rows (forward, dQ) or 128 keys (dK, dV) of a sequence with the 64-row tiles that it visits on the other
 // side.  Strips much longer than a compute unit's share of all tiles are cut into chunks, each an item of its own that leaves float
-// sums in a slot of the workspace, and joined in chunk order by another kernel.  Lists are ordered by length, longest first (what
+// sums in a slot of the workspace, and joined in chunk order by another kernel.  With a window a strip of rows visits the tiles of the first keys
+// and those of its window; `skip` tiles between them are left out, and tile numbers of an item are counted without them.  Lists are ordered by length, longest first (what
 // starts last should be short), those of up to three tiles about as the rows are; items of equal length come in any order, which no result depends on.
 #pragma once
 #include <hip/hip_runtime_api.h>
@@ -21,6 +22,7 @@ namespace tpl {
 
 constexpr int PACK_BLK = 128, PACK_TILE = 64;
 constexpr int PACK_MAX_GROUP = 128;
+enum PackMask { PACK_ALL = 0, PACK_CAUSAL = 1, PACK_WINDOW = 2 };     // PACK_WINDOW: causal, the last `window` keys and the first `sinks`
 constexpr int PACK_MIN_CHUNK = 8;         // tiles, half of it where strips are few, see pack_shares
 
 struct PackItem {
@@ -29,14 +31,15 @@ struct PackItem {
     int tile0, tile1;      // tiles of the other side: [tile0, tile1)
     int slot;              // of this chunk's sums (of chunk 0's in the join lists), -1: the whole strip
     int chunks;            // of the strip
-    int pad;
+    int skip;              // tiles left out behind the first keys' tiles (forward, dQ with a window)
 };
 struct PackHeader {
-    int sequences, tokens, nq, nkv, causal;
+    int sequences, tokens, nq, nkv, mask;
     int items[2];          // [0]: forward and dQ, [1]: dK, dV
     int joins[2];          // strips that were cut
     int first_short[2];    // items of one or two tiles stand from here on (longer ones, and chunks of cut strips, may be among them)
-    int pad[5];
+    int window, sinks;     // 0 without a window
+    int pad[3];
 };
 // Word offsets of the plan's parts; a function of what the host knows, so host and device agree without a copy.
 struct PackLayout {
@@ -77,9 +80,27 @@ inline PackShares pack_shares(int64_t M, int64_t nq, int64_t nkv, int units) {
 
 #ifdef __HIPCC__
 __device__ __forceinline__ const PackItem* pack_items(const int* plan, int64_t at) { return reinterpret_cast<const PackItem*>(plan + at); }
-// Whether the plan at hand was made for this call.
-__device__ __forceinline__ bool pack_matches(const PackHeader* h, int sequences, int tokens, int nq, int nkv, int causal) {
-    return h->sequences == sequences && h->tokens == tokens && h->nq == nq && h->nkv == nkv && h->causal == causal;
+// Tiles of a strip that begins with row (side 0) or key (side 1) `first` of a sequence of `len` tokens.  Rows are below 2^30, a window and the first
+// keys at most as many as the batch has tokens.
+struct PackTiles { int tile0, tile1, skip; };
+__device__ __forceinline__ PackTiles pack_tiles(int mask, int window, int sinks, unsigned G, int side, int len, int first) {
+    const unsigned rows = (unsigned)len * G;
+    PackTiles t{0, 0, 0};
+    if (side == 0) {
+        const unsigned last = min(rows, (unsigned)first + PACK_BLK) - 1;
+        t.tile1 = mask != PACK_ALL ? (int)(last / G) / PACK_TILE + 1 : (len + PACK_TILE - 1) / PACK_TILE;
+        if (mask == PACK_WINDOW) {
+            const int near = max(0, (int)((unsigned)first / G) - window + 1) / PACK_TILE, stay = (sinks + PACK_TILE - 1) / PACK_TILE;
+            t.skip = max(0, near - stay);
+            t.tile1 -= t.skip;
+        }
+    } else {
+        unsigned end = rows;
+        if (mask == PACK_WINDOW && first >= sinks) end = min(rows, ((unsigned)min(first + PACK_BLK, len) - 1 + window) * G);
+        t.tile0 = mask != PACK_ALL ? (int)((unsigned)first * G / PACK_TILE) : 0;
+        t.tile1 = (int)((end + PACK_TILE - 1) / PACK_TILE);
+    }
+    return t;
 }
 #endif
 
@@ -87,14 +108,14 @@ __device__ __forceinline__ bool pack_matches(const PackHeader* h, int sequences,
 struct PackAttnArgs {
     int dtype;
     int64_t sequences, M;
-    int nq, nkv, dh, causal;
+    int nq, nkv, dh, mask, window, sinks;
     const int* plan;
     const void* qkv; void* o; float* lse;                         // lse [M, nq]
     const void* d_o; void* dqkv; float* dsum;                     // dsum [M, nq]
     void* ws; size_t ws_bytes;
     hipStream_t stream;
 };
-hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int causal, int* plan, hipStream_t s);
+hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int mask, int window, int sinks, int* plan, hipStream_t s);
 size_t attn_packed_workspace_bytes(const PackAttnArgs& a, bool bwd);
 hipError_t attn_packed_bf16(const PackAttnArgs& a, bool bwd);
 hipError_t attn_packed_f32(const PackAttnArgs& a, bool bwd);

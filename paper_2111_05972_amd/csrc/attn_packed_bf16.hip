@@ -91,9 +91,10 @@ template <int DH> __device__ __forceinline__ void strip_frags(bf16x8 (&f)[DH / 1
 constexpr int WAVES4 = 256;
 template <int DH> constexpr int fwd_lds() { return 4 * tile_bytes<DH>(); }
 
-template <int DH, bool CAUSAL>
+template <int DH, int MASK>
 __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2;
     constexpr int NCH = NCHUNKS<DH, WAVES4>;
     BStrip s;
@@ -115,7 +116,8 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
     unsigned off[NCH];
     dma_offsets<DH, WAVES4>(off, s.ld, p.dh, t);
-    auto fetch_tile = [&](int kt, unsigned stage) {
+    auto fetch_tile = [&](int v, unsigned stage) {
+        const int kt = WIN ? tile_of(p, s, v) : v;
         tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), stage, off, 0, wave);
         tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
     };
@@ -138,8 +140,8 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
     auto step = [&](int kt, auto stg) __attribute__((always_inline)) {
         constexpr int SOFF = decltype(stg)::value * 2 * TB;
         if (kt + 1 < s.it.tile1) fetch_tile(kt + 1, lds0 + (1 - decltype(stg)::value) * 2 * TB);
-        const int kv0 = kt * PACK_TILE;
-        if (kv0 < kv_end) {                                       // wavefront-uniform
+        const int kv0 = (WIN ? tile_of(p, s, kt) : kt) * PACK_TILE;
+        if (kv0 < kv_end && (!WIN || kv0 + PACK_TILE > q_lo + 1 - p.window || kv0 < p.sinks)) {    // wavefront-uniform
             f32x16 x[2] = {zero16(), zero16()};
             bf16x8 fr[2 * NF];                                    // keys 0..31 and 32..63 in turn, a chain of products each
 #pragma unroll
@@ -170,6 +172,16 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
                 for (int g = 0; g < 2; ++g)
 #pragma unroll
                     for (int v = 0; v < 16; ++v) x[g][v] = 32 * g + (v >> 2) * 8 + (v & 3) <= seen ? x[g][v] : -INFINITY;
+            }
+            if (WIN && kv0 < q_hi + 1 - p.window && kv0 + PACK_TILE > p.sinks) {
+                const int from = me.q + 1 - p.window - kv0 - half * 4, stay = p.sinks - kv0 - half * 4;   // first key of the window, end of the first ones
+#pragma unroll
+                for (int g = 0; g < 2; ++g)
+#pragma unroll
+                    for (int v = 0; v < 16; ++v) {
+                        const int k = 32 * g + (v >> 2) * 8 + (v & 3);
+                        x[g][v] = k >= from || k < stay ? x[g][v] : -INFINITY;
+                    }
             }
             float mb = fmaxf(x[0][0], x[1][0]);
 #pragma unroll
@@ -255,8 +267,12 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
         bf16_t* op = p.o + (s.it.t0 + w.q) * s.ldo + (int64_t)(s.hk * p.G + w.g) * p.dh;
         const int il = i - s.it.first;
         float mr, lr;
-        attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, s.it.tile0 * PACK_TILE, min(w.q + 1, s.it.tile1 * PACK_TILE), p.scale, whole, lane, mr, lr,
-                                     [&](int d, float v) { if (whole) op[d] = (bf16_t)v; else part[il * DH + d] = v; });
+        auto store = [&](int d, float v) { if (whole) op[d] = (bf16_t)v; else part[il * DH + d] = v; };
+        const int beg = s.it.tile0 * PACK_TILE, end = s.it.tile1 * PACK_TILE;
+        if constexpr (WIN)
+            attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, beg, end, p.scale, whole, lane, mr, lr, store, WindowKeys<bf16_t>{p, s, w.q});
+        else
+            attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, beg, min(w.q + 1, end), p.scale, whole, lane, mr, lr, store);
         if (lane == 0) {
             if (whole) p.lse[s.row0 + (int64_t)w.q * p.nq + w.g] = mr + logf(lr);
             else { part[PACK_BLK * DH + il] = mr * LOG2E; part[PACK_BLK * DH + PACK_BLK + il] = lr; }
@@ -272,12 +288,13 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_fwd_kernel(Params p) {
 // products of dQ, for the strips that begin with such rows.  Workgroups [0, strips) walk those, the others the rows.  Bound by memory: 18 us for the
 // 67 MB of O and dO of 8192 tokens of 16 heads of 128 in 12 documents, 25 us where all of 128 sequences have 64 tokens.
 template <int DH> constexpr int dsum_lds() { return 2 * tile_bytes<DH>(); }
-template <int DH, bool CAUSAL>
+template <int DH, int MASK>
 __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, int strips) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
+    constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, HALF = 32 * DH * 2, NCH = NCHUNKS<DH, WAVES4>;
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
-    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return;
+    if (!pack_matches(h, p)) return;
     if ((int)blockIdx.x >= strips) {
         dsum_rows(p, (int64_t)(blockIdx.x - strips) * 16, (int64_t)(gridDim.x - strips) * 16, PACK_TILE);
         return;
@@ -286,12 +303,18 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, i
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
     const float c2 = LOG2E * p.scale;
-    const int all = (h->items[0] - h->first_short[0]) * p.nkv;
+    // no row sees more keys than a tile has: all strips, each found by its first chunk
+    const bool narrow = WIN && p.window + p.sinks <= PACK_TILE;
+    const int begin = narrow ? 0 : h->first_short[0], all = (h->items[0] - begin) * p.nkv;
     for (int i = blockIdx.x; i < all; i += strips) {
         BStrip s;
-        s.it = pack_items(p.plan, p.items[0])[h->first_short[0] + i / p.nkv];
-        if (CAUSAL ? s.it.tile1 > 2 || s.it.first >= PACK_TILE * p.G : s.it.len > PACK_TILE) continue;   // uniform; such a strip is not cut
+        s.it = pack_items(p.plan, p.items[0])[begin + i / p.nkv];
+        if (narrow ? s.it.tile0 > 0 : CAUSAL ? s.it.tile1 > 2 || s.it.first >= PACK_TILE * p.G : s.it.len > PACK_TILE) continue;   // uniform; but for the narrow ones such a strip is not cut
         set_strip(p, i % p.nkv, s);
+        int tiles = 1;
+        if constexpr (WIN) {
+            if (narrow) tiles = pack_tiles(PACK_WINDOW, p.window, p.sinks, (unsigned)p.G, 0, s.it.len, s.it.first).tile1;
+        }
         const int len = s.it.len, r = s.it.first + wave * 32 + (lane & 31);
         const bool valid = r < s.rows;
         const Row me = row_of(p, valid ? r : s.rows - 1);
@@ -300,8 +323,11 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, i
         const float l2 = p.lse[at] * LOG2E;
         unsigned off[NCH];
         dma_offsets<DH, WAVES4>(off, s.ld, p.dh, t);
-        tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, 0, len, p.dh), lds0, off, 0, wave);
-        tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, 0, len, p.dh), lds0 + TB, off, 0, wave);
+        auto fetch_tile = [&](int kt) {
+            tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), lds0, off, 0, wave);
+            tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), lds0 + TB, off, 0, wave);
+        };
+        fetch_tile(WIN ? tile_of(p, s, 0) : 0);
         bf16x8 qf[NF], dof[NF];
 #pragma unroll
         for (int ks = 0; ks < NF; ++ks) {
@@ -312,30 +338,40 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, i
         for (int ks = 0; ks < NF; ++ks) { settle(qf[ks]); settle(dof[ks]); }
         dma_wait();
         __syncthreads();
-        f32x16 x[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
-#pragma unroll
-        for (int ks = 0; ks < NF; ++ks) {
-            const unsigned ka = lds0 + frag_k_off<DH>(0, ks, lane);
-            x[0] = MFMA(lds_frag_k<0>(ka), qf[ks], x[0]);
-            x[1] = MFMA(lds_frag_k<HALF>(ka), qf[ks], x[1]);
-            dp[0] = MFMA(lds_frag_k<TB>(ka), dof[ks], dp[0]);
-            dp[1] = MFMA(lds_frag_k<TB + HALF>(ka), dof[ks], dp[1]);
-        }
-        const int seen = min(CAUSAL ? me.q : len, len - 1) - half * 4;
         float d = 0.0f;
+        for (int n = 0;;) {
+            f32x16 x[2] = {zero16(), zero16()}, dp[2] = {zero16(), zero16()};
 #pragma unroll
-        for (int g = 0; g < 2; ++g)
+            for (int ks = 0; ks < NF; ++ks) {
+                const unsigned ka = lds0 + frag_k_off<DH>(0, ks, lane);
+                x[0] = MFMA(lds_frag_k<0>(ka), qf[ks], x[0]);
+                x[1] = MFMA(lds_frag_k<HALF>(ka), qf[ks], x[1]);
+                dp[0] = MFMA(lds_frag_k<TB>(ka), dof[ks], dp[0]);
+                dp[1] = MFMA(lds_frag_k<TB + HALF>(ka), dof[ks], dp[1]);
+            }
+            const int kv0 = WIN ? tile_of(p, s, n) * PACK_TILE : 0;
+            const int seen = min(CAUSAL ? me.q : len, len - 1) - kv0 - half * 4, from = WIN ? me.q + 1 - p.window - kv0 - half * 4 : 0, stay = WIN ? p.sinks - kv0 - half * 4 : 0;
 #pragma unroll
-            for (int v = 0; v < 16; ++v)
-                d += 32 * g + (v >> 2) * 8 + (v & 3) <= seen ? fast_exp2(fmaf(x[g][v], c2, -l2)) * dp[g][v] : 0.0f;
+            for (int g = 0; g < 2; ++g)
+#pragma unroll
+                for (int v = 0; v < 16; ++v) {
+                    const int k = 32 * g + (v >> 2) * 8 + (v & 3);
+                    d += k <= seen && (!WIN || k >= from || k < stay) ? fast_exp2(fmaf(x[g][v], c2, -l2)) * dp[g][v] : 0.0f;
+                }
+            if (!WIN || ++n >= tiles) break;
+            __syncthreads();
+            fetch_tile(tile_of(p, s, n));
+            dma_wait();
+            __syncthreads();
+        }
         d += __shfl_xor(d, 32, 64);
-        if (valid && half == 0 && (!CAUSAL || me.q < PACK_TILE)) p.dsum[at] = d;
+        if (valid && half == 0 && (!CAUSAL || narrow || me.q < PACK_TILE)) p.dsum[at] = d;
         __syncthreads();                                          // the next strip's tiles
     }
 }
 
 // The rows of a wavefront again, one by one (see the head of the file).
-template <int DH, bool DK_ROLE>
+template <int DH, bool DK_ROLE, bool WIN>
 __device__ __forceinline__ void dkv_rows_again(float* k_s, const Params& p, const BStrip& s, int k0, int lane) {
     constexpr int NA = (DH + 63) / 64;
     const int len = s.it.len, G = p.G;
@@ -349,7 +385,8 @@ __device__ __forceinline__ void dkv_rows_again(float* k_s, const Params& p, cons
         load_row(k_s + DH, s.v + j * s.ld, p.dh, lane);
         row_loaded();
         float sum[NA] = {};
-        for (int i = max(j * G, s.it.tile0 * PACK_TILE); i < last; ++i) {          // a row after another: this is no common case
+        const int end = WIN && j >= p.sinks ? min(last, (j + p.window) * G) : last;
+        for (int i = max(j * G, s.it.tile0 * PACK_TILE); i < end; ++i) {           // a row after another: this is no common case
             const Row w = row_of(p, i);
             const bf16_t* qp = s.q + w.q * s.ld + w.g * p.dh;
             const bf16_t* dp = dobase + w.q * s.ldo + w.g * p.dh;
@@ -377,7 +414,7 @@ __device__ __forceinline__ void dkv_rows_again(float* k_s, const Params& p, cons
     }
 }
 
-template <int DH>
+template <int DH, bool WIN>
 __device__ __forceinline__ void dq_rows_again(float* q_s, const Params& p, const BStrip& s, int r0, int lane) {
     const bool whole = s.it.slot < 0;
     const bf16_t* dobase = p.d_o + s.it.t0 * s.ldo + (int64_t)s.hk * p.G * p.dh;
@@ -389,8 +426,12 @@ __device__ __forceinline__ void dq_rows_again(float* q_s, const Params& p, const
         row_loaded();
         bf16_t* dqp = p.dqkv + (s.it.t0 + w.q) * s.ld + (int64_t)(s.hk * p.G + w.g) * p.dh;
         const int64_t a = s.row0 + (int64_t)w.q * p.nq + w.g;
-        attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, s.it.tile0 * PACK_TILE, min(w.q + 1, s.it.tile1 * PACK_TILE), p.scale, p.lse[a], p.dsum[a], lane,
-                                    [&](int d, float v) { if (whole) dqp[d] = (bf16_t)(v * p.scale); else part[(i - s.it.first) * DH + d] = v; });
+        auto store = [&](int d, float v) { if (whole) dqp[d] = (bf16_t)(v * p.scale); else part[(i - s.it.first) * DH + d] = v; };
+        const int beg = s.it.tile0 * PACK_TILE, end = s.it.tile1 * PACK_TILE;
+        if constexpr (WIN)
+            attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, beg, end, p.scale, p.lse[a], p.dsum[a], lane, store, WindowKeys<bf16_t>{p, s, w.q});
+        else
+            attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, beg, min(w.q + 1, end), p.scale, p.lse[a], p.dsum[a], lane, store);
         row_loaded();
     }
 }
@@ -404,8 +445,9 @@ __device__ __forceinline__ void dq_rows_again(float* q_s, const Params& p, const
 constexpr int WAVES8 = 512;
 constexpr int P_BYTES = 32 * 32 * 4;
 template <int DH> constexpr int dkv_lds() { return 5 * tile_bytes<DH>() + 3 * 2 * PACK_TILE * 4 + 2 * 4 * P_BYTES; }
-template <int DH, bool CAUSAL, bool DK_ROLE>
+template <int DH, int MASK, bool DK_ROLE>
 __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStrip& s) {
+    constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2;
     constexpr int TERMS = 5 * TB, PS = TERMS + 3 * 2 * PACK_TILE * 4;  // three Q tiles, two dO tiles, three times LSE*log2e and D, P
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
@@ -475,7 +517,9 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
     __syncthreads();                                       // those stages are free
 
     // rows that see one of this wavefront's keys, in scalar registers: with the products in the loop it spilled
-    const int see_lo = __builtin_amdgcn_readfirstlane(CAUSAL ? k0 * G - 31 : 0), see_hi = __builtin_amdgcn_readfirstlane(k0 < len ? rows : 0);
+    const int see_lo = __builtin_amdgcn_readfirstlane(CAUSAL ? k0 * G - 31 : 0), see_hi = __builtin_amdgcn_readfirstlane(k0 >= len ? 0 : WIN && k0 >= p.sinks ? min(rows, (min(k0 + 31, len - 1) + p.window) * G) : rows);
+    // the first row that does not see one of them any more
+    const int gone = WIN && k0 + 31 >= p.sinks ? __builtin_amdgcn_readfirstlane((max(k0, p.sinks) + p.window) * G) : 0x7fffffff;
     unsigned other = TB;                                   // to the other stage of dO
     f32x16 x;                                              // scores, then P; or dP, then dS
     bool pending = false;                                  // dP of the sub-tile before waits for its P
@@ -532,8 +576,9 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
             product(stg, sbc);
             bf16x8 fr[NF];
             fetch_t(stg, sbc, fr);
-            if (qs0 + 31 >= rows || k0 + 31 >= len || (CAUSAL && (k0 + 31) * G > qs0)) {   // wave-uniform: diagonal or an end
-                const int from = kv < len ? (CAUSAL ? kv * G : 0) - qs0 - 4 * half : 1 << 30, to = rows - qs0 - 4 * half;
+            if (qs0 + 31 >= rows || k0 + 31 >= len || (CAUSAL && (k0 + 31) * G > qs0) || (WIN && qs0 + 31 >= gone)) {   // wave-uniform: diagonal or an end
+                const int from = kv < len ? (CAUSAL ? kv * G : 0) - qs0 - 4 * half : 1 << 30;
+                const int to = (WIN && kv >= p.sinks ? min(rows, (min(kv, len) + p.window) * G) : rows) - qs0 - 4 * half;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) {
                     const int r = 8 * (v >> 2) + (v & 3);
@@ -618,7 +663,7 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
     }
     if (!CAUSAL || !any_nonfinite(z)) return;
     rows_stored();
-    dkv_rows_again<DH, DK_ROLE>(reinterpret_cast<float*>(smem) + wave * 2 * DH, p, s, k0, lane);
+    dkv_rows_again<DH, DK_ROLE, WIN>(reinterpret_cast<float*>(smem) + wave * 2 * DH, p, s, k0, lane);
 }
 
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
@@ -626,8 +671,9 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
 // halves are added through LDS at the end.  Transposed score tile: lane = row.  1.18 us a tile, 1.36 PFLOP/s over the chip, and about 6 us to begin and
 // end a strip (item 0.9, loads 2.6 to 3.2, end 2.2): 1038 workgroups of 22 us in the batch above, both lists in one launch of 276 us.
 template <int DH> constexpr int dq_lds() { return std::max(6 * tile_bytes<DH>(), 4 * 64 * (DH / 2) * 4); }
-template <int DH, bool CAUSAL>
+template <int DH, int MASK>
 __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStrip& s) {
+    constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32;
     constexpr int NCH = NCHUNKS<DH, WAVES8>;
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
@@ -650,7 +696,8 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
     unsigned off[NCH];
     dma_offsets<DH, WAVES8>(off, s.ld, p.dh, t);
-    auto fetch_tile = [&](int kt, unsigned stage) {
+    auto fetch_tile = [&](int v, unsigned stage) {
+        const int kt = WIN ? tile_of(p, s, v) : v;
         tile_dma<DH, WAVES8>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), stage, off, 0, wave);
         tile_dma<DH, WAVES8>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
     };
@@ -679,8 +726,8 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
     auto step = [&](int kt, auto stg) __attribute__((always_inline)) {
         constexpr int OFF = decltype(stg)::value * 2 * TB;
         if (kt + 1 < ntiles) fetch_tile(kt + 1, lds0 + (1 - decltype(stg)::value) * 2 * TB);
-        const int kv0 = kt * PACK_TILE + kvh * 32;
-        if (kv0 < kv_end) {                                        // wavefront-uniform
+        const int kv0 = (WIN ? tile_of(p, s, kt) : kt) * PACK_TILE + kvh * 32;
+        if (kv0 < kv_end && (!WIN || kv0 + 32 > q_lo + 1 - p.window || kv0 < p.sinks)) {   // wavefront-uniform
             // the fragments of the three products (K, V, K transposed) through a rolling window of W registers
             f32x16 x = zero16(), dp = zero16();
             constexpr int W = DH <= 64 ? NF : NF / 2;
@@ -707,6 +754,11 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
                 const int seen = valid ? min(CAUSAL ? me.q : len, len - 1) - kv0 - half * 4 : -1;
 #pragma unroll
                 for (int v = 0; v < 16; ++v) x[v] = (v >> 2) * 8 + (v & 3) <= seen ? x[v] : -INFINITY;
+            }
+            if (WIN && kv0 < q_hi + 1 - p.window && kv0 + 32 > p.sinks) {
+                const int from = me.q + 1 - p.window - kv0 - half * 4, stay = p.sinks - kv0 - half * 4;
+#pragma unroll
+                for (int v = 0; v < 16; ++v) x[v] = (v >> 2) * 8 + (v & 3) >= from || (v >> 2) * 8 + (v & 3) < stay ? x[v] : -INFINITY;
             }
 #pragma unroll
             for (int v = 0; v < 16; ++v) dp[v] = fast_exp2(fmaf(x[v], c2, -l2)) * (dp[v] - dsum);
@@ -771,44 +823,44 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
     }
     if (!CAUSAL || !any_nonfinite(z)) return;
     rows_stored();
-    dq_rows_again<DH>(reinterpret_cast<float*>(smem) + qs * (DH / 2) * 64, p, s, r0, lane);   // this wavefront alone reads its merge area
+    dq_rows_again<DH, WIN>(reinterpret_cast<float*>(smem) + qs * (DH / 2) * 64, p, s, r0, lane);   // this wavefront alone reads its merge area
 }
 
 // Workgroups: those of dK/dV, then those of dQ, then what the host, which does not know the lengths, has launched too many (between the two lists they kept
 // units waiting: 64 sequences of 128, 8 heads of 64, 43.8 -> 39.9 us, 512 of 16 100.9 -> 94.3).
 // Up to head size 64 two workgroups share a compute unit (128 registers, 80 KB of LDS each).
-template <int DH, bool CAUSAL>
+template <int DH, int MASK>
 __global__ __launch_bounds__(WAVES8, DH <= 64 ? 4 : 2) void attn_packed_bwd_kernel(Params p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     // another call's plan: some number within the list, so that what is read of it before it is refused is in the plan
     const int of_kv = (int)min((unsigned)reinterpret_cast<const PackHeader*>(p.plan + p.header)->items[1], (unsigned)p.kv_items) * p.nkv, wg = blockIdx.x;
     BStrip s;
     if (wg >= of_kv) {
-        if (take_strip(p, 0, wg - of_kv, s)) dq_body<DH, CAUSAL>(smem, p, s);
+        if (take_strip(p, 0, wg - of_kv, s)) dq_body<DH, MASK>(smem, p, s);
         return;
     }
     if (!take_strip(p, 1, wg, s)) return;
     // the role is uniform per wavefront; both bodies run the same loop and the same barriers
-    if ((threadIdx.x >> 6) < 4) dkv_body<DH, CAUSAL, false>(smem, p, s);
-    else dkv_body<DH, CAUSAL, true>(smem, p, s);
+    if ((threadIdx.x >> 6) < 4) dkv_body<DH, MASK, false>(smem, p, s);
+    else dkv_body<DH, MASK, true>(smem, p, s);
 }
 
-template <int DH, bool CAUSAL>
+template <int DH, int MASK>
 hipError_t run_fwd(const PackAttnArgs& a) {
     const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
     const PackLayout L = pack_layout(a.sequences, a.M, a.nq, a.nkv, shares);
     Params p = make_params<bf16_t>(a, L);
     p.part[0] = (float*)a.ws;
     constexpr int lds = fwd_lds<DH>();
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_fwd_kernel<DH, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_fwd_kernel<DH, MASK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, CAUSAL>), dim3((unsigned)(L.cap[0] * a.nkv)), dim3(WAVES4), lds, a.stream, p);
+    hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, MASK>), dim3((unsigned)(L.cap[0] * a.nkv)), dim3(WAVES4), lds, a.stream, p);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || shares.of[0] == 0) return e;
     hipLaunchKernelGGL((attn_packed_fwd_join_kernel<bf16_t, DH>), dim3(join_wgs(L, a.nkv)), dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
-template <int DH, bool CAUSAL>
+template <int DH, int MASK>
 hipError_t run_bwd(const PackAttnArgs& a) {
     const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
     const PackLayout L = pack_layout(a.sequences, a.M, a.nq, a.nkv, shares);
@@ -817,30 +869,32 @@ hipError_t run_bwd(const PackAttnArgs& a) {
     p.part[0] = (float*)a.ws;
     p.part[1] = (float*)((char*)a.ws + w.part[0]);
     const int strips = (int)std::min<int64_t>(L.cap[0] * a.nkv, 2 * compute_units()), rows = (int)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units());
-    hipLaunchKernelGGL((attn_packed_dsum_kernel<DH, CAUSAL>), dim3((unsigned)(strips + rows)), dim3(WAVES4), dsum_lds<DH>(), a.stream, p, strips);
+    hipLaunchKernelGGL((attn_packed_dsum_kernel<DH, MASK>), dim3((unsigned)(strips + rows)), dim3(WAVES4), dsum_lds<DH>(), a.stream, p, strips);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     p.kv_items = (int)L.cap[1];
     constexpr int lds = std::max(dkv_lds<DH>(), dq_lds<DH>());
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_bwd_kernel<DH, CAUSAL>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_bwd_kernel<DH, MASK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((attn_packed_bwd_kernel<DH, CAUSAL>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv)), dim3(WAVES8), lds, a.stream, p);
+    hipLaunchKernelGGL((attn_packed_bwd_kernel<DH, MASK>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv)), dim3(WAVES8), lds, a.stream, p);
     e = hipGetLastError();
     if (e != hipSuccess || shares.of[0] == 0) return e;
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<bf16_t, DH>), dim3(join_wgs(L, a.nkv)), dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
-template <bool CAUSAL>
+template <int MASK>
 hipError_t run(const PackAttnArgs& a, bool bwd) {
     switch (padded(a.dh)) {
-        case 32: return bwd ? run_bwd<32, CAUSAL>(a) : run_fwd<32, CAUSAL>(a);
-        case 64: return bwd ? run_bwd<64, CAUSAL>(a) : run_fwd<64, CAUSAL>(a);
-        case 96: return bwd ? run_bwd<96, CAUSAL>(a) : run_fwd<96, CAUSAL>(a);
-        default: return bwd ? run_bwd<128, CAUSAL>(a) : run_fwd<128, CAUSAL>(a);
+        case 32: return bwd ? run_bwd<32, MASK>(a) : run_fwd<32, MASK>(a);
+        case 64: return bwd ? run_bwd<64, MASK>(a) : run_fwd<64, MASK>(a);
+        case 96: return bwd ? run_bwd<96, MASK>(a) : run_fwd<96, MASK>(a);
+        default: return bwd ? run_bwd<128, MASK>(a) : run_fwd<128, MASK>(a);
     }
 }
 }  // namespace
 
-hipError_t attn_packed_bf16(const PackAttnArgs& a, bool bwd) { return a.causal ? run<true>(a, bwd) : run<false>(a, bwd); }
+hipError_t attn_packed_bf16(const PackAttnArgs& a, bool bwd) {
+    return a.mask == PACK_WINDOW ? run<PACK_WINDOW>(a, bwd) : a.mask == PACK_CAUSAL ? run<PACK_CAUSAL>(a, bwd) : run<PACK_ALL>(a, bwd);
+}
 
 }  // namespace tpl

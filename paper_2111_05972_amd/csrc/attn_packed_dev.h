@@ -15,7 +15,7 @@ namespace {
 
 template <typename T>
 struct PackParams {
-    int sequences, M, nq, nkv, G, dh, causal;
+    int sequences, M, nq, nkv, G, dh, mask, window, sinks;
     unsigned div_g;               // 65536 / G + 1: x / G = x * div_g >> 16 for x < 64 + G
     const int* plan;
     int64_t seen, header, items[2], joins[2];
@@ -26,6 +26,11 @@ struct PackParams {
     int many;                     // float: short strips above which a wavefront has a quarter to itself
     float scale;
 };
+// Whether the plan at hand was made for this call.
+template <typename T>
+__device__ __forceinline__ bool pack_matches(const PackHeader* h, const PackParams<T>& p) {
+    return h->sequences == p.sequences && h->tokens == p.M && h->nq == p.nq && h->nkv == p.nkv && h->mask == p.mask && h->window == p.window && h->sinks == p.sinks;
+}
 // What a workgroup works on.
 template <typename T>
 struct Strip {
@@ -54,7 +59,7 @@ __device__ __forceinline__ bool take_strip(const PackParams<T>& p, int side, int
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
     const int i = wg / p.nkv;
     s.it = pack_items(p.plan, p.items[side])[i];                  // within the plan: requested beside the header, not after it
-    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal) || i >= h->items[side]) return false;
+    if (!pack_matches(h, p) || i >= h->items[side]) return false;
     set_strip(p, wg - i * p.nkv, s);
     return true;
 }
@@ -65,6 +70,23 @@ __device__ __forceinline__ void strip_at(const PackParams<T>& p, int side, int i
     s.it = pack_items(p.plan, p.items[side])[n];
     set_strip(p, i - n * p.nkv, s);
 }
+// The keys of an item's tiles when tiles are left out: number `j` of them, counted without these, is key tile_key(j).
+template <typename T>
+__device__ __forceinline__ int tile_of(const PackParams<T>& p, const Strip<T>& s, int v) { return v * PACK_TILE >= p.sinks ? v + s.it.skip : v; }
+// Whether query q sees key j under a window.
+template <typename T>
+__device__ __forceinline__ bool window_sees(const PackParams<T>& p, int q, int j) { return j <= q && (j > q - p.window || j < p.sinks); }
+// For the row-by-row form: key number j of the tiles for query q, -1: it does not see it.
+template <typename T>
+struct WindowKeys {
+    const PackParams<T>& p;
+    const Strip<T>& s;
+    int q;
+    __device__ __forceinline__ int operator()(int j) const {
+        const int k = (j & (PACK_TILE - 1)) + tile_of(p, s, j / PACK_TILE) * PACK_TILE;
+        return window_sees(p, q, k) ? k : -1;
+    }
+};
 // A flattened row: its query and its head in the group.
 struct Row { int q, g; };
 template <typename T>
@@ -95,7 +117,7 @@ template <typename T, int DH>
 __global__ __launch_bounds__(32 * JOIN_ROWS) void attn_packed_fwd_join_kernel(PackParams<T> p) {
     constexpr int PSZ = PACK_BLK * (DH + 2);
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
-    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return;
+    if (!pack_matches(h, p)) return;
     const int all = h->joins[0] * p.nkv * JOIN_WGS, col = 4 * (threadIdx.x & 31);
     for (int i = blockIdx.x; i < all; i += gridDim.x) {
         const int hk = i % p.nkv, rest = i / p.nkv;
@@ -150,7 +172,7 @@ __device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int64_t first,
 template <typename T, int DH>
 __global__ __launch_bounds__(32 * JOIN_ROWS) void attn_packed_bwd_join_kernel(PackParams<T> p) {
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
-    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return;
+    if (!pack_matches(h, p)) return;
     const int of_q = h->joins[0] * p.nkv * JOIN_WGS, of_kv = h->joins[1] * p.nkv * JOIN_WGS, col = 4 * (threadIdx.x & 31);
     for (int i = blockIdx.x; i < of_q + 2 * of_kv; i += gridDim.x) {
         const int which = i < of_q ? 0 : i < of_q + of_kv ? 1 : 2, side = which > 0, n = i - (which == 0 ? 0 : which == 1 ? of_q : of_q + of_kv);
@@ -176,7 +198,8 @@ __global__ __launch_bounds__(32 * JOIN_ROWS) void attn_packed_bwd_join_kernel(Pa
 template <typename T>
 PackParams<T> make_params(const PackAttnArgs& a, const PackLayout& L) {
     PackParams<T> p{};
-    p.sequences = (int)a.sequences; p.M = (int)a.M; p.nq = a.nq; p.nkv = a.nkv; p.G = a.nq / a.nkv; p.dh = a.dh; p.causal = a.causal;
+    p.sequences = (int)a.sequences; p.M = (int)a.M; p.nq = a.nq; p.nkv = a.nkv; p.G = a.nq / a.nkv; p.dh = a.dh;
+    p.mask = a.mask; p.window = a.window; p.sinks = a.sinks;
     p.div_g = 65536u / (unsigned)p.G + 1u;
     p.plan = a.plan; p.seen = L.seen; p.header = L.header;
     for (int s = 0; s < 2; ++s) { p.items[s] = L.items[s]; p.joins[s] = L.joins[s]; }

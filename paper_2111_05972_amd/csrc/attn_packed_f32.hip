@@ -24,6 +24,11 @@ using FParams = PackParams<float>;
 using FStrip = Strip<float>;
 constexpr int QUARTERS = PACK_BLK / XT;
 
+// Of the 32-row tiles that an item counts, with a window without those it leaves out: the first key of tile t, and how many there are up to key `seen`.
+template <bool WIN> __device__ __forceinline__ int xfirst(const FParams& p, const FStrip& s, int t) {
+    return WIN ? (t & 1) * XT + tile_of(p, s, t >> 1) * PACK_TILE : t * XT;
+}
+template <bool WIN> __device__ __forceinline__ int xtiles(const FParams& p, const FStrip& s, int seen) { return (seen + XT - 1) / XT - (WIN ? 2 * s.it.skip : 0); }
 // 32 rows of K or V from row `row0` on: zero past the sequence.
 __device__ __forceinline__ i32x4 xtile_rsrc(const float* base, int64_t ld, int row0, int rows, int dh) {
     const int left = rows - row0 < XT ? rows - row0 : XT;
@@ -55,7 +60,7 @@ __device__ __forceinline__ void xfetch_flat(const FParams& p, const FStrip& s, c
 constexpr int ALONE = -1;
 template <bool MANY> __device__ __forceinline__ int take_quarter(const FParams& p, bool bwd, int u, FStrip& s, int& sub) {
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
-    if (!pack_matches(h, p.sequences, p.M, p.nq, p.nkv, p.causal)) return -1;
+    if (!pack_matches(h, p)) return -1;
     const int first[2] = {h->first_short[0] * p.nkv, bwd ? h->first_short[1] * p.nkv : 0};
     const int after[2] = {h->items[0] * p.nkv - first[0], bwd ? h->items[1] * p.nkv - first[1] : 0};        // short ones
     for (int side = 1; side >= 0; --side) {
@@ -91,7 +96,7 @@ __device__ __forceinline__ float xalone(const f32x16 (&acc)[DH / 32], float f, P
     return z;
 }
 
-template <int DH, bool MANY>
+template <int DH, bool MANY, bool WIN>
 __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr int TB = xtile_bytes<DH>(), NL = xloads<DH>();
@@ -115,26 +120,26 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[d][v] = 0.0f;
     float m = -INFINITY, l = 0.0f;
-    const int t0 = 2 * s.it.tile0, seen = p.causal ? q_hi + 1 : len, nt = min(2 * s.it.tile1, (seen + XT - 1) / XT);
+    const int t0 = 2 * s.it.tile0, seen = p.mask != PACK_ALL ? q_hi + 1 : len, nt = min(2 * s.it.tile1, xtiles<WIN>(p, s, seen));
     char* kt_ = smem + wave * 2 * TB;
     const unsigned lk = (unsigned)(uintptr_t)(lds_void_ptr)kt_, lv = lk + TB;
     unsigned off[NL];
     xoffsets<DH>(off, s.ld, p.dh, lane);
-    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? t * XT : len, len, p.dh), lds, off, 0, s.ld); };
+    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? xfirst<WIN>(p, s, t) : len, len, p.dh), lds, off, 0, s.ld); };
     if (t0 + mine < nt) { fetch(s.k, lk, t0 + mine); fetch(s.v, lv, t0 + mine); }
     for (int t = t0 + mine; t < nt; t += step) {
         xwait<NL>();                                              // K of this tile (V is younger)
         f32x16 x = xscores<DH>(kt_, qr, lane);
         xreads_done();
         fetch(s.k, lk, t + step);                                    // past the last tile: zeros, so that the count of loads in flight stays
-        const int k0 = t * XT;
-        const bool edge = k0 + XT > len || (p.causal && k0 + XT - 1 > q_lo);
+        const int k0 = xfirst<WIN>(p, s, t);
+        const bool edge = k0 + XT > len || (p.mask != PACK_ALL && k0 + XT - 1 > q_lo) || (WIN && k0 < q_hi + 1 - p.window);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             x[v] *= p.scale;
             if (edge) {
                 const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
-                if (k >= len || (p.causal && k > me.q)) x[v] = -INFINITY;
+                if (k >= len || (WIN ? !window_sees(p, me.q, k) : p.mask != PACK_ALL && k > me.q)) x[v] = -INFINITY;
             }
         }
         float mt = x[0];
@@ -194,7 +199,7 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
         z = xcombine<DH>(smem, acc, f, wave, lane, put);
         if (wave == 0 && half == 0) stats(mt, lt);
     }
-    if (!p.causal || !__any(z != 0.0f)) return;
+    if (p.mask == PACK_ALL || !__any(z != 0.0f)) return;
     rows_stored();
     float* q_s = xrows<DH>(smem, wave);
     for (int i = r0; i < r0 + XT && i < s.rows; ++i) {
@@ -203,8 +208,12 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
         row_loaded();
         float* oi = whole ? p.o + (s.it.t0 + w.q) * s.ldo + (head + w.g) * p.dh : part + (i - s.it.first) * DH;
         float mr, lr;
-        attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, s.it.tile0 * PACK_TILE, min(w.q + 1, s.it.tile1 * PACK_TILE), p.scale, whole, lane, mr, lr,
-                                     [&](int d, float v) { if (alone || xmine(d, wave)) oi[d] = v; });
+        auto store = [&](int d, float v) { if (alone || xmine(d, wave)) oi[d] = v; };
+        const int beg = s.it.tile0 * PACK_TILE, end = s.it.tile1 * PACK_TILE;
+        if constexpr (WIN)
+            attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, beg, end, p.scale, whole, lane, mr, lr, store, WindowKeys<float>{p, s, w.q});
+        else
+            attn_row_fwd<(DH + 63) / 64>(q_s, s.k, s.v, s.ld, p.dh, beg, min(w.q + 1, end), p.scale, whole, lane, mr, lr, store);
         if (lane == 0 && (alone || wave == 0)) {
             if (whole) p.lse[s.row0 + (int64_t)w.q * p.nq + w.g] = mr + logf(lr);
             else { part[PACK_BLK * DH + i - s.it.first] = mr; part[PACK_BLK * DH + PACK_BLK + i - s.it.first] = lr; }
@@ -213,7 +222,7 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
     }
 }
 
-template <int DH, bool MANY>
+template <int DH, bool MANY, bool WIN>
 __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStrip& s, int sub) {
     constexpr int TB = xtile_bytes<DH>(), NL = xloads<DH>();
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -239,10 +248,10 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[d][v] = 0.0f;
-    const int t0 = 2 * s.it.tile0, seen = p.causal ? q_hi + 1 : len, nt = min(2 * s.it.tile1, (seen + XT - 1) / XT);
+    const int t0 = 2 * s.it.tile0, seen = p.mask != PACK_ALL ? q_hi + 1 : len, nt = min(2 * s.it.tile1, xtiles<WIN>(p, s, seen));
     unsigned off[NL];
     xoffsets<DH>(off, s.ld, p.dh, lane);
-    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? t * XT : len, len, p.dh), lds, off, 0, s.ld); };
+    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? xfirst<WIN>(p, s, t) : len, len, p.dh), lds, off, 0, s.ld); };
     if (t0 + mine < nt) { fetch(s.v, lv, t0 + mine); fetch(s.k, lk, t0 + mine); }   // V is read first
     for (int t = t0 + mine; t < nt; t += step) {
         xwait<NL>();
@@ -251,15 +260,15 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
         fetch(s.v, lv, t + step);
         xwait<NL>();
         const f32x16 x = xscores<DH>(kt_, qr, lane);
-        const int k0 = t * XT;
-        const bool edge = k0 + XT > len || (p.causal && k0 + XT - 1 > q_lo);
+        const int k0 = xfirst<WIN>(p, s, t);
+        const bool edge = k0 + XT > len || (p.mask != PACK_ALL && k0 + XT - 1 > q_lo) || (WIN && k0 < q_hi + 1 - p.window);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
             float w = expf(x[v] * p.scale - L);
             w *= dp[v] - D;
             if (edge) {
                 const int k = k0 + 8 * (v >> 2) + 4 * half + (v & 3);
-                if (k >= len || (p.causal && k > me.q)) w = 0.0f;
+                if (k >= len || (WIN ? !window_sees(p, me.q, k) : p.mask != PACK_ALL && k > me.q)) w = 0.0f;
             }
             dp[v] = w;
         }
@@ -277,7 +286,7 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
         if (!whole || (valid && c < p.dh)) *reinterpret_cast<float4*>(dqp + c) = make_float4(v[0], v[1], v[2], v[3]);
     };
     const float z = alone ? xalone<DH>(acc, f1, put) : xcombine<DH>(smem, acc, f, wave, lane, put);
-    if (!p.causal || !__any(z != 0.0f)) return;
+    if (p.mask == PACK_ALL || !__any(z != 0.0f)) return;
     rows_stored();
     float* q_s = xrows<DH>(smem, wave);
     for (int i = r0; i < r0 + XT && i < s.rows; ++i) {
@@ -287,13 +296,17 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
         row_loaded();
         float* dqi = whole ? p.dqkv + (s.it.t0 + w.q) * s.ld + (head + w.g) * p.dh : part + (i - s.it.first) * DH;
         const int64_t a = s.row0 + (int64_t)w.q * p.nq + w.g;
-        attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, s.it.tile0 * PACK_TILE, min(w.q + 1, s.it.tile1 * PACK_TILE), p.scale, p.lse[a], p.dsum[a],
-                                    lane, [&](int d, float v) { if (alone || xmine(d, wave)) dqi[d] = v * f1; });
+        auto store = [&](int d, float v) { if (alone || xmine(d, wave)) dqi[d] = v * f1; };
+        const int beg = s.it.tile0 * PACK_TILE, end = s.it.tile1 * PACK_TILE;
+        if constexpr (WIN)
+            attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, beg, end, p.scale, p.lse[a], p.dsum[a], lane, store, WindowKeys<float>{p, s, w.q});
+        else
+            attn_row_dq<(DH + 63) / 64>(q_s, q_s + DH, s.k, s.v, s.ld, p.dh, beg, min(w.q + 1, end), p.scale, p.lse[a], p.dsum[a], lane, store);
         row_loaded();
     }
 }
 
-template <int DH, bool MANY>
+template <int DH, bool MANY, bool WIN>
 __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStrip& s, int sub) {
     constexpr int TB = xtile_bytes<DH>();
     const int lane = threadIdx.x & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -316,7 +329,10 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
     char* qt_ = smem + wave * 2 * TB;
     const unsigned lq = (unsigned)(uintptr_t)(lds_void_ptr)qt_, lg = lq + TB;
     float* terms = reinterpret_cast<float*>(smem + 8 * TB) + wave * 2 * XT;   // LSE, D of the tile's rows
-    const int t0 = max(2 * s.it.tile0, p.causal ? k0 * p.G / XT : 0), nt = min(2 * s.it.tile1, (s.rows + XT - 1) / XT);
+    // rows that see one of the keys: below `rows`, and with a window all but the first keys are out of sight from some row on
+    const int rows = WIN && k0 >= p.sinks ? min(s.rows, (min(k0 + XT, len) - 1 + p.window) * p.G) : s.rows;
+    const int gone = WIN && k0 + XT > p.sinks ? (max(k0, p.sinks) + p.window) * p.G : 0x7fffffff;
+    const int t0 = max(2 * s.it.tile0, p.mask != PACK_ALL ? k0 * p.G / XT : 0), nt = min(2 * s.it.tile1, (rows + XT - 1) / XT);
     auto term = [&](int t) {                                      // lanes 0..31: LSE, lanes 32..63: D
         const int i = t * XT + (lane & 31);
         const Row w = row_of(p, min(i, s.rows - 1));
@@ -330,7 +346,8 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
         fetch_q(t0 + mine);
         fetch_g(t0 + mine);
     }
-    const int from = p.causal ? k * p.G : 0;                      // the first row that sees this lane's key
+    const int from = p.mask != PACK_ALL ? k * p.G : 0;            // the first row that sees this lane's key
+    const int to = WIN && k >= p.sinks ? min(s.rows, (min(k, len) + p.window) * p.G) : s.rows;
     for (int t = t0 + mine; t < nt; t += step) {
         const int nx = t + step;
         terms[lane] = tn;
@@ -339,7 +356,7 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
         f32x16 w = xscores<DH>(qt_, kr, lane);
         f32x16 ds = xscores<DH>(qt_ + TB, vr, lane);              // dP = dO V^T
         const int q0 = t * XT;
-        const bool edge = q0 + XT > s.rows || k0 + XT > len || (p.causal && (k0 + XT - 1) * p.G > q0);
+        const bool edge = q0 + XT > s.rows || k0 + XT > len || (p.mask != PACK_ALL && (k0 + XT - 1) * p.G > q0) || (WIN && q0 + XT > gone);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float4 l4 = *reinterpret_cast<const float4*>(terms + 8 * i + 4 * half);
@@ -349,7 +366,7 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
             for (int j = 0; j < 4; ++j) {
                 const int v = 4 * i + j, row = q0 + 8 * i + 4 * half + j;
                 const float e = expf(w[v] * p.scale - lv[j]), g = e * (ds[v] - dv4[j]);
-                const bool out = edge && (row >= s.rows || !valid || row < from);
+                const bool out = edge && (row >= to || !valid || row < from);
                 w[v] = out ? 0.0f : e;
                 ds[v] = out ? 0.0f : g;
             }
@@ -382,7 +399,7 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
         z = xcombine<DH>(smem, dk, fk, wave, lane, put(kp));
         z += xcombine<DH>(smem, dv, fv, wave, lane, put(vp));
     }
-    if (!p.causal || !__any(z != 0.0f)) return;
+    if (p.mask == PACK_ALL || !__any(z != 0.0f)) return;
     rows_stored();
     constexpr int NA = (DH + 63) / 64;
     float* k_s = xrows<DH>(smem, wave);
@@ -392,7 +409,8 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
         row_loaded();
         float dks[NA] = {}, dvs[NA] = {};
         const int last = min(s.rows, s.it.tile1 * PACK_TILE);
-        for (int i = max(j * p.G, s.it.tile0 * PACK_TILE); i < last; ++i) {
+        const int end = WIN && j >= p.sinks ? min(last, (j + p.window) * p.G) : last;
+        for (int i = max(j * p.G, s.it.tile0 * PACK_TILE); i < end; ++i) {
             const Row w = row_of(p, i);
             const float* qp = s.q + w.q * s.ld + w.g * p.dh;
             const float* gp = dobase + w.q * s.ldo + w.g * p.dh;
@@ -422,31 +440,31 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
 }
 
 __global__ __launch_bounds__(256) void attn_packed_f32_dsum_kernel(FParams p) {
-    if (pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p.sequences, p.M, p.nq, p.nkv, p.causal))
+    if (pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p))
         dsum_rows(p, (int64_t)blockIdx.x * 16, (int64_t)gridDim.x * 16, 0);
 }
 
 // Two workgroups share a compute unit up to head size 64 (see attn_f32.hip); wider heads need more than 256 registers.
-template <int DH, bool MANY>
+template <int DH, bool MANY, bool WIN>
 __global__ __launch_bounds__(256, DH <= 64 ? 2 : 1) void attn_packed_f32_bwd_kernel(FParams p) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     FStrip s;
     int sub;
     const int side = take_quarter<MANY>(p, true, blockIdx.x, s, sub);
     if (side < 0) return;
-    if (side) f32_dkv<DH, MANY>(smem, p, s, sub);
-    else f32_dq<DH, MANY>(smem, p, s, sub);
+    if (side) f32_dkv<DH, MANY, WIN>(smem, p, s, sub);
+    else f32_dq<DH, MANY, WIN>(smem, p, s, sub);
 }
 
 // Short strips above which a wavefront has a quarter to itself: three quarters of the workgroups that run at once.  48 sequences of 918 tokens together,
 // 32 / 8 heads of 96, forward and backward 55 and 117 us, so 33 and 98; 60 of 600, 8 heads of 64, 14.7 and 32.4, so 11.2 and 28.5; but 30 of 1489, 2 heads of 64,
 // 25 us backward, so 51: each wavefront then has up to six tiles in a row.
 int many_strips(int DH) { return compute_units() * (DH <= 32 ? 4 : DH <= 64 ? 2 : 1) * 3 / 4; }
-template <int DH, bool MANY>
+template <int DH, bool MANY, bool WIN>
 hipError_t launch(const PackAttnArgs& a, bool bwd) {
     constexpr int lds = xlds_bytes<DH>();
-    static const hipError_t attr_f = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_fwd_kernel<DH, MANY>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    static const hipError_t attr_b = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_bwd_kernel<DH, MANY>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr_f = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_fwd_kernel<DH, MANY, WIN>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    static const hipError_t attr_b = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_f32_bwd_kernel<DH, MANY, WIN>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
     if (attr_f != hipSuccess || attr_b != hipSuccess) return attr_f != hipSuccess ? attr_f : attr_b;
     const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
     const PackLayout L = pack_layout(a.sequences, a.M, a.nq, a.nkv, shares);
@@ -456,7 +474,7 @@ hipError_t launch(const PackAttnArgs& a, bool bwd) {
     const dim3 join(join_wgs(L, a.nkv));
     hipError_t e;
     if (!bwd) {
-        hipLaunchKernelGGL((attn_packed_f32_fwd_kernel<DH, MANY>), dim3((unsigned)(L.cap[0] * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
+        hipLaunchKernelGGL((attn_packed_f32_fwd_kernel<DH, MANY, WIN>), dim3((unsigned)(L.cap[0] * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
         if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
         hipLaunchKernelGGL((attn_packed_fwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
         return hipGetLastError();
@@ -464,14 +482,16 @@ hipError_t launch(const PackAttnArgs& a, bool bwd) {
     p.part[1] = (float*)((char*)a.ws + ws_of(a, true).part[0]);
     hipLaunchKernelGGL(attn_packed_f32_dsum_kernel, dim3((unsigned)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units())), dim3(256), 0, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL((attn_packed_f32_bwd_kernel<DH, MANY>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
+    hipLaunchKernelGGL((attn_packed_f32_bwd_kernel<DH, MANY, WIN>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
 // MANY: the kernels that can give a wavefront a quarter of its own, 3 % slower in backward where they do not, only where there are sequences enough for it.
+template <int DH, bool WIN>
+hipError_t run_mask(const PackAttnArgs& a, bool bwd) { return a.sequences * a.nkv > many_strips(DH) ? launch<DH, true, WIN>(a, bwd) : launch<DH, false, WIN>(a, bwd); }
 template <int DH>
-hipError_t run(const PackAttnArgs& a, bool bwd) { return a.sequences * a.nkv > many_strips(DH) ? launch<DH, true>(a, bwd) : launch<DH, false>(a, bwd); }
+hipError_t run(const PackAttnArgs& a, bool bwd) { return a.mask == PACK_WINDOW ? run_mask<DH, true>(a, bwd) : run_mask<DH, false>(a, bwd); }
 }  // namespace
 
 hipError_t attn_packed_f32(const PackAttnArgs& a, bool bwd) {

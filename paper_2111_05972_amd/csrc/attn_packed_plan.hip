@@ -42,25 +42,16 @@ template <bool MAX> __device__ int block_scan(int v, int* tmp, int& total) {
 }
 
 struct PlanParams {
-    int n, M, nq, nkv, causal;
+    int n, M, nq, nkv, mask, window, sinks;
     PackShares shares;
     const int* offsets;
     int* plan;
     PackLayout L;
 };
 
-// Strip `i` of a sequence: its first row or key and its tiles.  Rows are below 2^30.
-__device__ __forceinline__ void strip_of(const PlanParams& p, int side, int len, int i, int& first, int& tile0, int& tile1) {
-    const unsigned G = (unsigned)(p.nq / p.nkv), rows = (unsigned)len * G;
-    first = i * PACK_BLK;
-    if (side == 0) {
-        const unsigned last = min(rows, (unsigned)first + PACK_BLK) - 1;
-        tile0 = 0;
-        tile1 = p.causal ? (int)(last / G) / PACK_TILE + 1 : (len + PACK_TILE - 1) / PACK_TILE;
-    } else {
-        tile0 = p.causal ? (int)((unsigned)first * G / PACK_TILE) : 0;
-        tile1 = (int)((rows + PACK_TILE - 1) / PACK_TILE);
-    }
+// Strip `i` of a sequence: its first row or key and its tiles.
+__device__ __forceinline__ PackTiles strip_of(const PlanParams& p, int side, int len, int i) {
+    return pack_tiles(p.mask, p.window, p.sinks, (unsigned)(p.nq / p.nkv), side, len, i * PACK_BLK);
 }
 // Longest first, `top` above the longest.  Strips of up to LEVEL tiles, which memory bounds and not their length, stay in the order of the
 // rows: sorted, the units would all read the same part of every sequence at a time, and where lengths are equal and even those parts lie on the same channels
@@ -103,7 +94,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                     if (begin[mid] <= m) lo = mid; else hi = mid - 1;
                 }
                 p.plan[m] = (int)m - begin[lo];
-                p.plan[p.L.seen + m] = p.causal ? (int)m - begin[lo] + 1 : begin[lo + 1] - begin[lo];
+                const int at = (int)m - begin[lo];
+                int seen = p.mask != PACK_ALL ? at + 1 : begin[lo + 1] - begin[lo];
+                if (p.mask == PACK_WINDOW) seen = min(seen, p.window) + min(p.sinks, max(0, seen - p.window));
+                p.plan[p.L.seen + m] = seen;
             }
             __syncthreads();
         }
@@ -150,10 +144,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         int most = 0;
         for (int k = t; k < carry[side]; k += PLAN_THREADS) {
             const int b = find(pre, k);
-            int first, t0, t1;
-            strip_of(p, side, start[b + 1] - start[b], k - pre[b], first, t0, t1);
-            mine += (unsigned)(t1 - t0);
-            most = max(most, t1 - t0);
+            const PackTiles s = strip_of(p, side, start[b + 1] - start[b], k - pre[b]);
+            mine += (unsigned)(s.tile1 - s.tile0);
+            most = max(most, s.tile1 - s.tile0);
         }
         if (mine) {
             atomicAdd(&tiles[side], mine);
@@ -175,8 +168,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                 PackItem it{};
                 it.t0 = start[b];
                 it.len = start[b + 1] - start[b];
-                int a, z;
-                strip_of(p, side, it.len, k - pre[b], it.first, a, z);
+                it.first = (k - pre[b]) * PACK_BLK;
+                const PackTiles s = strip_of(p, side, it.len, k - pre[b]);
+                const int a = s.tile0, z = s.tile1;
+                it.skip = s.skip;
                 it.chunks = (z - a + chunk - 1) / chunk;
                 const int each = (z - a + it.chunks - 1) / it.chunks;
                 const int bucket = bucket_of(each, top);
@@ -215,7 +210,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
             h->items[side] = min(hist[side][BUCKETS - 1], (int)p.L.cap[side]);   // the end of the last bucket
             h->joins[side] = min(joins[side], (int)p.L.join_cap[side]);
             h->first_short[side] = min(first_short[side], h->items[side]);
-            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->causal = p.causal; }
+            if (side == 0) { h->sequences = p.n; h->tokens = p.M; h->nq = p.nq; h->nkv = p.nkv; h->mask = p.mask; h->window = p.window; h->sinks = p.sinks; }
         }
     }
 }
@@ -224,9 +219,9 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
 
 size_t attn_packed_workspace_bytes(const PackAttnArgs& a, bool bwd) { return ws_of(a, bwd).total; }
 
-hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int causal, int* plan, hipStream_t s) {
+hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, int nkv, int mask, int window, int sinks, int* plan, hipStream_t s) {
     PlanParams p{};
-    p.n = (int)sequences; p.M = (int)M; p.nq = nq; p.nkv = nkv; p.causal = causal;
+    p.n = (int)sequences; p.M = (int)M; p.nq = nq; p.nkv = nkv; p.mask = mask; p.window = window; p.sinks = sinks;
     p.shares = pack_shares(M, nq, nkv, compute_units());
     p.offsets = offsets; p.plan = plan;
     p.L = pack_layout(sequences, M, nq, nkv, p.shares);

@@ -27,16 +27,19 @@ __device__ __forceinline__ void row_loaded() { asm volatile("s_waitcnt lgkmcnt(0
 // What this wavefront has stored so far is in memory: its next stores to the same places come after it.
 __device__ __forceinline__ void rows_stored() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// Keys as they are: number j is row j.  Another numbering returns the row of number j, or -1 where it is masked and not to be read.
+struct AllKeys { __device__ __forceinline__ int operator()(int j) const { return j; } };
+
 // Forward over keys [jbeg, jend): row maximum m and sum l of the scaled scores' exponentials, and store(d, O[d]), divided by
 // l if normalise.  q_s: the query in LDS.
-template <int NA, typename T, typename Store>
+template <int NA, typename T, typename Store, typename Key = AllKeys>
 __device__ __forceinline__ void attn_row_fwd(const float* q_s, const T* kbase, const T* vbase, int64_t ld, int dh, int jbeg, int jend,
-                                             float scale, bool normalise, int lane, float& m, float& l, Store store) {
+                                             float scale, bool normalise, int lane, float& m, float& l, Store store, Key key = Key()) {
     // pass 1: row maximum and sum of exponentials
     float mx = -INFINITY, sum = 0.0f;
     for (int j0 = jbeg; j0 < jend; j0 += 64) {
-        int j = j0 + lane;
-        if (j < jend) {
+        int j = j0 + lane < jend ? key(j0 + lane) : -1;
+        if (j >= 0) {
             const T* kp = kbase + (int64_t)j * ld;
             float s = 0.0f;
             for (int d = 0; d < dh; ++d) s = fmaf(q_s[d], to_f32(kp[d]), s);
@@ -53,9 +56,9 @@ __device__ __forceinline__ void attn_row_fwd(const float* q_s, const T* kbase, c
     // pass 2: O = sum_j p_j V_j
     float acc[NA] = {};
     for (int j0 = jbeg; j0 < jend; j0 += 64) {
-        int j = j0 + lane;
+        int j = j0 + lane < jend ? key(j0 + lane) : -1;
         float p = 0.0f;
-        if (j < jend) {
+        if (j >= 0) {
             const T* kp = kbase + (int64_t)j * ld;
             float s = 0.0f;
             for (int d = 0; d < dh; ++d) s = fmaf(q_s[d], to_f32(kp[d]), s);
@@ -64,7 +67,9 @@ __device__ __forceinline__ void attn_row_fwd(const float* q_s, const T* kbase, c
         int cnt = min(64, jend - j0);
         for (int jj = 0; jj < cnt; ++jj) {
             float pj = __shfl(p, jj, 64);
-            const T* vp = vbase + (int64_t)(j0 + jj) * ld;
+            const int row = key(j0 + jj);
+            if (row < 0) continue;
+            const T* vp = vbase + (int64_t)row * ld;
 #pragma unroll
             for (int t = 0; t < NA; ++t) {
                 int d = lane + 64 * t;
@@ -81,14 +86,14 @@ __device__ __forceinline__ void attn_row_fwd(const float* q_s, const T* kbase, c
 
 // dQ over keys [jbeg, jend), not scaled: store(d, sum_j dS_j K_j[d]), dS_j = P_j (dO . V_j - D).  q_s, do_s: the rows in LDS;
 // L, D: the row's log-sum-exp and dO . O.
-template <int NA, typename T, typename Store>
+template <int NA, typename T, typename Store, typename Key = AllKeys>
 __device__ __forceinline__ void attn_row_dq(const float* q_s, const float* do_s, const T* kbase, const T* vbase, int64_t ld, int dh,
-                                            int jbeg, int jend, float scale, float L, float D, int lane, Store store) {
+                                            int jbeg, int jend, float scale, float L, float D, int lane, Store store, Key key = Key()) {
     float acc[NA] = {};
     for (int j0 = jbeg; j0 < jend; j0 += 64) {
-        int j = j0 + lane;
+        int j = j0 + lane < jend ? key(j0 + lane) : -1;
         float ds = 0.0f;
-        if (j < jend) {
+        if (j >= 0) {
             const T* kp = kbase + (int64_t)j * ld;
             const T* vp = vbase + (int64_t)j * ld;
             float s = 0.0f, dp = 0.0f;
@@ -101,7 +106,9 @@ __device__ __forceinline__ void attn_row_dq(const float* q_s, const float* do_s,
         int cnt = min(64, jend - j0);
         for (int jj = 0; jj < cnt; ++jj) {
             float dsj = __shfl(ds, jj, 64);
-            const T* kp = kbase + (int64_t)(j0 + jj) * ld;
+            const int row = key(j0 + jj);
+            if (row < 0) continue;
+            const T* kp = kbase + (int64_t)row * ld;
 #pragma unroll
             for (int t = 0; t < NA; ++t) {
                 int d = lane + 64 * t;

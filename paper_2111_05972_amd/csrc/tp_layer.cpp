@@ -952,7 +952,7 @@ int tp_layer_pack_plan(int64_t sequences, int64_t M, const int32_t* offsets, int
     if (!offsets || !plan) return TPL_EINVAL;
     if (((uintptr_t)offsets & 3u) != 0 || misaligned(plan)) return TPL_EALIGN;
     if (plan_bytes < tp_layer_pack_plan_bytes(sequences, M, nq, nkv)) return TPL_EWORKSPACE;
-    return hip_rc(pack_plan(sequences, M, offsets, nq, nkv, causal != 0, (int*)plan, (hipStream_t)hip_stream));
+    return hip_rc(pack_plan(sequences, M, offsets, nq, nkv, causal ? PACK_CAUSAL : PACK_ALL, 0, 0, (int*)plan, (hipStream_t)hip_stream));
 }
 
 static int attn_packed_check(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh) {
@@ -962,43 +962,83 @@ static int attn_packed_check(int dtype, int64_t sequences, int64_t M, int nq, in
     if (rc) return rc;
     return dh <= 128 && dh % 8 == 0 ? TPL_OK : TPL_EUNSUPPORTED;
 }
-static PackAttnArgs attn_packed_args(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal) {
+static PackAttnArgs attn_packed_args(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int mask, int64_t window, int64_t sinks) {
     PackAttnArgs a{};
-    a.dtype = dtype; a.sequences = sequences; a.M = M; a.nq = nq; a.nkv = nkv; a.dh = dh; a.causal = causal != 0;
+    a.dtype = dtype; a.sequences = sequences; a.M = M; a.nq = nq; a.nkv = nkv; a.dh = dh;
+    a.mask = mask; a.window = (int)std::min(window, M); a.sinks = (int)std::min(sinks, M);        // no sequence is longer than the batch
     return a;
+}
+static int attn_packed_mask(int causal) { return causal ? PACK_CAUSAL : PACK_ALL; }
+static size_t attn_packed_ws(const PackAttnArgs& a, int bwd) { return std::max(ALIGN, up(attn_packed_workspace_bytes(a, bwd != 0))); }
+static int attn_packed_fwd_call(PackAttnArgs a, const void* plan, size_t plan_bytes, const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream) {
+    if (!plan || !qkv || !o || !lse || !ws) return TPL_EINVAL;
+    const void* ptrs[] = {plan, qkv, o, lse, ws};
+    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
+    if (plan_bytes < tp_layer_pack_plan_bytes(a.sequences, a.M, a.nq, a.nkv) || ws_bytes < attn_packed_ws(a, 0)) return TPL_EWORKSPACE;
+    a.plan = (const int*)plan; a.qkv = qkv; a.o = o; a.lse = lse; a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(a.dtype == TPL_BF16 ? attn_packed_bf16(a, false) : attn_packed_f32(a, false));
+}
+static int attn_packed_bwd_call(PackAttnArgs a, const void* plan, size_t plan_bytes, const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv,
+                                float* d_scratch, void* ws, size_t ws_bytes, void* hip_stream) {
+    if (!plan || !qkv || !o || !lse || !d_o || !dqkv || !d_scratch || !ws) return TPL_EINVAL;
+    const void* ptrs[] = {plan, qkv, o, lse, d_o, dqkv, d_scratch, ws};
+    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
+    if (plan_bytes < tp_layer_pack_plan_bytes(a.sequences, a.M, a.nq, a.nkv) || ws_bytes < attn_packed_ws(a, 1)) return TPL_EWORKSPACE;
+    a.plan = (const int*)plan; a.qkv = qkv; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse); a.d_o = d_o; a.dqkv = dqkv; a.dsum = d_scratch;
+    a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
+    return hip_rc(a.dtype == TPL_BF16 ? attn_packed_bf16(a, true) : attn_packed_f32(a, true));
 }
 size_t tp_layer_attn_packed_workspace_bytes(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, int bwd) {
     if (attn_packed_check(dtype, sequences, M, nq, nkv, dh)) return 0;
-    return std::max(ALIGN, up(attn_packed_workspace_bytes(attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal), bwd != 0)));
+    return attn_packed_ws(attn_packed_args(dtype, sequences, M, nq, nkv, dh, attn_packed_mask(causal), 0, 0), bwd);
 }
 int tp_layer_attn_packed_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, size_t plan_bytes,
                              const void* qkv, void* o, float* lse,
                              void* ws, size_t ws_bytes, void* hip_stream) {
     const int rc = attn_packed_check(dtype, sequences, M, nq, nkv, dh);
     if (rc) return rc;
-    if (!plan || !qkv || !o || !lse || !ws) return TPL_EINVAL;
-    const void* ptrs[] = {plan, qkv, o, lse, ws};
-    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
-    if (plan_bytes < tp_layer_pack_plan_bytes(sequences, M, nq, nkv) ||
-        ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 0)) return TPL_EWORKSPACE;
-    PackAttnArgs a = attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal);
-    a.plan = (const int*)plan; a.qkv = qkv; a.o = o; a.lse = lse; a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
-    return hip_rc(dtype == TPL_BF16 ? attn_packed_bf16(a, false) : attn_packed_f32(a, false));
+    return attn_packed_fwd_call(attn_packed_args(dtype, sequences, M, nq, nkv, dh, attn_packed_mask(causal), 0, 0), plan, plan_bytes, qkv, o, lse, ws, ws_bytes, hip_stream);
 }
 int tp_layer_attn_packed_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int causal, const void* plan, size_t plan_bytes,
                              const void* qkv, const void* o,
                              const float* lse, const void* d_o, void* dqkv, float* d_scratch, void* ws, size_t ws_bytes, void* hip_stream) {
     const int rc = attn_packed_check(dtype, sequences, M, nq, nkv, dh);
     if (rc) return rc;
-    if (!plan || !qkv || !o || !lse || !d_o || !dqkv || !d_scratch || !ws) return TPL_EINVAL;
-    const void* ptrs[] = {plan, qkv, o, lse, d_o, dqkv, d_scratch, ws};
-    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
-    if (plan_bytes < tp_layer_pack_plan_bytes(sequences, M, nq, nkv) ||
-        ws_bytes < tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causal, 1)) return TPL_EWORKSPACE;
-    PackAttnArgs a = attn_packed_args(dtype, sequences, M, nq, nkv, dh, causal);
-    a.plan = (const int*)plan; a.qkv = qkv; a.o = const_cast<void*>(o); a.lse = const_cast<float*>(lse); a.d_o = d_o; a.dqkv = dqkv; a.dsum = d_scratch;
-    a.ws = ws; a.ws_bytes = ws_bytes; a.stream = (hipStream_t)hip_stream;
-    return hip_rc(dtype == TPL_BF16 ? attn_packed_bf16(a, true) : attn_packed_f32(a, true));
+    return attn_packed_bwd_call(attn_packed_args(dtype, sequences, M, nq, nkv, dh, attn_packed_mask(causal), 0, 0), plan, plan_bytes, qkv, o, lse, d_o, dqkv, d_scratch, ws,
+                                ws_bytes, hip_stream);
+}
+
+// The same with a sliding window and first tokens that stay visible.
+size_t tp_layer_window_plan_bytes(int64_t sequences, int64_t M, int nq, int nkv) { return tp_layer_pack_plan_bytes(sequences, M, nq, nkv); }
+int tp_layer_window_plan(int64_t sequences, int64_t M, const int32_t* offsets, int nq, int nkv, int64_t window, int64_t sinks, void* plan, size_t plan_bytes,
+                         void* hip_stream) {
+    const int rc = pack_check(sequences, M, nq, nkv);
+    if (rc) return rc;
+    if (window <= 0 || sinks < 0 || !offsets || !plan) return TPL_EINVAL;
+    if (((uintptr_t)offsets & 3u) != 0 || misaligned(plan)) return TPL_EALIGN;
+    if (plan_bytes < tp_layer_window_plan_bytes(sequences, M, nq, nkv)) return TPL_EWORKSPACE;
+    return hip_rc(pack_plan(sequences, M, offsets, nq, nkv, PACK_WINDOW, (int)std::min(window, M), (int)std::min(sinks, M), (int*)plan, (hipStream_t)hip_stream));
+}
+static int attn_window_check(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks) {
+    return window <= 0 || sinks < 0 ? TPL_EINVAL : attn_packed_check(dtype, sequences, M, nq, nkv, dh);
+}
+size_t tp_layer_attn_window_workspace_bytes(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks, int bwd) {
+    if (attn_window_check(dtype, sequences, M, nq, nkv, dh, window, sinks)) return 0;
+    return attn_packed_ws(attn_packed_args(dtype, sequences, M, nq, nkv, dh, PACK_WINDOW, window, sinks), bwd);
+}
+int tp_layer_attn_window_fwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks, const void* plan, size_t plan_bytes,
+                             const void* qkv, void* o, float* lse, void* ws, size_t ws_bytes, void* hip_stream) {
+    const int rc = attn_window_check(dtype, sequences, M, nq, nkv, dh, window, sinks);
+    if (rc) return rc;
+    return attn_packed_fwd_call(attn_packed_args(dtype, sequences, M, nq, nkv, dh, PACK_WINDOW, window, sinks), plan, plan_bytes, qkv, o, lse, ws, ws_bytes, hip_stream);
+}
+int tp_layer_attn_window_bwd(int dtype, int64_t sequences, int64_t M, int nq, int nkv, int dh, int64_t window, int64_t sinks, const void* plan, size_t plan_bytes,
+                             const void* qkv, const void* o, const float* lse, const void* d_o, void* dqkv, float* d_scratch, void* ws, size_t ws_bytes,
+                             void* hip_stream) {
+    const int rc = attn_window_check(dtype, sequences, M, nq, nkv, dh, window, sinks);
+    if (rc) return rc;
+    return attn_packed_bwd_call(attn_packed_args(dtype, sequences, M, nq, nkv, dh, PACK_WINDOW, window, sinks), plan, plan_bytes, qkv, o, lse, d_o, dqkv, d_scratch, ws,
+                                ws_bytes, hip_stream);
 }
 
 static int lm_loss_check(int dtype, int64_t M, int64_t H, int64_t V, int64_t first) {
