@@ -235,6 +235,25 @@ size_t tp_layer_slice_epilogue_workspace_bytes(int64_t M, int64_t N);
 int tp_layer_slice_epilogue_bwd(int dtype, int act, int64_t M, int64_t N, const void* dout, const void* u,
                                 void* din, void* dbias, void* ws, size_t ws_bytes, void* hip_stream);
 
+/* Bias, dropout and residual of a slice [M, N], with a mask that is worked out where it is needed and never stored:
+ *   forward : out = keep (in + bias) scale + resid   (bias [N], resid [M, N]: NULL where there is none)
+ *   backward: din = keep dout scale;  dbias = sum_m din, in float, fixed order (NULL: not wanted, and no ws); the gradient of resid is dout itself
+ * The slice is rows first_row .. + M and columns first_col .. + N of a tensor whose rows have `width` elements, and has that tensor's mask: ranks
+ * that hold slices of it, or work on some of its rows at a time, draw what one call over all of it draws.  rng: two 64-bit words in DEVICE memory,
+ * seed and step, so that a captured step draws a new mask whenever its replays find another step there; backward has to find what forward found.
+ * site: number of this dropout within the step (two with the same site, step and seed have the same mask).  Element (r, c) is
+ * number e = (r width + c) % 8 of group g = (r width + c) / 8; Philox4x32-10 (Salmon et al., SC 2011) of the counter (g mod 2^32, g / 2^32 + 4096 site,
+ * step mod 2^32, step / 2^32) and the key (seed mod 2^32, seed / 2^32) gives four words; u = 16 bits of word e / 2, the lower ones where e is even.
+ * keep = u >= t, t = min(65535, floor(65536 p + 1/2)), scale = 65536 / (65536 - t).  What is dropped does not matter, infinities and NaN included.
+ * p in [0, 1).  N, first_col and width multiples of 8, site < 2^20, M and width below 2^31, (first_row + M) width / 8 up to 2^44 (TPL_EUNSUPPORTED: others).
+ * out may be in or resid itself, din may be dout, but they may not overlap otherwise (TPL_EINVAL).  rng 8-byte aligned.
+ * ws_bytes >= tp_layer_dropout_workspace_bytes(M, N). */
+int tp_layer_dropout_fwd(int dtype, int64_t M, int64_t N, double p, const uint64_t* rng, int64_t site, int64_t first_row, int64_t first_col,
+                         int64_t width, const void* in, const void* bias, const void* resid, void* out, void* hip_stream);
+size_t tp_layer_dropout_workspace_bytes(int64_t M, int64_t N);
+int tp_layer_dropout_bwd(int dtype, int64_t M, int64_t N, double p, const uint64_t* rng, int64_t site, int64_t first_row, int64_t first_col,
+                         int64_t width, const void* dout, void* din, void* dbias, void* ws, size_t ws_bytes, void* hip_stream);
+
 /* tp_layer_slice_epilogue_bwd for callers that cannot allocate or pass a workspace (code under HIP graph capture,
  * tight serving loops, harnesses that forbid hipMalloc): the same kernels, with the column-sum partials in a
  * static device array of the library instead of `ws`.  The array is tp_layer_static_scratch_bytes() (4 MiB) per
@@ -316,6 +335,23 @@ int tp_layer_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
                       const int32_t* positions, int64_t seq, const void* qkv, void* out, void* hip_stream);
 int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor,
                       const int32_t* positions, int64_t seq, const void* dqkv, void* out, void* hip_stream);
+
+/* RMS norm of every query and key head, and the rotation above, in one pass: qkv, positions, seq, freq, factor, rot and pairs as there.
+ *   forward : y = turn(x rstd gamma), rstd = 1 / sqrt(mean_dh(x^2) + eps); v is copied
+ *   backward: g = turn back(dqkv); dx = rstd (g gamma - x rstd mean_dh(g gamma x rstd)); dv is copied;  dgamma = sum g x rstd
+ * gamma_q, dgamma_q, gamma_k, dgamma_k (dtype): [dh] for all heads, dgamma the sum over rows and heads; with per_head != 0 [nq, dh] and [nkv, dh], a
+ * row for each head.  Backward takes the qkv of before the norm and works rstd out again.  out may be qkv itself (forward; the input of backward is then gone) or dqkv
+ * itself (backward): then v is not touched; otherwise tensors may not overlap (TPL_EINVAL).  eps >= 0, finite.  Squares are summed in float.  M < 2^24, at most
+ * 4096 heads of a kind, dh a multiple of 8 up to 512 (TPL_EUNSUPPORTED: others).  ws_bytes >= tp_layer_qk_norm_rope_workspace_bytes(...).
+ * Results are deterministic. */
+int tp_layer_qk_norm_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor,
+                              const int32_t* positions, int64_t seq, const void* gamma_q, const void* gamma_k, int per_head, float eps,
+                              const void* qkv, void* out, void* hip_stream);
+size_t tp_layer_qk_norm_rope_workspace_bytes(int dtype, int64_t M, int nq, int nkv, int dh);
+int tp_layer_qk_norm_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor,
+                              const int32_t* positions, int64_t seq, const void* gamma_q, const void* gamma_k, int per_head, float eps,
+                              const void* qkv, const void* dqkv, void* out, void* dgamma_q, void* dgamma_k, void* ws, size_t ws_bytes,
+                              void* hip_stream);
 
 /* Attention of packed sequences with grouped heads.  Sequence b is rows offsets[b] .. offsets[b + 1] - 1 of the [M, ...] tensors
  * (lengths from 0 on); query head h reads key and value head h / (nq / nkv); causal: query i of a sequence sees its keys j <= i, otherwise

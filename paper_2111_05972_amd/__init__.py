@@ -22,6 +22,8 @@ from .binding import (  # noqa: F401
     tp_layer_rope_frequencies, tp_layer_rope_fwd, tp_layer_rope_bwd,
     tp_layer_pack_plan_bytes, tp_layer_pack_plan,
     tp_layer_attn_packed_workspace_bytes, tp_layer_attn_packed_fwd, tp_layer_attn_packed_bwd,
+    tp_layer_qk_norm_rope_fwd, tp_layer_qk_norm_rope_workspace_bytes, tp_layer_qk_norm_rope_bwd,
+    tp_layer_dropout_fwd, tp_layer_dropout_workspace_bytes, tp_layer_dropout_bwd,
     tp_layer_window_plan_bytes, tp_layer_window_plan,
     tp_layer_attn_window_workspace_bytes, tp_layer_attn_window_fwd, tp_layer_attn_window_bwd,
     tp_layer_lm_loss_workspace_bytes, tp_layer_lm_loss_fwd, tp_layer_lm_loss_join, tp_layer_lm_loss_bwd,

@@ -103,6 +103,12 @@ def load_library():
         "tp_layer_rope_frequencies": (ci, [ci, ctypes.c_double, ci, ctypes.c_double, ctypes.c_double, _vp, _vp]),
         "tp_layer_rope_fwd": (ci, [ci, i64, ci, ci, ci, ci, ci, _vp, ctypes.c_float, _vp, i64, _vp, _vp, _vp]),
         "tp_layer_rope_bwd": (ci, [ci, i64, ci, ci, ci, ci, ci, _vp, ctypes.c_float, _vp, i64, _vp, _vp, _vp]),
+        "tp_layer_qk_norm_rope_fwd": (ci, [ci, i64, ci, ci, ci, ci, ci, _vp, ctypes.c_float, _vp, i64, _vp, _vp, ci, ctypes.c_float, _vp, _vp, _vp]),
+        "tp_layer_qk_norm_rope_workspace_bytes": (sz, [ci, i64, ci, ci, ci]),
+        "tp_layer_qk_norm_rope_bwd": (ci, [ci, i64, ci, ci, ci, ci, ci, _vp, ctypes.c_float, _vp, i64, _vp, _vp, ci, ctypes.c_float, _vp, _vp, _vp, _vp, _vp, _vp, sz, _vp]),
+        "tp_layer_dropout_fwd": (ci, [ci, i64, i64, ctypes.c_double, _vp, i64, i64, i64, i64, _vp, _vp, _vp, _vp, _vp]),
+        "tp_layer_dropout_workspace_bytes": (sz, [i64, i64]),
+        "tp_layer_dropout_bwd": (ci, [ci, i64, i64, ctypes.c_double, _vp, i64, i64, i64, i64, _vp, _vp, _vp, _vp, sz, _vp]),
         "tp_layer_pack_plan_bytes": (sz, [i64, i64, ci, ci]),
         "tp_layer_pack_plan": (ci, [i64, i64, _vp, ci, ci, ci, _vp, sz, _vp]),
         "tp_layer_attn_packed_workspace_bytes": (sz, [ci, i64, i64, ci, ci, ci, ci, ci]),
@@ -421,6 +427,41 @@ def tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions
     rc = load_library().tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(dqkv),
                                           _ptr(out), _stream(stream))
     return _checked(rc, "tp_layer_rope_bwd", check)
+
+
+def tp_layer_qk_norm_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, gamma_q, gamma_k, per_head, eps, qkv, out, seq=0,
+                              stream=None, check=True):
+    rc = load_library().tp_layer_qk_norm_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(gamma_q),
+                                                  _ptr(gamma_k), int(bool(per_head)), float(eps), _ptr(qkv), _ptr(out), _stream(stream))
+    return _checked(rc, "tp_layer_qk_norm_rope_fwd", check)
+
+
+def tp_layer_qk_norm_rope_workspace_bytes(dtype, M, nq, nkv, dh):
+    return load_library().tp_layer_qk_norm_rope_workspace_bytes(dtype, M, nq, nkv, dh)
+
+
+def tp_layer_qk_norm_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, gamma_q, gamma_k, per_head, eps, qkv, dqkv, out, dgamma_q,
+                              dgamma_k, ws, ws_bytes=None, seq=0, stream=None, check=True):
+    rc = load_library().tp_layer_qk_norm_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(gamma_q),
+                                                  _ptr(gamma_k), int(bool(per_head)), float(eps), _ptr(qkv), _ptr(dqkv), _ptr(out), _ptr(dgamma_q),
+                                                  _ptr(dgamma_k), _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_qk_norm_rope_bwd", check)
+
+
+def tp_layer_dropout_fwd(dtype, M, N, p, rng, site, first_row, first_col, width, inp, bias, resid, out, stream=None, check=True):
+    rc = load_library().tp_layer_dropout_fwd(dtype, M, N, float(p), _ptr(rng), site, first_row, first_col, width, _ptr(inp), _ptr(bias), _ptr(resid),
+                                             _ptr(out), _stream(stream))
+    return _checked(rc, "tp_layer_dropout_fwd", check)
+
+
+def tp_layer_dropout_workspace_bytes(M, N):
+    return load_library().tp_layer_dropout_workspace_bytes(M, N)
+
+
+def tp_layer_dropout_bwd(dtype, M, N, p, rng, site, first_row, first_col, width, dout, din, dbias=None, ws=None, ws_bytes=None, stream=None, check=True):
+    rc = load_library().tp_layer_dropout_bwd(dtype, M, N, float(p), _ptr(rng), site, first_row, first_col, width, _ptr(dout), _ptr(din), _ptr(dbias),
+                                             _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    return _checked(rc, "tp_layer_dropout_bwd", check)
 
 
 def tp_layer_pack_plan_bytes(sequences, M, nq, nkv):

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libtp_layer.so")
 SOURCES = ["tp_layer.cpp", "simple_kernels.hip", "gemm_bf16.hip", "attn_bf16.hip", "gemm_f32.hip", "attn_f32.hip", "layernorm.hip",
-           "rope.hip", "attn_packed_plan.hip", "attn_packed_bf16.hip", "attn_packed_f32.hip", "lm_loss.hip"]
+           "rope.hip", "qk_norm_rope.hip", "dropout.hip", "attn_packed_plan.hip", "attn_packed_bf16.hip", "attn_packed_f32.hip", "lm_loss.hip"]
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-Wno-option-ignored"]

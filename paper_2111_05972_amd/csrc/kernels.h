@@ -162,6 +162,35 @@ struct RopeArgs {
 };
 hipError_t rope(const RopeArgs& a, bool back);
 
+// Norms of query and key heads and the rotation: see tp_layer_qk_norm_rope_fwd.
+struct QkNormArgs {
+    int dtype;
+    int64_t M, seq;
+    int nq, nkv, dh, rot, adjacent, per_head;
+    const double* freq; float factor, eps;
+    const int* positions;
+    const void* gamma_q; const void* gamma_k;
+    const void* qkv; const void* dqkv; void* out;     // dqkv: bwd
+    void* dgamma_q; void* dgamma_k; void* ws;
+    hipStream_t stream;
+};
+size_t qk_norm_rope_workspace_bytes(int64_t M, int nq, int nkv, int dh);
+hipError_t qk_norm_rope(const QkNormArgs& a, bool bwd);
+
+// Dropout of a slice: see tp_layer_dropout_fwd.  Backward: in is dout, bias and resid are null.
+struct DropoutArgs {
+    int dtype;
+    int64_t M, N;
+    double p;
+    const void* rng;
+    int64_t site, first_row, first_col, width;
+    const void* in; const void* bias; const void* resid; void* out;
+    void* dbias; void* ws;
+    hipStream_t stream;
+};
+size_t dropout_workspace_bytes(int64_t M, int64_t N);
+hipError_t dropout(const DropoutArgs& a);
+
 // Softmax cross entropy of a vocabulary shard: see tp_layer_lm_loss_fwd.
 struct LmLossArgs {
     int dtype;

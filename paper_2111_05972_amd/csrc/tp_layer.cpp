@@ -933,6 +933,96 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
     return rope_call(true, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, dqkv, out, hip_stream);
 }
 
+static bool overlap(const void* a, const void* b, int64_t bytes) {
+    const uintptr_t lo = std::min((uintptr_t)a, (uintptr_t)b), hi = std::max((uintptr_t)a, (uintptr_t)b);
+    return hi - lo < (uintptr_t)bytes;
+}
+static int qk_norm_check(int dtype, int64_t M, int nq, int nkv, int dh) {
+    if (dtype != TPL_F32 && dtype != TPL_BF16) return TPL_EINVAL;
+    if (M <= 0 || nq <= 0 || nkv <= 0 || dh <= 0) return TPL_EINVAL;
+    return M >= (int64_t)1 << 24 || nq > 1 << 12 || nkv > 1 << 12 || dh > 512 || dh % 8 ? TPL_EUNSUPPORTED : TPL_OK;
+}
+static int qk_norm_args(QkNormArgs& a, int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor, const int32_t* positions,
+                        int64_t seq, const void* gamma_q, const void* gamma_k, int per_head, float eps, const void* qkv, void* out, void* hip_stream) {
+    if (rot <= 0 || rot % 2 || rot > dh || (pairs != TPL_ROPE_HALF && pairs != TPL_ROPE_ADJACENT)) return TPL_EINVAL;
+    if (!freq || !gamma_q || !gamma_k || !qkv || !out || (!positions && seq <= 0) || !(eps >= 0.0f) || !std::isfinite(eps)) return TPL_EINVAL;
+    const int rc = qk_norm_check(dtype, M, nq, nkv, dh);
+    if (rc) return rc;
+    const void* ptrs[] = {freq, positions, gamma_q, gamma_k, qkv, out};
+    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
+    a.dtype = dtype; a.M = M; a.seq = seq; a.nq = nq; a.nkv = nkv; a.dh = dh; a.rot = rot; a.adjacent = pairs == TPL_ROPE_ADJACENT; a.per_head = per_head != 0;
+    a.freq = freq; a.factor = factor; a.eps = eps; a.positions = positions; a.gamma_q = gamma_q; a.gamma_k = gamma_k; a.qkv = qkv; a.out = out;
+    a.stream = (hipStream_t)hip_stream;
+    return TPL_OK;
+}
+int tp_layer_qk_norm_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor, const int32_t* positions, int64_t seq,
+                              const void* gamma_q, const void* gamma_k, int per_head, float eps, const void* qkv, void* out, void* hip_stream) {
+    QkNormArgs a{};
+    const int rc = qk_norm_args(a, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, gamma_q, gamma_k, per_head, eps, qkv, out, hip_stream);
+    if (rc) return rc;
+    if (qkv != out && overlap(qkv, out, M * ((int64_t)nq + 2 * nkv) * dh * (dtype == TPL_BF16 ? 2 : 4))) return TPL_EINVAL;
+    return hip_rc(qk_norm_rope(a, false));
+}
+size_t tp_layer_qk_norm_rope_workspace_bytes(int dtype, int64_t M, int nq, int nkv, int dh) {
+    return qk_norm_check(dtype, M, nq, nkv, dh) ? 0 : up(qk_norm_rope_workspace_bytes(M, nq, nkv, dh));
+}
+int tp_layer_qk_norm_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor, const int32_t* positions, int64_t seq,
+                              const void* gamma_q, const void* gamma_k, int per_head, float eps, const void* qkv, const void* dqkv, void* out, void* dgamma_q,
+                              void* dgamma_k, void* ws, size_t ws_bytes, void* hip_stream) {
+    QkNormArgs a{};
+    const int rc = qk_norm_args(a, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, gamma_q, gamma_k, per_head, eps, qkv, out, hip_stream);
+    if (rc) return rc;
+    if (!dqkv || !dgamma_q || !dgamma_k || !ws) return TPL_EINVAL;
+    const void* ptrs[] = {dqkv, dgamma_q, dgamma_k, ws};
+    for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
+    const int64_t bytes = M * ((int64_t)nq + 2 * nkv) * dh * (dtype == TPL_BF16 ? 2 : 4);
+    if ((dqkv != out && overlap(dqkv, out, bytes)) || overlap(qkv, out, bytes)) return TPL_EINVAL;
+    if (ws_bytes < tp_layer_qk_norm_rope_workspace_bytes(dtype, M, nq, nkv, dh)) return TPL_EWORKSPACE;
+    a.dqkv = dqkv; a.dgamma_q = dgamma_q; a.dgamma_k = dgamma_k; a.ws = ws;
+    return hip_rc(qk_norm_rope(a, true));
+}
+
+static int dropout_args(DropoutArgs& a, int dtype, int64_t M, int64_t N, double p, const uint64_t* rng, int64_t site, int64_t first_row, int64_t first_col, int64_t width,
+                        const void* in, void* out, void* hip_stream) {
+    int rc = ew_check(dtype, M, N);
+    if (rc) return rc;
+    if (!(p >= 0.0) || p >= 1.0 || !rng || !in || !out || site < 0 || first_row < 0 || first_col < 0 || width < N || first_col > width - N) return TPL_EINVAL;
+    const int64_t most = (int64_t)1 << 44;                                     // groups of eight elements of the whole tensor
+    if (width % 8 || first_col % 8 || site >= (int64_t)1 << 20 || M >= (int64_t)1 << 31 || width >= (int64_t)1 << 31 || first_row >= most ||
+        first_row + M > most / (width / 8)) return TPL_EUNSUPPORTED;
+    if (misaligned(in) || misaligned(out) || ((uintptr_t)rng & 7u) != 0) return TPL_EALIGN;
+    a.dtype = dtype; a.M = M; a.N = N; a.p = p; a.rng = rng; a.site = site; a.first_row = first_row; a.first_col = first_col; a.width = width;
+    a.in = in; a.out = out; a.stream = (hipStream_t)hip_stream;
+    return TPL_OK;
+}
+int tp_layer_dropout_fwd(int dtype, int64_t M, int64_t N, double p, const uint64_t* rng, int64_t site, int64_t first_row, int64_t first_col, int64_t width,
+                         const void* in, const void* bias, const void* resid, void* out, void* hip_stream) {
+    DropoutArgs a{};
+    const int rc = dropout_args(a, dtype, M, N, p, rng, site, first_row, first_col, width, in, out, hip_stream);
+    if (rc) return rc;
+    if (misaligned(bias) || misaligned(resid)) return TPL_EALIGN;
+    const int64_t bytes = M * N * (dtype == TPL_BF16 ? 2 : 4);
+    if ((in != out && overlap(in, out, bytes)) || (resid && resid != out && overlap(resid, out, bytes))) return TPL_EINVAL;
+    a.bias = bias; a.resid = resid;
+    return hip_rc(dropout(a));
+}
+size_t tp_layer_dropout_workspace_bytes(int64_t M, int64_t N) {
+    if (M <= 0 || N <= 0 || N % 8 || M >= (int64_t)1 << 31 || N >= (int64_t)1 << 31) return 0;
+    return up(dropout_workspace_bytes(M, N));
+}
+int tp_layer_dropout_bwd(int dtype, int64_t M, int64_t N, double p, const uint64_t* rng, int64_t site, int64_t first_row, int64_t first_col, int64_t width,
+                         const void* dout, void* din, void* dbias, void* ws, size_t ws_bytes, void* hip_stream) {
+    DropoutArgs a{};
+    const int rc = dropout_args(a, dtype, M, N, p, rng, site, first_row, first_col, width, dout, din, hip_stream);
+    if (rc) return rc;
+    if (dbias && !ws) return TPL_EINVAL;
+    if (misaligned(dbias) || misaligned(ws)) return TPL_EALIGN;
+    if (dout != din && overlap(dout, din, M * N * (dtype == TPL_BF16 ? 2 : 4))) return TPL_EINVAL;
+    if (dbias && ws_bytes < tp_layer_dropout_workspace_bytes(M, N)) return TPL_EWORKSPACE;
+    a.dbias = dbias; a.ws = ws;
+    return hip_rc(dropout(a));
+}
+
 static int pack_check(int64_t sequences, int64_t M, int nq, int nkv) {
     if (sequences <= 0 || M <= 0 || nq <= 0 || nkv <= 0 || nq % nkv) return TPL_EINVAL;
     const int64_t G = nq / nkv;
