@@ -18,6 +18,7 @@
 namespace tpl {
 namespace {
 
+constexpr int FWD_THREADS = 256, FWD_HEADS = 4;   // heads that a group of lanes takes
 constexpr int MAX_THREADS = 512;
 constexpr int ANGLES = 4096;            // (token, pair) values of a workgroup at most: 32 KiB of LDS
 enum Mode { HALVES = 0, NEIGHBOURS = 1, APART = 2 };     // APART: halves that are not whole units
@@ -36,7 +37,7 @@ struct NormParams {
 
 template <typename T> constexpr int unit() { return 16 / sizeof(T); }
 typedef unsigned raw_t __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void widen(const raw_t& u, float (&v)[8], int at = 0) {
+__device__ __forceinline__ void widen(const raw_t& u, float (&v)[8]) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
 }
@@ -52,6 +53,9 @@ __device__ __forceinline__ raw_t narrow(const float (&v)[8]) {
     return u;
 }
 __device__ __forceinline__ raw_t narrow(const float (&v)[4]) { return raw_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}; }
+
+// The compiler is to widen again what it has widened before: 8 registers of a row kept instead of 16.
+__device__ __forceinline__ void again(raw_t& u) { asm volatile("" : "+v"(u)); }
 
 // Sums over aligned groups of `lanes` lanes (a power of two), in all of them.
 template <int CTRL> __device__ __forceinline__ float add_dpp(float x) { return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)); }
@@ -73,41 +77,35 @@ template <int N> __device__ __forceinline__ void group_sums(float (&v)[N], int l
         for (int j = 0; j < N; ++j) v[j] += __shfl_xor(v[j], d, 64);
 }
 
-template <typename T, int MODE, bool BWD>
-__global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_kernel(NormParams p, const T* x, const T* up, T* out, const T* gamma_q, const T* gamma_k, float* part) {
-    constexpr int E = unit<T>(), AHEAD = BWD ? 2 : 4;
-    extern __shared__ __attribute__((aligned(16))) float2 cs[];                       // [token][angle], then floats
-    const int t = threadIdx.x, threads = blockDim.x, lanes = p.lanes, group = t / lanes, slot = t & (lanes - 1);
-    const int row_lane = group / p.at_once, head_lane = group - row_lane * p.at_once;
-    const int half = p.rot / 2, turning = MODE == HALVES ? half / E : 0;              // slots that turn, HALVES
-    const bool turned = MODE == HALVES && slot < turning;
-    const int a = MODE == HALVES && !turned ? p.rot + (slot - turning) * 2 * E : slot * (turned ? E : 2 * E), b = turned ? a + half : a + E;
-    const bool has_a = row_lane < p.rows_at_once && slot < p.slots, has_b = has_a && b < p.dh;
-    const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.row_heads * p.dh;
-    const int n = (int)(p.M - m0 < p.tokens ? p.M - m0 : p.tokens);
-    float* const lds = reinterpret_cast<float*>(cs + p.chunk * p.angles);
-    float* const mine = lds + group * p.dh;                                            // APART: this group's head
+// Sine and cosine of position * frequency, times the factor.  Whole quarters of a turn are taken off in 64 bits; what is left, an eighth at most, is an
+// angle of 32 bits (off by 2^-24 of at most 0.79) for the Taylor series of both, whose first terms left out are below 2^-29 and 2^-33.
+__device__ __forceinline__ float2 angle(double where, double freq, float factor, float back) {
+    const double quarters = where * freq * 0.63661977236758134308, whole = rint(quarters);
+    const float x = (float)((quarters - whole) * 1.57079632679489661923), z = x * x;
+    const float s = fmaf(x * z, fmaf(z, fmaf(z, fmaf(z, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+    const float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+    const int q = (int)(whole - 4.0 * floor(whole * 0.25));       // 0 .. 3
+    const float cq = q & 1 ? s : c, sq = q & 1 ? c : s;
+    return make_float2((q == 1 || q == 2 ? -cq : cq) * factor, (q >= 2 ? -sq : sq) * factor * back);
+}
 
-    raw_t xr[AHEAD][2], ur[AHEAD][2];
-    const raw_t zero = {0u, 0u, 0u, 0u};
-    auto request = [&](int h, int k0, int end) __attribute__((always_inline)) {
-#pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int k = k0 + j * p.rows_at_once + row_lane;
-            const bool in = k < end && h < p.heads;
-            const int64_t at = (m0 + k) * row + (int64_t)h * p.dh;
-            const bool wanted = in && (!BWD || h < p.normed);
-            xr[j][0] = wanted && has_a ? *reinterpret_cast<const raw_t*>(x + at + a) : zero;
-            xr[j][1] = wanted && has_b ? *reinterpret_cast<const raw_t*>(x + at + b) : zero;
-            if (BWD) {
-                ur[j][0] = in && has_a ? *reinterpret_cast<const raw_t*>(up + at + a) : zero;
-                ur[j][1] = in && has_b ? *reinterpret_cast<const raw_t*>(up + at + b) : zero;
-            }
-        }
-    };
-    // Turns (v0, v1) of the chunk's token k.
-    auto turn = [&](float (&v0)[E], float (&v1)[E], int k) __attribute__((always_inline)) {
-        const float2* w = cs + k * p.angles;
+// What a lane has of a head.
+template <typename T, int MODE>
+struct Slot {
+    static constexpr int E = unit<T>();
+    int number, a, b;                                             // its two units begin at elements a and b
+    bool turned, has_a, has_b;
+    __device__ __forceinline__ Slot(const NormParams& p, int slot) {
+        const int half = p.rot / 2, turning = MODE == HALVES ? half / E : 0;
+        number = slot;
+        turned = MODE == HALVES && slot < turning;
+        a = MODE == HALVES && !turned ? p.rot + (slot - turning) * 2 * E : slot * (turned ? E : 2 * E);
+        b = turned ? a + half : a + E;
+        has_a = slot < p.slots;
+        has_b = has_a && b < p.dh;
+    }
+    // Turns (v0, v1) by the angles at w; APART: through `mine`, the head's place in LDS.
+    __device__ __forceinline__ void turn(const NormParams& p, float (&v0)[E], float (&v1)[E], const float2* w, float* mine) const {
         if constexpr (MODE == HALVES) {
             if (!turned) return;
 #pragma unroll
@@ -136,6 +134,7 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_kernel(NormParams p,
                 if (has_b) mine[b + e] = v1[e];
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            const int half = p.rot / 2;
             auto partner = [&](float& v, int i) {
                 if (i >= p.rot) return;
                 const bool first = i < half;
@@ -148,114 +147,207 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_kernel(NormParams p,
                 if (has_a) partner(v0[e], a + e);
                 if (has_b) partner(v1[e], b + e);
             }
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before the next row is written
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // read before the next head is written
+        }
+    }
+};
+// The angles of tokens m0 .. m0 + n into LDS; past the last pair: as it is.
+__device__ __forceinline__ void angles_of(const NormParams& p, float2* cs, int64_t m0, int n) {
+    for (int i = threadIdx.x; i < n * p.angles; i += blockDim.x) {
+        const int k = i / p.angles, f = i - k * p.angles;
+        const int64_t m = m0 + k;
+        cs[i] = f < p.rot / 2 ? angle(p.pos ? (double)p.pos[m] : (double)(m % p.seq), p.freq[f], p.factor, p.back) : make_float2(1.0f, 0.0f);
+    }
+}
+template <typename T> __device__ __forceinline__ const T* weights_of(const NormParams& p, const T* gamma_q, const T* gamma_k, int h) {
+    return h < p.nq ? gamma_q + (p.per_head ? (int64_t)h * p.dh : 0) : gamma_k + (p.per_head ? (int64_t)(h - p.nq) * p.dh : 0);
+}
+
+// Forward: a group takes every so many heads of its workgroup's rows, AHEAD of them at a time, whose loads are out before the angles are worked out.
+template <typename T, int MODE>
+__global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormParams p, const T* x, T* out, const T* gamma_q, const T* gamma_k) {
+    constexpr int E = unit<T>(), AHEAD = 4;
+    extern __shared__ __attribute__((aligned(16))) float2 cs[];                       // [token][angle], then APART: [group][dh] floats
+    const int group = threadIdx.x / p.lanes, groups = FWD_THREADS / p.lanes;
+    const Slot<T, MODE> s(p, threadIdx.x & (p.lanes - 1));
+    const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.row_heads * p.dh;
+    const int n = (int)(p.M - m0 < p.tokens ? p.M - m0 : p.tokens);
+    float* const mine = reinterpret_cast<float*>(cs + p.tokens * p.angles) + group * p.dh;
+    const int next_token = groups / p.heads, next_head = groups - next_token * p.heads;
+    int token = group / p.heads, head = group - token * p.heads;
+    int tk[AHEAD], hd[AHEAD];
+    raw_t xr[AHEAD][2];
+    auto request = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            tk[j] = token;
+            hd[j] = head;
+            const T* from = x + (m0 + token) * row + (int64_t)head * p.dh;
+            xr[j][0] = xr[j][1] = raw_t{0u, 0u, 0u, 0u};
+            if (token < n) {
+                if (s.has_a) xr[j][0] = *reinterpret_cast<const raw_t*>(from + s.a);
+                if (s.has_b) xr[j][1] = *reinterpret_cast<const raw_t*>(from + s.b);
+            }
+            token += next_token;
+            head += next_head;
+            if (head >= p.heads) { head -= p.heads; ++token; }
         }
     };
-    auto angles = [&](int k0, int end) __attribute__((always_inline)) {
-        for (int i = t; i < (end - k0) * p.angles; i += threads) {
-            const int k = i / p.angles, f = i - k * p.angles;
-            const int64_t m = m0 + k0 + k;
-            float s = 0.0f, c = 1.0f, by = 1.0f;                    // past the last pair: as it is
-            if (f < half) {
-                const double where = p.pos ? (double)p.pos[m] : (double)(m % p.seq);
-                const double turns = where * p.freq[f] * 0.15915494309189533577;     // of a whole circle
-                sincosf((float)((turns - rint(turns)) * 6.28318530717958647692), &s, &c);
-                by = p.factor;
+    request();
+    angles_of(p, cs, m0, n);
+    __syncthreads();
+    while (true) {                                                  // one way for the whole workgroup: the groups' first heads lie in order
+        float r[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            float x0[E], x1[E];
+            widen(xr[j][0], x0);
+            widen(xr[j][1], x1);
+            r[j] = 0.0f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) r[j] = fmaf(x0[e], x0[e], fmaf(x1[e], x1[e], r[j]));
+            again(xr[j][0]);
+            again(xr[j][1]);
+        }
+        group_sums(r, p.lanes);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (tk[j] >= n) continue;
+            raw_t o0 = xr[j][0], o1 = xr[j][1];
+            if (hd[j] < p.normed) {
+                const T* w = weights_of(p, gamma_q, gamma_k, hd[j]);
+                const float rstd = 1.0f / sqrtf(fmaf(r[j], p.inv_dh, p.eps));
+                float x0[E], x1[E], g0[E], g1[E];
+                widen(s.has_a ? *reinterpret_cast<const raw_t*>(w + s.a) : raw_t{0u, 0u, 0u, 0u}, g0);
+                widen(s.has_b ? *reinterpret_cast<const raw_t*>(w + s.b) : raw_t{0u, 0u, 0u, 0u}, g1);
+                widen(xr[j][0], x0);
+                widen(xr[j][1], x1);
+#pragma unroll
+                for (int e = 0; e < E; ++e) {
+                    x0[e] = x0[e] * rstd * g0[e];
+                    x1[e] = x1[e] * rstd * g1[e];
+                }
+                s.turn(p, x0, x1, cs + tk[j] * p.angles, mine);
+                o0 = narrow(x0);
+                o1 = narrow(x1);
             }
-            cs[i] = make_float2(c * by, s * by * p.back);
+            T* to = out + (m0 + tk[j]) * row + (int64_t)hd[j] * p.dh;
+            if (s.has_a) __builtin_nontemporal_store(o0, reinterpret_cast<raw_t*>(to + s.a));
+            if (s.has_b) __builtin_nontemporal_store(o1, reinterpret_cast<raw_t*>(to + s.b));
+        }
+        if (token >= n) break;
+        request();
+    }
+}
+
+// Backward: a group keeps its head over the rows of its workgroup, with gamma and the sums of dgamma in registers.
+template <typename T, int MODE>
+__global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormParams p, const T* x, const T* up, T* out, const T* gamma_q, const T* gamma_k, float* part) {
+    constexpr int E = unit<T>(), AHEAD = 2;
+    extern __shared__ __attribute__((aligned(16))) float2 cs[];                       // [token][angle], then floats
+    const int t = threadIdx.x, threads = blockDim.x, lanes = p.lanes, group = t / lanes;
+    const Slot<T, MODE> s(p, t & (lanes - 1));
+    const int row_lane = group / p.at_once, head_lane = group - row_lane * p.at_once;
+    const bool has_a = s.has_a && row_lane < p.rows_at_once, has_b = s.has_b && row_lane < p.rows_at_once;
+    const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.row_heads * p.dh;
+    const int n = (int)(p.M - m0 < p.tokens ? p.M - m0 : p.tokens);
+    float* const lds = reinterpret_cast<float*>(cs + p.chunk * p.angles);
+    float* const mine = lds + group * p.dh;                                           // APART: this group's head
+
+    raw_t xr[AHEAD][2], ur[AHEAD][2];
+    auto request = [&](int h, int k0, int end) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int k = k0 + j * p.rows_at_once + row_lane;
+            const bool in = k < end && h < p.heads, wanted = in && h < p.normed;
+            const int64_t at = (m0 + k) * row + (int64_t)h * p.dh;
+            xr[j][0] = xr[j][1] = ur[j][0] = ur[j][1] = raw_t{0u, 0u, 0u, 0u};
+            if (wanted && has_a) xr[j][0] = *reinterpret_cast<const raw_t*>(x + at + s.a);
+            if (wanted && has_b) xr[j][1] = *reinterpret_cast<const raw_t*>(x + at + s.b);
+            if (in && has_a) ur[j][0] = *reinterpret_cast<const raw_t*>(up + at + s.a);
+            if (in && has_b) ur[j][1] = *reinterpret_cast<const raw_t*>(up + at + s.b);
         }
     };
     request(head_lane, 0, min(n, p.chunk));
-    angles(0, min(n, p.chunk));
+    angles_of(p, cs, m0, min(n, p.chunk));
     float* const sums = lds;                                        // [2E][threads + 1]: a workgroup's dgamma of a pass
     float* const total = sums + 2 * E * (threads + 1);              // [q, k][dh] of all passes, where weights are shared
-    if (BWD && !p.per_head)
+    if (!p.per_head)
         for (int i = t; i < 2 * p.dh; i += threads) total[i] = 0.0f;
     __syncthreads();
     const int stride = threads + 1, each = p.at_once * lanes;
     for (int h0 = 0; h0 < p.heads; h0 += p.at_once) {
         const int h = h0 + head_lane;
         const bool normed = h < p.normed;
-        float g0[E], g1[E], d0[E], d1[E];
+        raw_t w0 = {0u, 0u, 0u, 0u}, w1 = w0;
+        float d0[E], d1[E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) g0[e] = g1[e] = d0[e] = d1[e] = 0.0f;
+        for (int e = 0; e < E; ++e) d0[e] = d1[e] = 0.0f;
         if (normed) {
-            const T* w = h < p.nq ? gamma_q + (p.per_head ? (int64_t)h * p.dh : 0) : gamma_k + (p.per_head ? (int64_t)(h - p.nq) * p.dh : 0);
-            if (has_a) widen(*reinterpret_cast<const raw_t*>(w + a), g0);
-            if (has_b) widen(*reinterpret_cast<const raw_t*>(w + b), g1);
+            const T* w = weights_of(p, gamma_q, gamma_k, h);
+            if (has_a) w0 = *reinterpret_cast<const raw_t*>(w + s.a);
+            if (has_b) w1 = *reinterpret_cast<const raw_t*>(w + s.b);
         }
         for (int c0 = 0; c0 < n; c0 += p.chunk) {
             const int end = min(n, c0 + p.chunk);
-            if (n > p.chunk && (h0 > 0 || c0 > 0)) {                  // uniform
+            if (n > p.chunk && (h0 > 0 || c0 > 0)) {                // uniform
                 __syncthreads();
-                angles(c0, end);
+                angles_of(p, cs, m0 + c0, end - c0);
                 __syncthreads();
             }
             for (int k0 = c0; k0 < end; k0 += AHEAD * p.rows_at_once) {
                 if (h0 > 0 || k0 > 0) request(h, k0, end);
-                float r1[AHEAD], r2[AHEAD];
-                float v0[AHEAD][E], v1[AHEAD][E];                       // backward: dy turned back
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) {
-                    float x0[E], x1[E];
-                    widen(xr[j][0], x0);
-                    widen(xr[j][1], x1);
-                    r1[j] = 0.0f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) r1[j] = fmaf(x0[e], x0[e], fmaf(x1[e], x1[e], r1[j]));
-                    if constexpr (BWD) {
-                        widen(ur[j][0], v0[j]);
-                        widen(ur[j][1], v1[j]);
-                        turn(v0[j], v1[j], min(k0 + j * p.rows_at_once + row_lane, end - 1) - c0);
-                        r2[j] = 0.0f;
-#pragma unroll
-                        for (int e = 0; e < E; ++e) r2[j] = fmaf(v0[j][e] * g0[e], x0[e], fmaf(v1[j][e] * g1[e], x1[e], r2[j]));
-                    }
-                }
-                group_sums(r1, lanes);
-                if constexpr (BWD) group_sums(r2, lanes);
-#pragma unroll
-                for (int j = 0; j < AHEAD; ++j) {
+                for (int j = 0; j < AHEAD; ++j) {                   // a row after another: two at once do not fit 128 registers
                     const int k = k0 + j * p.rows_at_once + row_lane;
-                    const float rstd = 1.0f / sqrtf(fmaf(r1[j], p.inv_dh, p.eps));
-                    float x0[E], x1[E];
-                    widen(xr[j][0], x0);
-                    widen(xr[j][1], x1);
-                    raw_t o0, o1;
-                    if constexpr (BWD) {
-                        const float c = rstd * r2[j] * p.inv_dh;
-                        float y0[E], y1[E];
+                    float v0[E], v1[E], sum[2] = {0.0f, 0.0f};      // dy turned back; sums of x^2 and g gamma x
+                    widen(ur[j][0], v0);
+                    widen(ur[j][1], v1);
+                    s.turn(p, v0, v1, cs + (min(k, end - 1) - c0) * p.angles, mine);
+                    {
+                        float x[E], g[E];
+                        widen(xr[j][0], x);
+                        widen(w0, g);
 #pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            const float u = x0[e] * rstd, z = x1[e] * rstd;
-                            y0[e] = rstd * fmaf(v0[j][e], g0[e], -u * c);
-                            y1[e] = rstd * fmaf(v1[j][e], g1[e], -z * c);
-                            if (k < end && normed) {
-                                d0[e] = fmaf(v0[j][e], u, d0[e]);
-                                d1[e] = fmaf(v1[j][e], z, d1[e]);
+                        for (int e = 0; e < E; ++e) { sum[0] = fmaf(x[e], x[e], sum[0]); sum[1] = fmaf(v0[e] * g[e], x[e], sum[1]); }
+                        widen(xr[j][1], x);
+                        widen(w1, g);
+#pragma unroll
+                        for (int e = 0; e < E; ++e) { sum[0] = fmaf(x[e], x[e], sum[0]); sum[1] = fmaf(v1[e] * g[e], x[e], sum[1]); }
+                    }
+                    group_sums(sum, lanes);
+                    again(xr[j][0]);
+                    again(xr[j][1]);
+                    again(w0);
+                    again(w1);
+                    raw_t o0 = ur[j][0], o1 = ur[j][1];
+                    if (normed && k < end) {
+                        const float rstd = 1.0f / sqrtf(fmaf(sum[0], p.inv_dh, p.eps)), c = rstd * sum[1] * p.inv_dh;
+                        auto finish = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E], float (&d)[E]) __attribute__((always_inline)) {
+                            float x[E], g[E];
+                            widen(xraw, x);
+                            widen(w, g);
+#pragma unroll
+                            for (int e = 0; e < E; ++e) {
+                                const float u = x[e] * rstd;
+                                d[e] = fmaf(v[e], u, d[e]);
+                                x[e] = rstd * fmaf(v[e], g[e], -u * c);
                             }
-                        }
-                        o0 = normed ? narrow(y0) : ur[j][0];
-                        o1 = normed ? narrow(y1) : ur[j][1];
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < E; ++e) {
-                            x0[e] = x0[e] * rstd * g0[e];
-                            x1[e] = x1[e] * rstd * g1[e];
-                        }
-                        turn(x0, x1, min(k, end - 1) - c0);
-                        o0 = normed ? narrow(x0) : xr[j][0];
-                        o1 = normed ? narrow(x1) : xr[j][1];
+                            return narrow(x);
+                        };
+                        o0 = finish(xr[j][0], w0, v0, d0);
+                        o1 = finish(xr[j][1], w1, v1, d1);
                     }
                     if (k < end && h < p.heads) {
                         T* to = out + (m0 + k) * row + (int64_t)h * p.dh;
-                        if (has_a) __builtin_nontemporal_store(o0, reinterpret_cast<raw_t*>(to + a));
-                        if (has_b) __builtin_nontemporal_store(o1, reinterpret_cast<raw_t*>(to + b));
+                        if (has_a) __builtin_nontemporal_store(o0, reinterpret_cast<raw_t*>(to + s.a));
+                        if (has_b) __builtin_nontemporal_store(o1, reinterpret_cast<raw_t*>(to + s.b));
                     }
+                    __builtin_amdgcn_sched_barrier(0);
                 }
             }
         }
-        if constexpr (!BWD) continue;
         if (h0 >= p.normed) continue;                               // uniform: v alone
         __syncthreads();                                            // the sums of the pass before have been read, and the heads of APART
 #pragma unroll
@@ -264,50 +356,56 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_kernel(NormParams p,
             sums[(E + e) * stride + t] = d1[e];
         }
         __syncthreads();
-        auto place = [&](int s, int e) {                            // element of the head that is number e of slot s
-            const bool tu = MODE == HALVES && s < turning;
-            const int first = MODE == HALVES && !tu ? p.rot + (s - turning) * 2 * E : s * (tu ? E : 2 * E);
-            return e < E ? first + e : tu ? first + half + e - E : first + e;
+        auto place = [&](int slot, int e) {                         // element of the head that is number e of the slot
+            const Slot<T, MODE> o(p, slot);
+            return e < E ? o.a + e : o.b + e - E;
         };
         if (p.per_head) {
             for (int i = t; i < each * 2 * E; i += threads) {
-                const int e = i % (2 * E), at = i / (2 * E), s = at & (lanes - 1), head = h0 + at / lanes, el = place(s, e);
-                if (s >= p.slots || head >= p.normed || el >= p.dh) continue;
+                const int e = i % (2 * E), at = i / (2 * E), slot = at & (lanes - 1), head = h0 + at / lanes, el = place(slot, e);
+                if (slot >= p.slots || head >= p.normed || el >= p.dh) continue;
                 float v = sums[e * stride + at];
                 for (int r = 1; r < p.rows_at_once; ++r) v += sums[e * stride + r * each + at];
                 part[((int64_t)blockIdx.x * p.normed + head) * p.dh + el] = v;
             }
         } else {
             for (int i = t; i < 2 * lanes * 2 * E; i += threads) {
-                const int e = i % (2 * E), s = i / (2 * E) & (lanes - 1), side = i / (2 * E * lanes), el = place(s, e);
-                if (s >= p.slots || el >= p.dh) continue;
+                const int e = i % (2 * E), slot = i / (2 * E) & (lanes - 1), side = i / (2 * E * lanes), el = place(slot, e);
+                if (slot >= p.slots || el >= p.dh) continue;
                 const int from = max(side ? p.nq - h0 : 0, 0), to = min((side ? p.normed : p.nq) - h0, p.at_once);
                 float v = total[side * p.dh + el];
                 for (int r = 0; r < p.rows_at_once; ++r)
-                    for (int g = from; g < to; ++g) v += sums[e * stride + r * each + g * lanes + s];
+                    for (int g = from; g < to; ++g) v += sums[e * stride + r * each + g * lanes + slot];
                 total[side * p.dh + el] = v;                        // this thread's alone
             }
         }
         if (MODE == APART) __syncthreads();                         // heads go where the sums were
     }
-    if (BWD && !p.per_head) {
+    if (!p.per_head) {
         __syncthreads();
         for (int i = t; i < 2 * p.dh; i += threads) part[(int64_t)blockIdx.x * 2 * p.dh + i] = total[i];
     }
 }
 
 // Workgroups of backward, each of which leaves sums: two to a compute unit at most.
-int64_t tokens_each(int64_t M, bool bwd) { const int64_t groups = (bwd ? 2 : 4) * (int64_t)compute_units(); return (M + groups - 1) / groups; }
+int64_t tokens_each(int64_t M) { const int64_t groups = 2 * (int64_t)compute_units(); return (M + groups - 1) / groups; }
 
 template <typename T, int MODE>
-hipError_t launch(const QkNormArgs& a, NormParams& p, bool bwd) {
+hipError_t launch_fwd(const QkNormArgs& a, NormParams& p) {
+    // heads of a group: one batch, fewer where units would be left without rows
+    const int groups = FWD_THREADS / p.lanes;
+    const int64_t most = std::max(1, FWD_HEADS * groups / p.heads), spread = (a.M + 4 * compute_units() - 1) / (4 * compute_units());
+    p.tokens = (int)std::min<int64_t>(std::min(most, spread), std::max(1, ANGLES / p.angles));
+    const size_t lds = (size_t)p.tokens * p.angles * sizeof(float2) + (MODE == APART ? (size_t)groups * a.dh * sizeof(float) : 0);
+    hipLaunchKernelGGL((qk_norm_rope_fwd_kernel<T, MODE>), dim3((unsigned)((a.M + p.tokens - 1) / p.tokens)), dim3(FWD_THREADS), lds, a.stream, p, (const T*)a.qkv,
+                       (T*)a.out, (const T*)a.gamma_q, (const T*)a.gamma_k);
+    return hipGetLastError();
+}
+template <typename T, int MODE>
+hipError_t launch_bwd(const QkNormArgs& a, NormParams& p) {
     constexpr int E = unit<T>();
-    const int turning = MODE == HALVES ? a.rot / 2 / E : 0;
-    p.slots = MODE == HALVES ? turning + ((a.dh - a.rot) / E + 1) / 2 : (a.dh + 2 * E - 1) / (2 * E);
-    for (p.lanes = 1; p.lanes < p.slots; p.lanes *= 2) {}
-    p.angles = MODE == NEIGHBOURS ? p.slots * E : a.rot / 2;
     // Threads, heads at a time and rows at a time that leave the fewest groups idle; fewer passes over the heads where that is alike.
-    const int64_t spread = tokens_each(a.M, bwd);
+    const int64_t spread = tokens_each(a.M);
     int threads = 0;
     double best = 0.0;
     for (int passes = 1; passes <= p.heads; ++passes) {
@@ -315,35 +413,36 @@ hipError_t launch(const QkNormArgs& a, NormParams& p, bool bwd) {
         if (passes > 1 && at_once == (p.heads + passes - 2) / (passes - 1)) continue;
         if (at_once * p.lanes > MAX_THREADS) continue;
         for (int th = 64; th <= MAX_THREADS; th += 64) {
-            const int groups = th / p.lanes, rows = (int)std::min<int64_t>(groups / std::max(1, at_once), spread);
+            const int groups = th / p.lanes, rows = (int)std::min<int64_t>(groups / at_once, spread);
             if (rows < 1) continue;
             const double full = (double)p.heads * rows / ((double)passes * groups) * (th >= 256 ? 1.0 : 0.9) - 0.01 * passes;
             if (full > best) { best = full; threads = th; p.at_once = at_once; p.rows_at_once = rows; }
         }
         if (at_once * p.lanes <= 64) break;
     }
+    // no more workgroups than the workspace has rows for, whose angles come in chunks
     const int64_t fits = std::max(1, ANGLES / p.angles), step = p.rows_at_once;
-    // Backward: no more workgroups than the workspace has rows for, whose angles come in chunks.
     p.tokens = (int)((spread + step - 1) / step * step);
     p.chunk = (int)std::min<int64_t>(p.tokens, fits >= step ? fits / step * step : fits);
-    if (!bwd) p.tokens = p.chunk;
     const dim3 grid((unsigned)((a.M + p.tokens - 1) / p.tokens));
-    const size_t angles = (size_t)p.chunk * p.angles * sizeof(float2);
-    const size_t apart = MODE == APART ? (size_t)(threads / p.lanes) * a.dh * sizeof(float) : 0;
-    const size_t sums = bwd ? (size_t)(2 * E * (threads + 1) + 2 * a.dh) * sizeof(float) : 0;
-    const size_t lds = angles + std::max(apart, sums);
-    const T *x = (const T*)a.qkv, *up = (const T*)a.dqkv, *gq = (const T*)a.gamma_q, *gk = (const T*)a.gamma_k;
-    if (!bwd) {
-        hipLaunchKernelGGL((qk_norm_rope_kernel<T, MODE, false>), grid, dim3((unsigned)threads), lds, a.stream, p, x, up, (T*)a.out, gq, gk, nullptr);
-        return hipGetLastError();
-    }
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&qk_norm_rope_kernel<T, MODE, true>), hipFuncAttributeMaxDynamicSharedMemorySize, 160 << 10);
+    const size_t apart = MODE == APART ? (size_t)(threads / p.lanes) * a.dh * sizeof(float) : 0, sums = (size_t)(2 * E * (threads + 1) + 2 * a.dh) * sizeof(float);
+    const size_t lds = (size_t)p.chunk * p.angles * sizeof(float2) + std::max(apart, sums);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&qk_norm_rope_bwd_kernel<T, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 << 10);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, MODE, true>), grid, dim3((unsigned)threads), lds, a.stream, p, x, up, (T*)a.out, gq, gk, (float*)a.ws);
+    hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, MODE>), grid, dim3((unsigned)threads), lds, a.stream, p, (const T*)a.qkv, (const T*)a.dqkv, (T*)a.out,
+                       (const T*)a.gamma_q, (const T*)a.gamma_k, (float*)a.ws);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t cols = (a.per_head ? p.normed : 2) * (int64_t)a.dh;
     return row_sums<T>(grid.x, cols, (a.per_head ? a.nq : 1) * (int64_t)a.dh, (const float*)a.ws, a.dgamma_q, a.dgamma_k, a.stream);
+}
+template <typename T, int MODE>
+hipError_t launch(const QkNormArgs& a, NormParams& p, bool bwd) {
+    constexpr int E = unit<T>();
+    p.slots = MODE == HALVES ? a.rot / 2 / E + ((a.dh - a.rot) / E + 1) / 2 : (a.dh + 2 * E - 1) / (2 * E);
+    for (p.lanes = 1; p.lanes < p.slots; p.lanes *= 2) {}
+    p.angles = MODE == NEIGHBOURS ? p.slots * E : a.rot / 2;
+    return bwd ? launch_bwd<T, MODE>(a, p) : launch_fwd<T, MODE>(a, p);
 }
 template <typename T>
 hipError_t run(const QkNormArgs& a, NormParams& p, bool bwd) {
@@ -353,7 +452,7 @@ hipError_t run(const QkNormArgs& a, NormParams& p, bool bwd) {
 }  // namespace
 
 size_t qk_norm_rope_workspace_bytes(int64_t M, int nq, int nkv, int dh) {
-    const int64_t each = tokens_each(M, true);
+    const int64_t each = tokens_each(M);
     return (size_t)((M + each - 1) / each) * ((size_t)nq + nkv) * dh * sizeof(float);
 }
 hipError_t qk_norm_rope(const QkNormArgs& a, bool bwd) {
