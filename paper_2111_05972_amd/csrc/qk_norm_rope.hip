@@ -243,8 +243,8 @@ __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormPa
 
 // Backward: a group keeps its head over the rows of its workgroup, with gamma and the sums of dgamma in registers.
 template <typename T, int MODE>
-__global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormParams p, const T* x, const T* up, T* out, const T* gamma_q, const T* gamma_k, float* part) {
-    constexpr int E = unit<T>(), AHEAD = 2;
+__global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParams p, const T* x, const T* up, T* out, const T* gamma_q, const T* gamma_k, float* part) {
+    constexpr int E = unit<T>();
     extern __shared__ __attribute__((aligned(16))) float2 cs[];                       // [token][angle], then floats
     const int t = threadIdx.x, threads = blockDim.x, lanes = p.lanes, group = t / lanes;
     const Slot<T, MODE> s(p, t & (lanes - 1));
@@ -252,38 +252,46 @@ __global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormPa
     const bool has_a = s.has_a && row_lane < p.rows_at_once, has_b = s.has_b && row_lane < p.rows_at_once;
     const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.row_heads * p.dh;
     const int n = (int)(p.M - m0 < p.tokens ? p.M - m0 : p.tokens);
-    float* const lds = reinterpret_cast<float*>(cs + p.chunk * p.angles);
-    float* const mine = lds + group * p.dh;                                           // APART: this group's head
-
-    raw_t xr[AHEAD][2], ur[AHEAD][2];
-    auto request = [&](int h, int k0, int end) __attribute__((always_inline)) {
+    // sums of dgamma, [2E][threads + 1]: of a pass (per_head), or of all of them, q, then k (where APART has its heads until then)
+    float* const sums = reinterpret_cast<float*>(cs + p.chunk * p.angles);
+    const int stride = threads + 1, each = p.at_once * lanes;
+    float* const sums_k = sums + 2 * E * stride;
+    float* const mine = sums_k + group * p.dh;                                        // APART: this group's head
+    struct Raw { raw_t x[2], up[2]; };
+    Raw one;
+    auto request = [&](Raw& r, int h, int k, int end) __attribute__((always_inline)) {
+        const bool in = k < end && h < p.heads, wanted = in && h < p.normed;
+        const int64_t at = (m0 + k) * row + (int64_t)h * p.dh;
+        r.x[0] = r.x[1] = r.up[0] = r.up[1] = raw_t{0u, 0u, 0u, 0u};
+        if (wanted && has_a) r.x[0] = *reinterpret_cast<const raw_t*>(x + at + s.a);
+        if (wanted && has_b) r.x[1] = *reinterpret_cast<const raw_t*>(x + at + s.b);
+        if (in && has_a) r.up[0] = *reinterpret_cast<const raw_t*>(up + at + s.a);
+        if (in && has_b) r.up[1] = *reinterpret_cast<const raw_t*>(up + at + s.b);
+    };
+    request(one, head_lane, row_lane, min(n, p.chunk));
+    angles_of(p, cs, m0, min(n, p.chunk));
+    float d0[E], d1[E];
+    auto leave = [&](float* to) __attribute__((always_inline)) {    // this thread's sums, and begin again
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int k = k0 + j * p.rows_at_once + row_lane;
-            const bool in = k < end && h < p.heads, wanted = in && h < p.normed;
-            const int64_t at = (m0 + k) * row + (int64_t)h * p.dh;
-            xr[j][0] = xr[j][1] = ur[j][0] = ur[j][1] = raw_t{0u, 0u, 0u, 0u};
-            if (wanted && has_a) xr[j][0] = *reinterpret_cast<const raw_t*>(x + at + s.a);
-            if (wanted && has_b) xr[j][1] = *reinterpret_cast<const raw_t*>(x + at + s.b);
-            if (in && has_a) ur[j][0] = *reinterpret_cast<const raw_t*>(up + at + s.a);
-            if (in && has_b) ur[j][1] = *reinterpret_cast<const raw_t*>(up + at + s.b);
+        for (int e = 0; e < E; ++e) {
+            to[e * stride + t] = d0[e];
+            to[(E + e) * stride + t] = d1[e];
+            d0[e] = d1[e] = 0.0f;
         }
     };
-    request(head_lane, 0, min(n, p.chunk));
-    angles_of(p, cs, m0, min(n, p.chunk));
-    float* const sums = lds;                                        // [2E][threads + 1]: a workgroup's dgamma of a pass
-    float* const total = sums + 2 * E * (threads + 1);              // [q, k][dh] of all passes, where weights are shared
-    if (!p.per_head)
-        for (int i = t; i < 2 * p.dh; i += threads) total[i] = 0.0f;
+#pragma unroll
+    for (int e = 0; e < E; ++e) d0[e] = d1[e] = 0.0f;
+    auto place = [&](int slot, int e) {                             // element of the head that is number e of the slot
+        const Slot<T, MODE> o(p, slot);
+        return e < E ? o.a + e : o.b + e - E;
+    };
+    bool left = false;
     __syncthreads();
-    const int stride = threads + 1, each = p.at_once * lanes;
     for (int h0 = 0; h0 < p.heads; h0 += p.at_once) {
         const int h = h0 + head_lane;
         const bool normed = h < p.normed;
         raw_t w0 = {0u, 0u, 0u, 0u}, w1 = w0;
-        float d0[E], d1[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) d0[e] = d1[e] = 0.0f;
+        if (!p.per_head && h >= p.nq && !left) { leave(sums); left = true; }
         if (normed) {
             const T* w = weights_of(p, gamma_q, gamma_k, h);
             if (has_a) w0 = *reinterpret_cast<const raw_t*>(w + s.a);
@@ -296,94 +304,79 @@ __global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormPa
                 angles_of(p, cs, m0 + c0, end - c0);
                 __syncthreads();
             }
-            for (int k0 = c0; k0 < end; k0 += AHEAD * p.rows_at_once) {
-                if (h0 > 0 || k0 > 0) request(h, k0, end);
+            auto work = [&](Raw& r, int k) __attribute__((always_inline)) {
+                float v0[E], v1[E], sum[2] = {0.0f, 0.0f};          // dy turned back; sums of x^2 and g gamma x
+                widen(r.up[0], v0);
+                widen(r.up[1], v1);
+                s.turn(p, v0, v1, cs + (min(k, end - 1) - c0) * p.angles, mine);
+                auto add = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E]) __attribute__((always_inline)) {
+                    float x[E], g[E];
+                    widen(xraw, x);
+                    widen(w, g);
 #pragma unroll
-                for (int j = 0; j < AHEAD; ++j) {                   // a row after another: two at once do not fit 128 registers
-                    const int k = k0 + j * p.rows_at_once + row_lane;
-                    float v0[E], v1[E], sum[2] = {0.0f, 0.0f};      // dy turned back; sums of x^2 and g gamma x
-                    widen(ur[j][0], v0);
-                    widen(ur[j][1], v1);
-                    s.turn(p, v0, v1, cs + (min(k, end - 1) - c0) * p.angles, mine);
-                    {
+                    for (int e = 0; e < E; ++e) { sum[0] = fmaf(x[e], x[e], sum[0]); sum[1] = fmaf(v[e] * g[e], x[e], sum[1]); }
+                };
+                add(r.x[0], w0, v0);
+                add(r.x[1], w1, v1);
+                group_sums(sum, lanes);
+                again(r.x[0]);
+                again(r.x[1]);
+                again(w0);
+                again(w1);
+                raw_t o0 = r.up[0], o1 = r.up[1];
+                if (normed && k < end) {
+                    const float rstd = 1.0f / sqrtf(fmaf(sum[0], p.inv_dh, p.eps)), c = rstd * sum[1] * p.inv_dh;
+                    auto finish = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E], float (&d)[E]) __attribute__((always_inline)) {
                         float x[E], g[E];
-                        widen(xr[j][0], x);
-                        widen(w0, g);
+                        widen(xraw, x);
+                        widen(w, g);
 #pragma unroll
-                        for (int e = 0; e < E; ++e) { sum[0] = fmaf(x[e], x[e], sum[0]); sum[1] = fmaf(v0[e] * g[e], x[e], sum[1]); }
-                        widen(xr[j][1], x);
-                        widen(w1, g);
-#pragma unroll
-                        for (int e = 0; e < E; ++e) { sum[0] = fmaf(x[e], x[e], sum[0]); sum[1] = fmaf(v1[e] * g[e], x[e], sum[1]); }
-                    }
-                    group_sums(sum, lanes);
-                    again(xr[j][0]);
-                    again(xr[j][1]);
-                    again(w0);
-                    again(w1);
-                    raw_t o0 = ur[j][0], o1 = ur[j][1];
-                    if (normed && k < end) {
-                        const float rstd = 1.0f / sqrtf(fmaf(sum[0], p.inv_dh, p.eps)), c = rstd * sum[1] * p.inv_dh;
-                        auto finish = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E], float (&d)[E]) __attribute__((always_inline)) {
-                            float x[E], g[E];
-                            widen(xraw, x);
-                            widen(w, g);
-#pragma unroll
-                            for (int e = 0; e < E; ++e) {
-                                const float u = x[e] * rstd;
-                                d[e] = fmaf(v[e], u, d[e]);
-                                x[e] = rstd * fmaf(v[e], g[e], -u * c);
-                            }
-                            return narrow(x);
-                        };
-                        o0 = finish(xr[j][0], w0, v0, d0);
-                        o1 = finish(xr[j][1], w1, v1, d1);
-                    }
-                    if (k < end && h < p.heads) {
-                        T* to = out + (m0 + k) * row + (int64_t)h * p.dh;
-                        if (has_a) __builtin_nontemporal_store(o0, reinterpret_cast<raw_t*>(to + s.a));
-                        if (has_b) __builtin_nontemporal_store(o1, reinterpret_cast<raw_t*>(to + s.b));
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                        for (int e = 0; e < E; ++e) {
+                            const float u = x[e] * rstd;
+                            d[e] = fmaf(v[e], u, d[e]);
+                            x[e] = rstd * fmaf(v[e], g[e], -u * c);
+                        }
+                        return narrow(x);
+                    };
+                    o0 = finish(r.x[0], w0, v0, d0);
+                    o1 = finish(r.x[1], w1, v1, d1);
                 }
+                if (k < end && h < p.heads) {
+                    T* to = out + (m0 + k) * row + (int64_t)h * p.dh;
+                    if (has_a) __builtin_nontemporal_store(o0, reinterpret_cast<raw_t*>(to + s.a));
+                    if (has_b) __builtin_nontemporal_store(o1, reinterpret_cast<raw_t*>(to + s.b));
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            for (int k = c0 + row_lane; k - row_lane < end; k += p.rows_at_once) {     // uniform
+                if (h0 > 0 || k > row_lane) request(one, h, k, end);
+                work(one, k);
             }
         }
-        if (h0 >= p.normed) continue;                               // uniform: v alone
-        __syncthreads();                                            // the sums of the pass before have been read, and the heads of APART
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            sums[e * stride + t] = d0[e];
-            sums[(E + e) * stride + t] = d1[e];
+        if (!p.per_head || h0 >= p.normed) continue;                // uniform
+        leave(sums);
+        __syncthreads();
+        for (int i = t; i < each * 2 * E; i += threads) {
+            const int e = i % (2 * E), at = i / (2 * E), slot = at & (lanes - 1), head = h0 + at / lanes, el = place(slot, e);
+            if (slot >= p.slots || head >= p.normed || el >= p.dh) continue;
+            float v = sums[e * stride + at];
+            for (int r = 1; r < p.rows_at_once; ++r) v += sums[e * stride + r * each + at];
+            part[((int64_t)blockIdx.x * p.normed + head) * p.dh + el] = v;
         }
         __syncthreads();
-        auto place = [&](int slot, int e) {                         // element of the head that is number e of the slot
-            const Slot<T, MODE> o(p, slot);
-            return e < E ? o.a + e : o.b + e - E;
-        };
-        if (p.per_head) {
-            for (int i = t; i < each * 2 * E; i += threads) {
-                const int e = i % (2 * E), at = i / (2 * E), slot = at & (lanes - 1), head = h0 + at / lanes, el = place(slot, e);
-                if (slot >= p.slots || head >= p.normed || el >= p.dh) continue;
-                float v = sums[e * stride + at];
-                for (int r = 1; r < p.rows_at_once; ++r) v += sums[e * stride + r * each + at];
-                part[((int64_t)blockIdx.x * p.normed + head) * p.dh + el] = v;
-            }
-        } else {
-            for (int i = t; i < 2 * lanes * 2 * E; i += threads) {
-                const int e = i % (2 * E), slot = i / (2 * E) & (lanes - 1), side = i / (2 * E * lanes), el = place(slot, e);
-                if (slot >= p.slots || el >= p.dh) continue;
-                const int from = max(side ? p.nq - h0 : 0, 0), to = min((side ? p.normed : p.nq) - h0, p.at_once);
-                float v = total[side * p.dh + el];
-                for (int r = 0; r < p.rows_at_once; ++r)
-                    for (int g = from; g < to; ++g) v += sums[e * stride + r * each + g * lanes + slot];
-                total[side * p.dh + el] = v;                        // this thread's alone
-            }
-        }
-        if (MODE == APART) __syncthreads();                         // heads go where the sums were
     }
-    if (!p.per_head) {
-        __syncthreads();
-        for (int i = t; i < 2 * p.dh; i += threads) part[(int64_t)blockIdx.x * 2 * p.dh + i] = total[i];
+    if (p.per_head) return;
+    if (MODE == APART) __syncthreads();                             // all heads have been read
+    if (left) leave(sums_k);
+    else { leave(sums); leave(sums_k); }
+    __syncthreads();
+    for (int i = t; i < 2 * lanes * 2 * E; i += threads) {
+        const int e = i % (2 * E), slot = i / (2 * E) & (lanes - 1), side = i / (2 * E * lanes), el = place(slot, e);
+        if (slot >= p.slots || el >= p.dh) continue;
+        const float* from = (side ? sums_k : sums) + e * stride + slot;
+        float v = 0.0f;
+        for (int g = 0; g < p.rows_at_once * p.at_once; ++g) v += from[g * lanes];
+        part[((int64_t)blockIdx.x * 2 + side) * p.dh + el] = v;
     }
 }
 
@@ -404,19 +397,20 @@ hipError_t launch_fwd(const QkNormArgs& a, NormParams& p) {
 template <typename T, int MODE>
 hipError_t launch_bwd(const QkNormArgs& a, NormParams& p) {
     constexpr int E = unit<T>();
-    // Threads, heads at a time and rows at a time that leave the fewest groups idle; fewer passes over the heads where that is alike.
+    // Threads, heads at a time and rows at a time: as many lanes at work as there may be, and few rows more than two workgroups to a unit leave each.
+    // A third of the lanes idle costs 6 % (8192 tokens, 32 + 2 x 8 heads of 128: 62 -> 58 us with 512 instead of 384 threads), a quarter more rows a quarter (12 + 2 x 12 heads: 39 -> 48).
     const int64_t spread = tokens_each(a.M);
     int threads = 0;
-    double best = 0.0;
+    double best = 1e30;
     for (int passes = 1; passes <= p.heads; ++passes) {
         const int at_once = (p.heads + passes - 1) / passes;
         if (passes > 1 && at_once == (p.heads + passes - 2) / (passes - 1)) continue;
         if (at_once * p.lanes > MAX_THREADS) continue;
-        for (int th = 64; th <= MAX_THREADS; th += 64) {
-            const int groups = th / p.lanes, rows = (int)std::min<int64_t>(groups / at_once, spread);
-            if (rows < 1) continue;
-            const double full = (double)p.heads * rows / ((double)passes * groups) * (th >= 256 ? 1.0 : 0.9) - 0.01 * passes;
-            if (full > best) { best = full; threads = th; p.at_once = at_once; p.rows_at_once = rows; }
+        const int64_t most = std::min<int64_t>(MAX_THREADS / p.lanes / at_once, spread);
+        for (int64_t rows = 1; rows <= most; ++rows) {
+            const double active = (double)p.heads * rows * p.lanes / passes, more = (double)((spread + rows - 1) / rows * rows) / spread;
+            const double cost = more * (1.0 + 0.2 * (MAX_THREADS / active - 1.0)) + 0.01 * passes;
+            if (cost < best) { best = cost; threads = (int)(at_once * rows * p.lanes + 63) / 64 * 64; p.at_once = at_once; p.rows_at_once = (int)rows; }
         }
         if (at_once * p.lanes <= 64) break;
     }
@@ -425,9 +419,9 @@ hipError_t launch_bwd(const QkNormArgs& a, NormParams& p) {
     p.tokens = (int)((spread + step - 1) / step * step);
     p.chunk = (int)std::min<int64_t>(p.tokens, fits >= step ? fits / step * step : fits);
     const dim3 grid((unsigned)((a.M + p.tokens - 1) / p.tokens));
-    const size_t apart = MODE == APART ? (size_t)(threads / p.lanes) * a.dh * sizeof(float) : 0, sums = (size_t)(2 * E * (threads + 1) + 2 * a.dh) * sizeof(float);
-    const size_t lds = (size_t)p.chunk * p.angles * sizeof(float2) + std::max(apart, sums);
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&qk_norm_rope_bwd_kernel<T, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, 80 << 10);
+    const size_t apart = MODE == APART ? (size_t)(threads / p.lanes) * a.dh * sizeof(float) : 0, sums = (size_t)(2 * E * (threads + 1)) * sizeof(float);
+    const size_t lds = (size_t)p.chunk * p.angles * sizeof(float2) + sums + std::max(apart, a.per_head ? 0 : sums);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&qk_norm_rope_bwd_kernel<T, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, 112 << 10);
     if (attr != hipSuccess) return attr;
     hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, MODE>), grid, dim3((unsigned)threads), lds, a.stream, p, (const T*)a.qkv, (const T*)a.dqkv, (T*)a.out,
                        (const T*)a.gamma_q, (const T*)a.gamma_k, (float*)a.ws);
