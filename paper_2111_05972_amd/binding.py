@@ -138,9 +138,10 @@ def load_library():
 def _ptr(x):
     if x is None:
         return None
-    if hasattr(x, "data_ptr"):
+    try:
         return x.data_ptr()
-    return int(x)
+    except AttributeError:
+        return int(x)
 
 
 def _nbytes(x):

@@ -78,6 +78,21 @@ inline PackShares pack_shares(int64_t M, int64_t nq, int64_t nkv, int units) {
     return PackShares{{each, each}};
 }
 
+// Whether strips of a side may be cut.  A window bounds their length, unless they are of first keys that all later rows see; up to 16 tiles are left whole where there
+// are two workgroups to a unit without (and up to 4, which no chunk is shorter than, anyway), and no kernel looks for what there is to join.
+struct PackCut { bool of[2]; };
+inline PackCut pack_cut(int mask, int64_t window, int64_t sinks, int64_t M, int64_t nq, int64_t nkv, int units) {
+    const PackShares shares = pack_shares(M, nq, nkv, units);
+    PackCut cut{{shares.of[0] > 0, shares.of[1] > 0}};
+    if (mask != PACK_WINDOW) return cut;
+    const int64_t G = nq / nkv, stay = (sinks + PACK_TILE - 1) / PACK_TILE;
+    const int64_t longest[2] = {stay + (window + (PACK_BLK + G - 1) / G) / PACK_TILE + 2, sinks > 0 ? M * G : (PACK_BLK + window) * G / PACK_TILE + 2};
+    const int64_t strips[2] = {M * G / PACK_BLK * nkv, M / PACK_BLK * nkv};
+    for (int s = 0; s < 2; ++s)
+        if (longest[s] <= PACK_MIN_CHUNK / 2 || (longest[s] <= 2 * PACK_MIN_CHUNK && strips[s] >= 2 * units)) cut.of[s] = false;
+    return cut;
+}
+
 #ifdef __HIPCC__
 __device__ __forceinline__ const PackItem* pack_items(const int* plan, int64_t at) { return reinterpret_cast<const PackItem*>(plan + at); }
 // Tiles of a strip that begins with row (side 0) or key (side 1) `first` of a sequence of `len` tokens.  Rows are below 2^30, a window and the first

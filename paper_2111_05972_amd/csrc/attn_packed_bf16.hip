@@ -296,7 +296,7 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, i
     const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
     if (!pack_matches(h, p)) return;
     if ((int)blockIdx.x >= strips) {
-        dsum_rows(p, (int64_t)(blockIdx.x - strips) * 16, (int64_t)(gridDim.x - strips) * 16, PACK_TILE);
+        dsum_rows<dsum_lanes<DH>()>(p, (int)blockIdx.x - strips, (int)gridDim.x - strips, PACK_TILE);
         return;
     }
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
@@ -845,6 +845,311 @@ __global__ __launch_bounds__(WAVES8, DH <= 64 ? 4 : 2) void attn_packed_bwd_kern
     else dkv_body<DH, MASK, true>(smem, p, s);
 }
 
+// ---- backward where strips fill the chip, head sizes up to 64 ---------------------------------------------------------------
+// Four wavefronts to a strip, three workgroups to a unit.  A wavefront has 32 keys (32 rows) with both of their sums: it works out scores and dP once
+// and takes P and dS to dV and dK from its own registers, so that neither P goes through LDS nor a tile of dQ's sums is joined at the end.  Longer per
+// strip, as two wavefronts share that work above, hence for many strips only (see small_pays).
+// LDS: two stages of a tile pair (Q and dO, or K and V), 2 TB each, and 2 TB more; the strip's own rows lie in the second stage and behind it until they are in registers.
+template <int DH> constexpr int small_lds() { return 6 * tile_bytes<DH>() + 2 * 2 * PACK_TILE * 4; }
+template <int DH, int MASK>
+__device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BStrip& s) {
+    constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
+    constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2, TERMS = 6 * TB;
+    const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int len = s.it.len, rows = s.rows, G = p.G;
+    const int k0 = s.it.first + wave * 32, kv = k0 + (lane & 31);
+    const bf16_t* dobase = p.d_o + s.it.t0 * s.ldo + (int64_t)s.hk * G * p.dh;
+    const float c2 = LOG2E * p.scale;
+    f32x16 dk[NT], dv[NT];
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt) { dk[dt] = zero16(); dv[dt] = zero16(); }
+    const int qt0 = s.it.tile0, ntiles = s.it.tile1;
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
+    float rl = 0.0f;
+    auto g2r = [&](int qt, unsigned stage) {
+        int n = t;                                         // what follows from it is worked out for every tile again: kept, it spilled the loop
+        keep_in_register(n);
+        FlatTile<DH, WAVES4> ft;
+        ft.init(p.dh, n);
+        ft.load(p, s, s.q, s.ld, qt, stage, wave);
+        ft.load(p, s, dobase, s.ldo, qt, stage + TB, wave);
+        if (n < 2 * PACK_TILE) {                           // LSE of the tile's rows, then D
+            const int r = qt * PACK_TILE + (n & (PACK_TILE - 1));
+            const Row w = row_of(p, r);
+            const int64_t at = s.row0 + (int64_t)w.q * p.nq + w.g;
+            rl = r >= rows ? 0.0f : n < PACK_TILE ? p.lse[at] * LOG2E : p.dsum[at];
+        }
+    };
+    auto r2s = [&](int stage) {
+        if (t < 2 * PACK_TILE) reinterpret_cast<float*>(smem + TERMS)[stage * 2 * PACK_TILE + t] = rl;
+    };
+    unsigned ka[NF], ta[NT][2];
+#pragma unroll
+    for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) { ta[dt][g] = lds0 + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(ta[dt][g]); }
+    const unsigned terms = lds0 + TERMS + half * 16;
+    g2r(qt0, lds0);
+    r2s(0);
+    {
+        unsigned off[NCHUNKS<DH, WAVES4>];
+        dma_offsets<DH, WAVES4>(off, s.ld, p.dh, t);
+        for (int j = 0; j < 2; ++j) {
+            tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + (2 + j) * TB, off, 0, wave);
+            tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + (4 + j) * TB, off, 0, wave);
+        }
+    }
+    dma_wait();
+    __syncthreads();
+    bf16x8 kf[NF], vf[NF];
+    strip_frags<DH>(kf, lds0 + 2 * TB, wave, lane);
+    strip_frags<DH>(vf, lds0 + 4 * TB, wave, lane);
+    __syncthreads();                                       // the second stage is free
+    const int see_lo = __builtin_amdgcn_readfirstlane(CAUSAL ? k0 * G - 31 : 0), see_hi = __builtin_amdgcn_readfirstlane(k0 >= len ? 0 : WIN && k0 >= p.sinks ? min(rows, (min(k0 + 31, len - 1) + p.window) * G) : rows);
+    const int gone = WIN && k0 + 31 >= p.sinks ? __builtin_amdgcn_readfirstlane((max(k0, p.sinks) + p.window) * G) : 0x7fffffff;
+    auto slot = [&](int qt, auto stg, auto sbc) __attribute__((always_inline)) {
+        constexpr int STG = decltype(stg)::value, SB = decltype(sbc)::value, OFF = STG * 2 * TB + SB * HALF;
+        const int qs0 = qt * PACK_TILE + SB * 32;
+        if (qs0 < see_lo || qs0 >= see_hi) return;         // wavefront-uniform
+        // the fragments of the four products (Q, dO, then both transposed) through a window of W: with NF of them the loop spilled
+        constexpr int W = NF > 2 ? NF / 2 : NF;
+        bf16x8 fr[W];
+        auto fetch = [&](int i) __attribute__((always_inline)) {       // i is a compile-time constant after unrolling
+            if (i < NF) return lds_frag_k<OFF>(ka[i]);
+            if (i < 2 * NF) return lds_frag_k<OFF + TB>(ka[i - NF]);
+            const int k = i < 3 * NF ? i - 2 * NF : i - 3 * NF;
+            if (i < 3 * NF) return k & 1 ? lds_frag_t<OFF + TB + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF + TB>(ta[k >> 1][0], ta[k >> 1][1]);
+            return k & 1 ? lds_frag_t<OFF + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF>(ta[k >> 1][0], ta[k >> 1][1]);
+        };
+#pragma unroll
+        for (int i = 0; i < W; ++i) fr[i] = fetch(i);
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+        for (int i = 0; i < 2 * NF; ++i) {
+            if (i < NF) x = MFMA(fr[i % W], kf[i], x);
+            else dp = MFMA(fr[i % W], vf[i - NF], dp);
+            fr[i % W] = fetch(i + W);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (qs0 + 31 >= rows || k0 + 31 >= len || (CAUSAL && (k0 + 31) * G > qs0) || (WIN && qs0 + 31 >= gone)) {   // wavefront-uniform: diagonal or an end
+            const int from = kv < len ? (CAUSAL ? kv * G : 0) - qs0 - 4 * half : 1 << 30;
+            const int to = (WIN && kv >= p.sinks ? min(rows, (min(kv, len) + p.window) * G) : rows) - qs0 - 4 * half;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) {
+                const int r = 8 * (v >> 2) + (v & 3);
+                x[v] = r >= from && r < to ? x[v] : -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 l = lds_f4(terms + STG * 2 * PACK_TILE * 4 + SB * 128 + i * 32), d = lds_f4(terms + STG * 2 * PACK_TILE * 4 + PACK_TILE * 4 + SB * 128 + i * 32);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                x[4 * i + j] = fast_exp2(fmaf(x[4 * i + j], c2, -l[j]));
+                dp[4 * i + j] = x[4 * i + j] * (dp[4 * i + j] - d[j]);
+            }
+        }
+        const bf16x8 g[2] = {pack_regs(x, 0), pack_regs(x, 8)}, h[2] = {pack_regs(dp, 0), pack_regs(dp, 8)};
+#pragma unroll
+        for (int k = 0; k < 2 * NF; ++k) {
+            if (k < NF) dv[k >> 1] = MFMA(fr[k % W], g[k & 1], dv[k >> 1]);
+            else dk[(k - NF) >> 1] = MFMA(fr[k % W], h[k & 1], dk[(k - NF) >> 1]);
+            if (k + W < 2 * NF) {
+                fr[k % W] = fetch(2 * NF + k + W);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    };
+    using C0 = std::integral_constant<int, 0>; using C1 = std::integral_constant<int, 1>;
+    auto step = [&](int qt, auto stg) __attribute__((always_inline)) {
+        constexpr int OTHER = 1 - decltype(stg)::value;
+        const bool more = qt + 1 < ntiles;
+        if (more) g2r(qt + 1, lds0 + OTHER * 2 * TB);
+        slot(qt, stg, C0{});
+        slot(qt, stg, C1{});
+        if (more) r2s(OTHER);
+        dma_wait();
+        __syncthreads();
+    };
+    for (int qt = qt0; qt < ntiles;) {
+        step(qt, C0{});
+        if (++qt >= ntiles) break;
+        step(qt, C1{});
+        ++qt;
+    }
+    const bool whole = s.it.slot < 0;
+    const int kl = wave * 32 + (lane & 31);
+    float z[2] = {0.0f, 0.0f};
+    auto store = [&](auto is_k, const f32x16 (&acc)[NT]) __attribute__((always_inline)) {
+        constexpr bool DK = decltype(is_k)::value;
+        const float f = DK && whole ? p.scale : 1.0f;
+        float* part = whole ? nullptr : p.part[1] + ((int64_t)s.it.slot * p.nkv + s.hk) * (2 * PACK_BLK * DH) + (DK ? 0 : PACK_BLK * DH);
+        bf16_t* outp = p.dqkv + (s.it.t0 + (kv < len ? kv : 0)) * s.ld + (int64_t)(p.nq + (DK ? 0 : p.nkv) + s.hk) * p.dh;
+#pragma unroll
+        for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float v4[4] = {acc[dt][4 * i] * f, acc[dt][4 * i + 1] * f, acc[dt][4 * i + 2] * f, acc[dt][4 * i + 3] * f};
+                if (CAUSAL && (!whole || kv < len)) note4(z[DK], v4);
+                if (!whole) store_f4(part + kl * DH + dt * 32 + 8 * i + 4 * half, v4[0], v4[1], v4[2], v4[3]);
+                else if (kv < len && dt * 32 + 8 * i + 4 * half < p.dh) store4(outp + dt * 32 + 8 * i + 4 * half, v4[0], v4[1], v4[2], v4[3]);
+            }
+    };
+    store(std::true_type{}, dk);
+    store(std::false_type{}, dv);
+    if (!CAUSAL) return;
+    float* mine = reinterpret_cast<float*>(smem) + wave * 2 * DH;  // the ring has been read
+    if (any_nonfinite(z[1])) {
+        rows_stored();
+        dkv_rows_again<DH, true, WIN>(mine, p, s, k0, lane);
+    }
+    if (any_nonfinite(z[0])) {
+        rows_stored();
+        dkv_rows_again<DH, false, WIN>(mine, p, s, k0, lane);
+    }
+}
+
+template <int DH, int MASK>
+__device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStrip& s) {
+    constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
+    constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2;
+    constexpr int NCH = NCHUNKS<DH, WAVES4>;
+    const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
+    const int len = s.it.len;
+    const int r0 = s.it.first + wave * 32, r = r0 + (lane & 31);
+    const bool valid = r < s.rows;
+    const Row me = row_of(p, valid ? r : s.rows - 1);
+    const int q_lo = (int)((unsigned)min(r0, s.rows - 1) / (unsigned)p.G), q_hi = (int)((unsigned)min(r0 + 31, s.rows - 1) / (unsigned)p.G);
+    const float c2 = LOG2E * p.scale;
+    const int64_t at = s.row0 + (int64_t)me.q * p.nq + me.g;
+    const float l2 = valid ? p.lse[at] * LOG2E : 0.0f, dsum = valid ? p.dsum[at] : 0.0f;
+    const bf16_t* dobase = p.d_o + s.it.t0 * s.ldo + (int64_t)s.hk * p.G * p.dh;
+    f32x16 dq[NT];
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt) dq[dt] = zero16();
+    const int kv_end = r0 >= s.rows ? 0 : CAUSAL ? q_hi + 1 : len;
+    const int tile0 = s.it.tile0, ntiles = s.it.tile1;
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
+    unsigned off[NCH];
+    dma_offsets<DH, WAVES4>(off, s.ld, p.dh, t);
+    auto fetch_tile = [&](int v, unsigned stage) {
+        const int kt = WIN ? tile_of(p, s, v) : v;
+        tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), stage, off, 0, wave);
+        tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
+    };
+    fetch_tile(tile0, lds0);
+    FlatTile<DH, WAVES4> ft;
+    ft.init(p.dh, t);
+    for (int j = 0; j < 2; ++j) {
+        ft.load(p, s, s.q, s.ld, s.it.first / PACK_TILE + j, lds0 + (2 + j) * TB, wave);
+        ft.load(p, s, dobase, s.ldo, s.it.first / PACK_TILE + j, lds0 + (4 + j) * TB, wave);
+    }
+    settle(l2);
+    settle(dsum);
+    dma_wait();
+    __syncthreads();
+    bf16x8 qf[NF], dof[NF];
+    strip_frags<DH>(qf, lds0 + 2 * TB, wave, lane);
+    strip_frags<DH>(dof, lds0 + 4 * TB, wave, lane);
+    __syncthreads();                                       // the second stage is free
+    unsigned ka[NF], ta[NT][2];
+#pragma unroll
+    for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int g = 0; g < 2; ++g) { ta[dt][g] = lds0 + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(ta[dt][g]); }
+    auto slot = [&](int kv0, auto stg, auto sbc) __attribute__((always_inline)) {
+        constexpr int OFF = decltype(stg)::value * 2 * TB + decltype(sbc)::value * HALF;
+        if (kv0 >= kv_end || (WIN && kv0 + 32 <= q_lo + 1 - p.window && kv0 >= p.sinks)) return;   // wavefront-uniform
+        bf16x8 fr[2 * NF];
+#pragma unroll
+        for (int i = 0; i < NF; ++i) { fr[2 * i] = lds_frag_k<OFF>(ka[i]); fr[2 * i + 1] = lds_frag_k<OFF + TB>(ka[i]); }
+        __builtin_amdgcn_sched_barrier(0);
+        f32x16 x = zero16(), dp = zero16();
+#pragma unroll
+        for (int i = 0; i < NF; ++i) { x = MFMA(fr[2 * i], qf[i], x); dp = MFMA(fr[2 * i + 1], dof[i], dp); }
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int k = 0; k < NF; ++k) fr[k] = k & 1 ? lds_frag_t<OFF + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF>(ta[k >> 1][0], ta[k >> 1][1]);
+        __builtin_amdgcn_sched_barrier(0);
+        if (r0 + 31 >= s.rows || kv0 + 31 >= len || (CAUSAL && kv0 + 31 > q_lo)) {
+            const int seen = valid ? min(CAUSAL ? me.q : len, len - 1) - kv0 - half * 4 : -1;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[v] = (v >> 2) * 8 + (v & 3) <= seen ? x[v] : -INFINITY;
+        }
+        if (WIN && kv0 < q_hi + 1 - p.window && kv0 + 32 > p.sinks) {
+            const int from = me.q + 1 - p.window - kv0 - half * 4, stay = p.sinks - kv0 - half * 4;
+#pragma unroll
+            for (int v = 0; v < 16; ++v) x[v] = (v >> 2) * 8 + (v & 3) >= from || (v >> 2) * 8 + (v & 3) < stay ? x[v] : -INFINITY;
+        }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) dp[v] = fast_exp2(fmaf(x[v], c2, -l2)) * (dp[v] - dsum);
+        const bf16x8 g[2] = {pack_regs(dp, 0), pack_regs(dp, 8)};
+#pragma unroll
+        for (int k = 0; k < NF; ++k) dq[k >> 1] = MFMA(fr[k], g[k & 1], dq[k >> 1]);
+    };
+    using C0 = std::integral_constant<int, 0>; using C1 = std::integral_constant<int, 1>;
+    auto step = [&](int kt, auto stg) __attribute__((always_inline)) {
+        if (kt + 1 < ntiles) fetch_tile(kt + 1, lds0 + (1 - decltype(stg)::value) * 2 * TB);
+        const int kv0 = (WIN ? tile_of(p, s, kt) : kt) * PACK_TILE;
+        slot(kv0, stg, C0{});
+        slot(kv0 + 32, stg, C1{});
+        dma_wait();
+        __syncthreads();
+    };
+    for (int kt = tile0; kt < ntiles;) {
+        step(kt, C0{});
+        if (++kt >= ntiles) break;
+        step(kt, C1{});
+        ++kt;
+    }
+    const bool whole = s.it.slot < 0;
+    float* part = whole ? nullptr : p.part[0] + ((int64_t)s.it.slot * p.nkv + s.hk) * (PACK_BLK * DH) + (wave * 32 + (lane & 31)) * DH;
+    bf16_t* dqp = p.dqkv + (s.it.t0 + me.q) * s.ld + (int64_t)(s.hk * p.G + me.g) * p.dh;
+    const float f = whole ? p.scale : 1.0f;
+    float z = 0.0f;
+#pragma unroll
+    for (int dt = 0; dt < NT; ++dt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float v4[4] = {dq[dt][4 * i] * f, dq[dt][4 * i + 1] * f, dq[dt][4 * i + 2] * f, dq[dt][4 * i + 3] * f};
+            if (CAUSAL && (!whole || valid)) note4(z, v4);
+            if (!whole) store_f4(part + dt * 32 + 8 * i + 4 * half, v4[0], v4[1], v4[2], v4[3]);
+            else if (valid && dt * 32 + 8 * i + 4 * half < p.dh) store4(dqp + dt * 32 + 8 * i + 4 * half, v4[0], v4[1], v4[2], v4[3]);
+        }
+    if (!CAUSAL || !any_nonfinite(z)) return;
+    rows_stored();
+    dq_rows_again<DH, WIN>(reinterpret_cast<float*>(smem) + wave * 2 * DH, p, s, r0, lane);    // the ring has been read
+}
+
+template <int DH, int MASK>
+__global__ __launch_bounds__(WAVES4, 3) void attn_packed_bwd_small_kernel(Params p) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    const int of_kv = (int)min((unsigned)reinterpret_cast<const PackHeader*>(p.plan + p.header)->items[1], (unsigned)p.kv_items) * p.nkv, wg = blockIdx.x;
+    BStrip s;
+    if (wg >= of_kv) {
+        if (take_strip(p, 0, wg - of_kv, s)) dq_small<DH, MASK>(smem, p, s);
+    } else if (take_strip(p, 1, wg, s)) {
+        dkv_small<DH, MASK>(smem, p, s);
+    }
+}
+// By the tiles of rows that a strip of keys visits, as far as the host can tell (sequences of average length), and strips.  us, eight wavefronts and four, 8 heads of
+// 64 unless said otherwise: 64 sequences of 64 tokens, causal 23.6 and 20.2, of 128 without a mask 37.0 and 31.9, 512 of 16 98.5 and 76.6, 8 of 2048, causal 160 and
+// 148, a window of 256, 8 / 4 heads, 16384 tokens 78.9 and 61.7, 8192 tokens (256 strips) 47.7 and 48.8; but a window of 1500 174 and 193, 8 sequences of 2048 of 16 / 4 heads 325 and 349, one
+// of 8192 276 and 316.
+bool small_pays(const PackAttnArgs& a) {
+    int64_t tokens = a.M / a.sequences;
+    if (a.mask == PACK_WINDOW) tokens = std::min<int64_t>(tokens, (int64_t)a.window + PACK_BLK);
+    const int64_t tiles = tokens * (a.nq / a.nkv) / PACK_TILE;
+    return tiles <= 8 || (tiles <= 32 && a.M / PACK_BLK * a.nkv >= 2 * compute_units());
+}
+
 template <int DH, int MASK>
 hipError_t run_fwd(const PackAttnArgs& a) {
     const PackShares shares = pack_shares(a.M, a.nq, a.nkv, compute_units());
@@ -856,7 +1161,7 @@ hipError_t run_fwd(const PackAttnArgs& a) {
     if (attr != hipSuccess) return attr;
     hipLaunchKernelGGL((attn_packed_fwd_kernel<DH, MASK>), dim3((unsigned)(L.cap[0] * a.nkv)), dim3(WAVES4), lds, a.stream, p);
     const hipError_t e = hipGetLastError();
-    if (e != hipSuccess || shares.of[0] == 0) return e;
+    if (e != hipSuccess || !cut_of(a).of[0]) return e;
     hipLaunchKernelGGL((attn_packed_fwd_join_kernel<bf16_t, DH>), dim3(join_wgs(L, a.nkv)), dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }
@@ -868,17 +1173,27 @@ hipError_t run_bwd(const PackAttnArgs& a) {
     const Ws w = ws_of(a, true);
     p.part[0] = (float*)a.ws;
     p.part[1] = (float*)((char*)a.ws + w.part[0]);
-    const int strips = (int)std::min<int64_t>(L.cap[0] * a.nkv, 2 * compute_units()), rows = (int)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units());
+    const bool narrow = MASK == PACK_WINDOW && a.window + a.sinks <= PACK_TILE;          // all strips, one to a workgroup
+    const int strips = (int)std::min<int64_t>(L.cap[0] * a.nkv, narrow ? 1 << 20 : 2 * compute_units()), rows = (int)dsum_wgs<dsum_lanes<DH>()>(a);
     hipLaunchKernelGGL((attn_packed_dsum_kernel<DH, MASK>), dim3((unsigned)(strips + rows)), dim3(WAVES4), dsum_lds<DH>(), a.stream, p, strips);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     p.kv_items = (int)L.cap[1];
-    constexpr int lds = std::max(dkv_lds<DH>(), dq_lds<DH>());
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_bwd_kernel<DH, MASK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((attn_packed_bwd_kernel<DH, MASK>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv)), dim3(WAVES8), lds, a.stream, p);
+    const dim3 grid((unsigned)((L.cap[0] + L.cap[1]) * a.nkv));
+    bool small = false;
+    if constexpr (DH <= 64) {
+        small = small_pays(a);
+        if (small) hipLaunchKernelGGL((attn_packed_bwd_small_kernel<DH, MASK>), grid, dim3(WAVES4), small_lds<DH>(), a.stream, p);
+    }
+    if (!small) {
+        constexpr int lds = std::max(dkv_lds<DH>(), dq_lds<DH>());
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_bwd_kernel<DH, MASK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (attr != hipSuccess) return attr;
+        hipLaunchKernelGGL((attn_packed_bwd_kernel<DH, MASK>), grid, dim3(WAVES8), lds, a.stream, p);
+    }
     e = hipGetLastError();
-    if (e != hipSuccess || shares.of[0] == 0) return e;
+    const PackCut cut = cut_of(a);
+    if (e != hipSuccess || !(cut.of[0] || cut.of[1])) return e;
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<bf16_t, DH>), dim3(join_wgs(L, a.nkv)), dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }

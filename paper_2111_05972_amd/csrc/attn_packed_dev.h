@@ -148,24 +148,46 @@ __global__ __launch_bounds__(32 * JOIN_ROWS) void attn_packed_fwd_join_kernel(Pa
 }
 
 // ---- D = rowsum(dO * O) of every row and head -------------------------------------------------------------------------------
-// A quarter wavefront to a row of 8-element chunks; rows of at most `above` keys are left out, and those of no sequence.
-template <typename T>
-__device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int64_t first, int64_t step, int above) {
-    const int c = (threadIdx.x & 15) * 8;
-    for (int64_t row = first + threadIdx.x / 16; row < (int64_t)p.M * p.nq; row += step) {
-        const bool wanted = p.plan[p.seen + (unsigned)row / (unsigned)p.nq] > above;
-        float a = 0.0f;
-        if (wanted && c < p.dh) {
-            float x[8], y[8];
-            load8(p.o + row * p.dh + c, x);
-            load8(p.d_o + row * p.dh + c, y);
+// LANES lanes to a row, eight elements each, four rows at a time so that their loads are under way together; rows of at most `above` keys are left out, and those
+// of no sequence.
+template <int DH> constexpr int dsum_lanes() { return DH <= 32 ? 4 : DH <= 64 ? 8 : 16; }
+template <int LANES, typename T>
+__device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int wg, int wgs, int above) {
+    constexpr int ROWS = 256 / LANES, AHEAD = 4;
+    const int c = (threadIdx.x % LANES) * 8;
+    const int64_t all = (int64_t)p.M * p.nq;
+    for (int64_t row0 = (int64_t)wg * ROWS + threadIdx.x / LANES; row0 < all; row0 += (int64_t)wgs * ROWS * AHEAD) {
+        bool wanted[AHEAD];
+        float x[AHEAD][8], y[AHEAD][8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a = fmaf(x[e], y[e], a);
+        for (int j = 0; j < AHEAD; ++j) {
+            const int64_t row = row0 + (int64_t)j * wgs * ROWS;
+            wanted[j] = row < all && p.plan[p.seen + (unsigned)row / (unsigned)p.nq] > above;
         }
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) a += __shfl_xor(a, off, 64);
-        if (wanted && c == 0) p.dsum[row] = a;
+        for (int j = 0; j < AHEAD; ++j) {
+            const int64_t row = row0 + (int64_t)j * wgs * ROWS;
+            if (wanted[j] && c < p.dh) {
+                load8(p.o + row * p.dh + c, x[j]);
+                load8(p.d_o + row * p.dh + c, y[j]);
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            float a = 0.0f;
+            if (wanted[j] && c < p.dh) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) a = fmaf(x[j][e], y[j][e], a);
+            }
+#pragma unroll
+            for (int off = LANES / 2; off > 0; off >>= 1) a += __shfl_xor(a, off, 64);
+            if (wanted[j] && c == 0) p.dsum[row0 + (int64_t)j * wgs * ROWS] = a;
+        }
     }
+}
+// Workgroups for that.
+template <int LANES> unsigned dsum_wgs(const PackAttnArgs& a) {
+    return (unsigned)std::min<int64_t>((a.M * a.nq * LANES + 255) / 256, 8 * compute_units());
 }
 
 // dQ, dK and dV of the strips that were cut: the sums of their chunks in chunk order.  dQ, then dK, then dV.
@@ -208,6 +230,7 @@ PackParams<T> make_params(const PackAttnArgs& a, const PackLayout& L) {
     p.scale = 1.0f / sqrtf((float)a.dh);
     return p;
 }
+PackCut cut_of(const PackAttnArgs& a) { return pack_cut(a.mask, a.window, a.sinks, a.M, a.nq, a.nkv, compute_units()); }
 int padded(int dh) { return (dh + 31) / 32 * 32; }
 // Sums of chunks: a cut strip of n tiles has at most 2 n / chunk of them.
 struct Ws { size_t part[2], total; };

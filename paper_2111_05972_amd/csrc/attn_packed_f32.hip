@@ -439,9 +439,10 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
     }
 }
 
+template <int LANES>
 __global__ __launch_bounds__(256) void attn_packed_f32_dsum_kernel(FParams p) {
     if (pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p))
-        dsum_rows(p, (int64_t)blockIdx.x * 16, (int64_t)gridDim.x * 16, 0);
+        dsum_rows<LANES>(p, (int)blockIdx.x, (int)gridDim.x, 0);
 }
 
 // Two workgroups share a compute unit up to head size 64 (see attn_f32.hip); wider heads need more than 256 registers.
@@ -472,18 +473,19 @@ hipError_t launch(const PackAttnArgs& a, bool bwd) {
     p.part[0] = (float*)a.ws;
     p.many = many_strips(DH);
     const dim3 join(join_wgs(L, a.nkv));
+    const PackCut cut = cut_of(a);
     hipError_t e;
     if (!bwd) {
         hipLaunchKernelGGL((attn_packed_f32_fwd_kernel<DH, MANY, WIN>), dim3((unsigned)(L.cap[0] * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
-        if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
+        if ((e = hipGetLastError()) != hipSuccess || !cut.of[0]) return e;
         hipLaunchKernelGGL((attn_packed_fwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
         return hipGetLastError();
     }
     p.part[1] = (float*)((char*)a.ws + ws_of(a, true).part[0]);
-    hipLaunchKernelGGL(attn_packed_f32_dsum_kernel, dim3((unsigned)std::min<int64_t>((a.M * a.nq + 15) / 16, 8 * compute_units())), dim3(256), 0, a.stream, p);
+    hipLaunchKernelGGL(attn_packed_f32_dsum_kernel<dsum_lanes<DH>()>, dim3(dsum_wgs<dsum_lanes<DH>()>(a)), dim3(256), 0, a.stream, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
     hipLaunchKernelGGL((attn_packed_f32_bwd_kernel<DH, MANY, WIN>), dim3((unsigned)((L.cap[0] + L.cap[1]) * a.nkv * QUARTERS)), dim3(256), lds, a.stream, p);
-    if ((e = hipGetLastError()) != hipSuccess || shares.of[0] == 0) return e;
+    if ((e = hipGetLastError()) != hipSuccess || !(cut.of[0] || cut.of[1])) return e;
     hipLaunchKernelGGL((attn_packed_bwd_join_kernel<float, DH>), join, dim3(32 * JOIN_ROWS), 0, a.stream, p);
     return hipGetLastError();
 }

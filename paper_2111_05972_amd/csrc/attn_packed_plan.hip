@@ -44,6 +44,7 @@ template <bool MAX> __device__ int block_scan(int v, int* tmp, int& total) {
 struct PlanParams {
     int n, M, nq, nkv, mask, window, sinks;
     PackShares shares;
+    PackCut cut;
     const int* offsets;
     int* plan;
     PackLayout L;
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         const int* pre = before[side];
         int chunk = 1 << 30;
         const bool few = (int64_t)(tiles[0] + tiles[1]) <= 5 * p.shares.of[side];          // a compute unit and a quarter to a chunk at most
-        if (p.shares.of[side] > 0) chunk = max(few ? PACK_MIN_CHUNK / 2 : PACK_MIN_CHUNK, (int)((tiles[side] + p.shares.of[side] - 1) / p.shares.of[side]));
+        if (p.cut.of[side]) chunk = max(few ? PACK_MIN_CHUNK / 2 : PACK_MIN_CHUNK, (int)((tiles[side] + p.shares.of[side] - 1) / p.shares.of[side]));
         const int top = min(longest[side], chunk) + 1;
         PackItem* items = reinterpret_cast<PackItem*>(p.plan + p.L.items[side]);
         PackItem* join = reinterpret_cast<PackItem*>(p.plan + p.L.joins[side]);
@@ -223,6 +224,7 @@ hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, i
     PlanParams p{};
     p.n = (int)sequences; p.M = (int)M; p.nq = nq; p.nkv = nkv; p.mask = mask; p.window = window; p.sinks = sinks;
     p.shares = pack_shares(M, nq, nkv, compute_units());
+    p.cut = pack_cut(mask, window, sinks, M, nq, nkv, compute_units());
     p.offsets = offsets; p.plan = plan;
     p.L = pack_layout(sequences, M, nq, nkv, p.shares);
     static_assert(BUCKETS == PLAN_THREADS && NEAR > PLAN_THREADS, "a thread to a bucket, 1024 sequences and an end in LDS");

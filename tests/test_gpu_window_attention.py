@@ -89,6 +89,19 @@ def test_edges(window, sinks, dtype, nq, nkv, dh):
     _run([1, 0, 63, 300, 65, 0], nq, nkv, dh, window, sinks, dtype, behind=3)
 
 
+# the same beside a long document: heads of up to 64 have a backward form for short strips (what is above) and one for long ones
+@pytest.mark.parametrize("window,sinks", [(64, 0), (65, 70), (500, 1), (2000, 0)])
+@pytest.mark.parametrize("nq,nkv,dh", [(8, 1, 64), (12, 2, 32), (8, 1, 40)])
+def test_edges_beside_a_long_document(nq, nkv, dh, window, sinks):
+    _run([1, 0, 63, 300, 65, 0, 1, 1300], nq, nkv, dh, window, sinks, BF16, behind=3)
+
+
+# and short strips that fill the chip: more than two strips of keys to a compute unit
+@pytest.mark.parametrize("window,sinks", [(200, 3), (1, 0), (40, 0)])
+def test_short_strips_that_fill_the_chip(window, sinks):
+    _run([520, 0, 300, 270], 64, 64, 64, window, sinks, BF16, behind=2)
+
+
 @pytest.mark.parametrize("dtype", [BF16, FLOAT])
 @pytest.mark.parametrize("dh", [8, 32, 40, 96, 104, 128])
 def test_head_sizes(dh, dtype):
