@@ -1,4 +1,4 @@
-"""ctypes binding of libtp_layer.so: same names as the C ABI, argument marshalling only.
+"""Binding of libtp_layer.so: same names as the C ABI, argument marshalling only (csrc/calls.cpp, and ctypes where arguments are structures).
 
 Device buffers are anything with a `.data_ptr()` (torch tensors) or plain integer addresses.
 There is no fallback: if the shared library is missing, loading raises.
@@ -131,6 +131,16 @@ def load_library():
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
+    # Entry points that take numbers and pointers only: called from C, with the same arguments, at a quarter of the time.  Tensors and streams
+    # may be passed as they are.
+    try:
+        from . import _calls
+    except ImportError as e:
+        raise ImportError("the module that calls the library is missing: build it with `python -m paper_2111_05972_amd.build`") from e
+    _calls.open(path)
+    for name in sig:
+        if hasattr(_calls, name):
+            setattr(lib, name, getattr(_calls, name))
     _lib = lib
     return lib
 
@@ -145,7 +155,7 @@ def _ptr(x):
 
 
 def _nbytes(x):
-    return x.numel() * x.element_size() if hasattr(x, "numel") else None
+    return getattr(x, "nbytes", None)
 
 
 def _stream(stream):
@@ -243,8 +253,8 @@ def tp_layer_ln_workspace_bytes(M, H):
 
 
 def tp_layer_ln_fwd(dtype, M, H, a, b, gamma, beta, eps, z, y, mean, rstd, stream=None, check=True):
-    rc = load_library().tp_layer_ln_fwd(dtype, M, H, _ptr(a), _ptr(b), _ptr(gamma), _ptr(beta), float(eps),
-                                        _ptr(z), _ptr(y), _ptr(mean), _ptr(rstd), _stream(stream))
+    rc = load_library().tp_layer_ln_fwd(dtype, M, H, a, b, gamma, beta, eps,
+                                        z, y, mean, rstd, stream)
     if check and rc != TPL_OK:
         raise TpLayerError(rc, "tp_layer_ln_fwd")
     return rc
@@ -252,9 +262,9 @@ def tp_layer_ln_fwd(dtype, M, H, a, b, gamma, beta, eps, z, y, mean, rstd, strea
 
 def tp_layer_ln_bwd(dtype, M, H, dy, z, mean, rstd, gamma, dz, dgamma, dbeta, ws, ws_bytes=None, stream=None,
                     check=True):
-    rc = load_library().tp_layer_ln_bwd(dtype, M, H, _ptr(dy), _ptr(z), _ptr(mean), _ptr(rstd), _ptr(gamma),
-                                        _ptr(dz), _ptr(dgamma), _ptr(dbeta), _ptr(ws),
-                                        (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_ln_bwd(dtype, M, H, dy, z, mean, rstd, gamma,
+                                        dz, dgamma, dbeta, ws,
+                                        (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     if check and rc != TPL_OK:
         raise TpLayerError(rc, "tp_layer_ln_bwd")
     return rc
@@ -267,24 +277,24 @@ def _checked(rc, what, check):
 
 
 def tp_layer_ln_moments(dtype, M, Hs, x_loc, sums, stream=None, check=True):
-    rc = load_library().tp_layer_ln_moments(dtype, M, Hs, _ptr(x_loc), _ptr(sums), _stream(stream))
+    rc = load_library().tp_layer_ln_moments(dtype, M, Hs, x_loc, sums, stream)
     return _checked(rc, "tp_layer_ln_moments", check)
 
 
 def tp_layer_ln_stats(M, H, eps, totals, mean, rstd, stream=None, check=True):
-    rc = load_library().tp_layer_ln_stats(M, H, float(eps), _ptr(totals), _ptr(mean), _ptr(rstd), _stream(stream))
+    rc = load_library().tp_layer_ln_stats(M, H, eps, totals, mean, rstd, stream)
     return _checked(rc, "tp_layer_ln_stats", check)
 
 
 def tp_layer_ln_apply_fwd(dtype, M, Hs, x_loc, mean, rstd, gamma_loc, beta_loc, y, stream=None, check=True):
-    rc = load_library().tp_layer_ln_apply_fwd(dtype, M, Hs, _ptr(x_loc), _ptr(mean), _ptr(rstd), _ptr(gamma_loc),
-                                              _ptr(beta_loc), _ptr(y), _stream(stream))
+    rc = load_library().tp_layer_ln_apply_fwd(dtype, M, Hs, x_loc, mean, rstd, gamma_loc,
+                                              beta_loc, y, stream)
     return _checked(rc, "tp_layer_ln_apply_fwd", check)
 
 
 def tp_layer_ln_apply_bwd_sums(dtype, M, Hs, dy, x_loc, mean, rstd, gamma_loc, sums, stream=None, check=True):
-    rc = load_library().tp_layer_ln_apply_bwd_sums(dtype, M, Hs, _ptr(dy), _ptr(x_loc), _ptr(mean), _ptr(rstd),
-                                                   _ptr(gamma_loc), _ptr(sums), _stream(stream))
+    rc = load_library().tp_layer_ln_apply_bwd_sums(dtype, M, Hs, dy, x_loc, mean, rstd,
+                                                   gamma_loc, sums, stream)
     return _checked(rc, "tp_layer_ln_apply_bwd_sums", check)
 
 
@@ -295,15 +305,15 @@ def tp_layer_ln_apply_workspace_bytes(M, Hs):
 def tp_layer_ln_apply_bwd(dtype, M, Hs, H, dy, x_loc, mean, rstd, gamma_loc, totals, dx_add, dx, dgamma_loc,
                           dbeta_loc, ws, ws_bytes=None, stream=None, check=True):
     rc = load_library().tp_layer_ln_apply_bwd(
-        dtype, M, Hs, H, _ptr(dy), _ptr(x_loc), _ptr(mean), _ptr(rstd), _ptr(gamma_loc), _ptr(totals), _ptr(dx_add),
-        _ptr(dx), _ptr(dgamma_loc), _ptr(dbeta_loc), _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
-        _stream(stream))
+        dtype, M, Hs, H, dy, x_loc, mean, rstd, gamma_loc, totals, dx_add,
+        dx, dgamma_loc, dbeta_loc, ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
+        stream)
     return _checked(rc, "tp_layer_ln_apply_bwd", check)
 
 
 def tp_layer_slice_epilogue_fwd(dtype, act, M, N, inp, bias, resid, u, out, stream=None, check=True):
-    rc = load_library().tp_layer_slice_epilogue_fwd(dtype, act, M, N, _ptr(inp), _ptr(bias), _ptr(resid), _ptr(u),
-                                                    _ptr(out), _stream(stream))
+    rc = load_library().tp_layer_slice_epilogue_fwd(dtype, act, M, N, inp, bias, resid, u,
+                                                    out, stream)
     return _checked(rc, "tp_layer_slice_epilogue_fwd", check)
 
 
@@ -312,9 +322,9 @@ def tp_layer_slice_epilogue_workspace_bytes(M, N):
 
 
 def tp_layer_slice_epilogue_bwd(dtype, act, M, N, dout, u, din, dbias, ws, ws_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_slice_epilogue_bwd(dtype, act, M, N, _ptr(dout), _ptr(u), _ptr(din), _ptr(dbias),
-                                                    _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
-                                                    _stream(stream))
+    rc = load_library().tp_layer_slice_epilogue_bwd(dtype, act, M, N, dout, u, din, dbias,
+                                                    ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
+                                                    stream)
     return _checked(rc, "tp_layer_slice_epilogue_bwd", check)
 
 
@@ -323,8 +333,8 @@ def tp_layer_static_scratch_bytes():
 
 
 def tp_layer_slice_epilogue_bwd_static(dtype, act, M, N, dout, u, din, dbias, stream=None, check=True):
-    rc = load_library().tp_layer_slice_epilogue_bwd_static(dtype, act, M, N, _ptr(dout), _ptr(u), _ptr(din),
-                                                           _ptr(dbias), _stream(stream))
+    rc = load_library().tp_layer_slice_epilogue_bwd_static(dtype, act, M, N, dout, u, din,
+                                                           dbias, stream)
     return _checked(rc, "tp_layer_slice_epilogue_bwd_static", check)
 
 
@@ -356,9 +366,9 @@ def tp_layer_gemm_workspace_bytes(dtype, M, N, K):
 def tp_layer_gemm(dtype, trans_a, trans_b, M, N, K, A, B, C, bias=None, resid=None, aux=None,
                   epi=TPL_EPI_NONE, ws=None, ws_bytes=None, stream=None, check=True):
     rc = load_library().tp_layer_gemm(
-        dtype, int(bool(trans_a)), int(bool(trans_b)), M, N, K, _ptr(A), _ptr(B), _ptr(C), _ptr(bias),
-        _ptr(resid), _ptr(aux), epi, _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
-        _stream(stream))
+        dtype, int(bool(trans_a)), int(bool(trans_b)), M, N, K, A, B, C, bias,
+        resid, aux, epi, ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
+        stream)
     if check and rc != TPL_OK:
         raise TpLayerError(rc, "tp_layer_gemm")
     return rc
@@ -392,9 +402,9 @@ def tp_layer_attn_workspace_bytes(dtype, B, S, nl, dh, causal, bwd):
 
 def tp_layer_attn_fwd(dtype, B, S, nl, dh, causal, qkv, o, lse, ws=None, ws_bytes=None, stream=None,
                       check=True):
-    rc = load_library().tp_layer_attn_fwd(dtype, B, S, nl, dh, int(bool(causal)), _ptr(qkv), _ptr(o),
-                                          _ptr(lse), _ptr(ws),
-                                          (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_attn_fwd(dtype, B, S, nl, dh, int(bool(causal)), qkv, o,
+                                          lse, ws,
+                                          (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     if check and rc != TPL_OK:
         raise TpLayerError(rc, "tp_layer_attn_fwd")
     return rc
@@ -402,9 +412,9 @@ def tp_layer_attn_fwd(dtype, B, S, nl, dh, causal, qkv, o, lse, ws=None, ws_byte
 
 def tp_layer_attn_bwd(dtype, B, S, nl, dh, causal, qkv, o, lse, d_o, dqkv, d_scratch, ws=None,
                       ws_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_attn_bwd(dtype, B, S, nl, dh, int(bool(causal)), _ptr(qkv), _ptr(o),
-                                          _ptr(lse), _ptr(d_o), _ptr(dqkv), _ptr(d_scratch), _ptr(ws),
-                                          (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_attn_bwd(dtype, B, S, nl, dh, int(bool(causal)), qkv, o,
+                                          lse, d_o, dqkv, d_scratch, ws,
+                                          (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     if check and rc != TPL_OK:
         raise TpLayerError(rc, "tp_layer_attn_bwd")
     return rc
@@ -419,21 +429,21 @@ def tp_layer_rope_frequencies(rot, base=10000.0, scaling=TPL_ROPE_PLAIN, stretch
 
 
 def tp_layer_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, qkv, out, seq=0, stream=None, check=True):
-    rc = load_library().tp_layer_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(qkv),
-                                          _ptr(out), _stream(stream))
+    rc = load_library().tp_layer_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, qkv,
+                                          out, stream)
     return _checked(rc, "tp_layer_rope_fwd", check)
 
 
 def tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, dqkv, out, seq=0, stream=None, check=True):
-    rc = load_library().tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(dqkv),
-                                          _ptr(out), _stream(stream))
+    rc = load_library().tp_layer_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, dqkv,
+                                          out, stream)
     return _checked(rc, "tp_layer_rope_bwd", check)
 
 
 def tp_layer_qk_norm_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, gamma_q, gamma_k, per_head, eps, qkv, out, seq=0,
                               stream=None, check=True):
-    rc = load_library().tp_layer_qk_norm_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(gamma_q),
-                                                  _ptr(gamma_k), int(bool(per_head)), float(eps), _ptr(qkv), _ptr(out), _stream(stream))
+    rc = load_library().tp_layer_qk_norm_rope_fwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, gamma_q,
+                                                  gamma_k, int(bool(per_head)), eps, qkv, out, stream)
     return _checked(rc, "tp_layer_qk_norm_rope_fwd", check)
 
 
@@ -443,15 +453,15 @@ def tp_layer_qk_norm_rope_workspace_bytes(dtype, M, nq, nkv, dh):
 
 def tp_layer_qk_norm_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, gamma_q, gamma_k, per_head, eps, qkv, dqkv, out, dgamma_q,
                               dgamma_k, ws, ws_bytes=None, seq=0, stream=None, check=True):
-    rc = load_library().tp_layer_qk_norm_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, _ptr(freq), float(factor), _ptr(positions), seq, _ptr(gamma_q),
-                                                  _ptr(gamma_k), int(bool(per_head)), float(eps), _ptr(qkv), _ptr(dqkv), _ptr(out), _ptr(dgamma_q),
-                                                  _ptr(dgamma_k), _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_qk_norm_rope_bwd(dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, gamma_q,
+                                                  gamma_k, int(bool(per_head)), eps, qkv, dqkv, out, dgamma_q,
+                                                  dgamma_k, ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_qk_norm_rope_bwd", check)
 
 
 def tp_layer_dropout_fwd(dtype, M, N, p, rng, site, first_row, first_col, width, inp, bias, resid, out, stream=None, check=True):
-    rc = load_library().tp_layer_dropout_fwd(dtype, M, N, float(p), _ptr(rng), site, first_row, first_col, width, _ptr(inp), _ptr(bias), _ptr(resid),
-                                             _ptr(out), _stream(stream))
+    rc = load_library().tp_layer_dropout_fwd(dtype, M, N, p, rng, site, first_row, first_col, width, inp, bias, resid,
+                                             out, stream)
     return _checked(rc, "tp_layer_dropout_fwd", check)
 
 
@@ -460,8 +470,8 @@ def tp_layer_dropout_workspace_bytes(M, N):
 
 
 def tp_layer_dropout_bwd(dtype, M, N, p, rng, site, first_row, first_col, width, dout, din, dbias=None, ws=None, ws_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_dropout_bwd(dtype, M, N, float(p), _ptr(rng), site, first_row, first_col, width, _ptr(dout), _ptr(din), _ptr(dbias),
-                                             _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_dropout_bwd(dtype, M, N, p, rng, site, first_row, first_col, width, dout, din, dbias,
+                                             ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_dropout_bwd", check)
 
 
@@ -470,8 +480,8 @@ def tp_layer_pack_plan_bytes(sequences, M, nq, nkv):
 
 
 def tp_layer_pack_plan(sequences, M, offsets, nq, nkv, causal, plan, plan_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_pack_plan(sequences, M, _ptr(offsets), nq, nkv, int(bool(causal)), _ptr(plan),
-                                           (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _stream(stream))
+    rc = load_library().tp_layer_pack_plan(sequences, M, offsets, nq, nkv, int(bool(causal)), plan,
+                                           (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, stream)
     return _checked(rc, "tp_layer_pack_plan", check)
 
 
@@ -481,18 +491,18 @@ def tp_layer_attn_packed_workspace_bytes(dtype, sequences, M, nq, nkv, dh, causa
 
 def tp_layer_attn_packed_fwd(dtype, sequences, M, nq, nkv, dh, causal, plan, qkv, o, lse, ws, ws_bytes=None, plan_bytes=None, stream=None,
                              check=True):
-    rc = load_library().tp_layer_attn_packed_fwd(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), _ptr(plan),
-                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _ptr(qkv), _ptr(o), _ptr(lse),
-                                                 _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_attn_packed_fwd(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), plan,
+                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, qkv, o, lse,
+                                                 ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_attn_packed_fwd", check)
 
 
 def tp_layer_attn_packed_bwd(dtype, sequences, M, nq, nkv, dh, causal, plan, qkv, o, lse, d_o, dqkv, d_scratch, ws, ws_bytes=None,
                              plan_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_attn_packed_bwd(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), _ptr(plan),
-                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _ptr(qkv), _ptr(o), _ptr(lse),
-                                                 _ptr(d_o), _ptr(dqkv), _ptr(d_scratch), _ptr(ws),
-                                                 (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_attn_packed_bwd(dtype, sequences, M, nq, nkv, dh, int(bool(causal)), plan,
+                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, qkv, o, lse,
+                                                 d_o, dqkv, d_scratch, ws,
+                                                 (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_attn_packed_bwd", check)
 
 
@@ -501,8 +511,8 @@ def tp_layer_window_plan_bytes(sequences, M, nq, nkv):
 
 
 def tp_layer_window_plan(sequences, M, offsets, nq, nkv, window, sinks, plan, plan_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_window_plan(sequences, M, _ptr(offsets), nq, nkv, window, sinks, _ptr(plan),
-                                             (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _stream(stream))
+    rc = load_library().tp_layer_window_plan(sequences, M, offsets, nq, nkv, window, sinks, plan,
+                                             (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, stream)
     return _checked(rc, "tp_layer_window_plan", check)
 
 
@@ -512,18 +522,18 @@ def tp_layer_attn_window_workspace_bytes(dtype, sequences, M, nq, nkv, dh, windo
 
 def tp_layer_attn_window_fwd(dtype, sequences, M, nq, nkv, dh, window, sinks, plan, qkv, o, lse, ws, ws_bytes=None, plan_bytes=None, stream=None,
                              check=True):
-    rc = load_library().tp_layer_attn_window_fwd(dtype, sequences, M, nq, nkv, dh, window, sinks, _ptr(plan),
-                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _ptr(qkv), _ptr(o), _ptr(lse),
-                                                 _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_attn_window_fwd(dtype, sequences, M, nq, nkv, dh, window, sinks, plan,
+                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, qkv, o, lse,
+                                                 ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_attn_window_fwd", check)
 
 
 def tp_layer_attn_window_bwd(dtype, sequences, M, nq, nkv, dh, window, sinks, plan, qkv, o, lse, d_o, dqkv, d_scratch, ws, ws_bytes=None,
                              plan_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_attn_window_bwd(dtype, sequences, M, nq, nkv, dh, window, sinks, _ptr(plan),
-                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, _ptr(qkv), _ptr(o), _ptr(lse),
-                                                 _ptr(d_o), _ptr(dqkv), _ptr(d_scratch), _ptr(ws),
-                                                 (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_attn_window_bwd(dtype, sequences, M, nq, nkv, dh, window, sinks, plan,
+                                                 (_nbytes(plan) or 0) if plan_bytes is None else plan_bytes, qkv, o, lse,
+                                                 d_o, dqkv, d_scratch, ws,
+                                                 (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_attn_window_bwd", check)
 
 
@@ -532,18 +542,18 @@ def tp_layer_lm_loss_workspace_bytes(dtype, M, H, V, bwd):
 
 
 def tp_layer_lm_loss_fwd(dtype, M, H, V, first, x, w, labels, stats, ws, ws_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_lm_loss_fwd(dtype, M, H, V, first, _ptr(x), _ptr(w), _ptr(labels), _ptr(stats), _ptr(ws),
-                                             (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, _stream(stream))
+    rc = load_library().tp_layer_lm_loss_fwd(dtype, M, H, V, first, x, w, labels, stats, ws,
+                                             (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes, stream)
     return _checked(rc, "tp_layer_lm_loss_fwd", check)
 
 
 def tp_layer_lm_loss_join(M, ranks, vocab, stats, labels, loss, lse, stream=None, check=True):
-    rc = load_library().tp_layer_lm_loss_join(M, ranks, vocab, _ptr(stats), _ptr(labels), _ptr(loss), _ptr(lse), _stream(stream))
+    rc = load_library().tp_layer_lm_loss_join(M, ranks, vocab, stats, labels, loss, lse, stream)
     return _checked(rc, "tp_layer_lm_loss_join", check)
 
 
 def tp_layer_lm_loss_bwd(dtype, M, H, V, first, vocab, x, w, labels, lse, dloss, dx_partial, dw, ws, ws_bytes=None, stream=None, check=True):
-    rc = load_library().tp_layer_lm_loss_bwd(dtype, M, H, V, first, vocab, _ptr(x), _ptr(w), _ptr(labels), _ptr(lse), _ptr(dloss),
-                                             _ptr(dx_partial), _ptr(dw), _ptr(ws), (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
-                                             _stream(stream))
+    rc = load_library().tp_layer_lm_loss_bwd(dtype, M, H, V, first, vocab, x, w, labels, lse, dloss,
+                                             dx_partial, dw, ws, (_nbytes(ws) or 0) if ws_bytes is None else ws_bytes,
+                                             stream)
     return _checked(rc, "tp_layer_lm_loss_bwd", check)

@@ -1,7 +1,8 @@
-"""Build the HIP shared library in-tree with hipcc for gfx950 (no torch involved)."""
+"""Build the HIP shared library in-tree with hipcc for gfx950, and the Python module that calls it (no torch involved)."""
 import os
 import subprocess
 import sys
+import sysconfig
 import tempfile
 from concurrent.futures import ThreadPoolExecutor
 
@@ -13,6 +14,7 @@ SOURCES = ["tp_layer.cpp", "simple_kernels.hip", "gemm_bf16.hip", "attn_bf16.hip
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wno-unused-command-line-argument", "-Wno-option-ignored"]
+CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))         # the Python module that calls the library
 JOBS = 4                    # compilers at once: each takes about 1 GB
 
 
@@ -29,7 +31,7 @@ def _run(cmd, verbose):
 
 
 def build(verbose=False, extra=(), out=LIB):
-    """Every source is compiled, side by side, and linked into `out`."""
+    """Every source is compiled, side by side, and linked into `out`; then the module that calls it."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
@@ -37,6 +39,8 @@ def build(verbose=False, extra=(), out=LIB):
         with ThreadPoolExecutor(JOBS) as pool:
             text = list(pool.map(compile_one, SOURCES, objects))
         text.append(_run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared"] + objects + ["-o", out], verbose))
+    text.append(_run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.cpp"),
+                      "-o", CALLS, "-ldl"], verbose))
     return "\n".join(t for t in text if t)
 
 

@@ -293,12 +293,12 @@ __global__ __launch_bounds__(WAVES4, 2) void attn_packed_dsum_kernel(Params p, i
     extern __shared__ __attribute__((aligned(16))) char smem[];
     constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
     constexpr int TB = tile_bytes<DH>(), NF = DH / 16, HALF = 32 * DH * 2, NCH = NCHUNKS<DH, WAVES4>;
-    const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
-    if (!pack_matches(h, p)) return;
     if ((int)blockIdx.x >= strips) {
         dsum_rows<dsum_lanes<DH>()>(p, (int)blockIdx.x - strips, (int)gridDim.x - strips, PACK_TILE);
         return;
     }
+    const PackHeader* h = reinterpret_cast<const PackHeader*>(p.plan + p.header);
+    if (!pack_matches(h, p)) return;
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;

@@ -149,13 +149,14 @@ __global__ __launch_bounds__(32 * JOIN_ROWS) void attn_packed_fwd_join_kernel(Pa
 
 // ---- D = rowsum(dO * O) of every row and head -------------------------------------------------------------------------------
 // LANES lanes to a row, eight elements each, four rows at a time so that their loads are under way together; rows of at most `above` keys are left out, and those
-// of no sequence.
+// of no sequence.  Whose plan it is shows while the keys that the first rows see are under way.
 template <int DH> constexpr int dsum_lanes() { return DH <= 32 ? 4 : DH <= 64 ? 8 : 16; }
 template <int LANES, typename T>
 __device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int wg, int wgs, int above) {
     constexpr int ROWS = 256 / LANES, AHEAD = 4;
     const int c = (threadIdx.x % LANES) * 8;
     const int64_t all = (int64_t)p.M * p.nq;
+    bool ours = false;
     for (int64_t row0 = (int64_t)wg * ROWS + threadIdx.x / LANES; row0 < all; row0 += (int64_t)wgs * ROWS * AHEAD) {
         bool wanted[AHEAD];
         float x[AHEAD][8], y[AHEAD][8];
@@ -164,6 +165,7 @@ __device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int wg, int wg
             const int64_t row = row0 + (int64_t)j * wgs * ROWS;
             wanted[j] = row < all && p.plan[p.seen + (unsigned)row / (unsigned)p.nq] > above;
         }
+        if (!ours && !(ours = pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p))) return;
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             const int64_t row = row0 + (int64_t)j * wgs * ROWS;

@@ -441,8 +441,7 @@ __device__ __forceinline__ void f32_dkv(char* smem, const FParams& p, const FStr
 
 template <int LANES>
 __global__ __launch_bounds__(256) void attn_packed_f32_dsum_kernel(FParams p) {
-    if (pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p))
-        dsum_rows<LANES>(p, (int)blockIdx.x, (int)gridDim.x, 0);
+    dsum_rows<LANES>(p, (int)blockIdx.x, (int)gridDim.x, 0);
 }
 
 // Two workgroups share a compute unit up to head size 64 (see attn_f32.hip); wider heads need more than 256 registers.

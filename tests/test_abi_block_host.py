@@ -77,3 +77,48 @@ def test_the_generator_of_the_definition():
     assert block_ref.philox([0] * 4, [0] * 2) == [0x6627E8D5, 0xE169C58D, 0xBC57AC4C, 0x9B00DBD8]
     assert block_ref.philox([0xFFFFFFFF] * 4, [0xFFFFFFFF] * 2) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
     assert block_ref.philox([0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344], [0xA4093822, 0x299F31D0]) == [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
+
+
+# Entry points that are called without ctypes: the same arguments, and what is not one of them.
+def test_arguments_that_are_none():
+    lib = pkg.load_library()
+    call = lib.tp_layer_dropout_workspace_bytes
+    assert call(8, 64) > 0 and call(True, 64) > 0
+    for bad in ((8,), (8, 64, 1), ()):
+        with pytest.raises(TypeError):
+            call(*bad)
+    for bad in ((8.5, 64), ("8", 64), (None, 64)):
+        with pytest.raises(TypeError):
+            call(*bad)
+    with pytest.raises(OverflowError):
+        call(1 << 63, 64)
+    plan = (2, 100, AT, 4, 2, True, AT)
+    with pytest.raises(OverflowError):
+        pkg.tp_layer_pack_plan(*plan, plan_bytes=-1)
+    with pytest.raises(OverflowError):
+        pkg.tp_layer_pack_plan(2, 100, AT, 1 << 31, 2, True, AT, plan_bytes=0)
+    with pytest.raises(TypeError):
+        pkg.tp_layer_pack_plan(2, 100, "offsets", 4, 2, True, AT, plan_bytes=0)
+
+
+class _Tensor:
+    """Something with an address: aligned or not."""
+
+    def __init__(self, address):
+        self.address, self.nbytes = address, 0
+
+    def data_ptr(self):
+        return self.address
+
+
+class _Stream:
+    cuda_stream = 0
+
+
+def test_tensors_and_streams_are_pointers():
+    for stream in (None, 0, _Stream(), _Stream()):
+        def rc(offsets, plan, stream=stream):
+            return pkg.tp_layer_pack_plan(2, 100, offsets, 4, 2, True, plan, stream=stream, check=False)
+        assert rc(_Tensor(AT), _Tensor(AT)) == pkg.TPL_EWORKSPACE          # of no bytes
+        assert rc(_Tensor(AT), _Tensor(AT + 8)) == pkg.TPL_EALIGN and rc(_Tensor(AT + 2), _Tensor(AT)) == pkg.TPL_EALIGN
+        assert rc(_Tensor(0), _Tensor(AT)) == pkg.TPL_EINVAL and rc(None, AT) == pkg.TPL_EINVAL
