@@ -474,6 +474,7 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
             const Row w = row_of(p, r);
             rl = r < rows ? p.lse[s.row0 + (int64_t)w.q * p.nq + w.g] * LOG2E : 0.0f;
             rd = r < rows ? p.dsum[s.row0 + (int64_t)w.q * p.nq + w.g] : 0.0f;
+            if (WIN) rd = -rd;                             // the sums of dP begin with it
         }
     };
     auto r2s = [&](int stage) {
@@ -528,9 +529,17 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
         bf16x8 fr[NF];
 #pragma unroll
         for (int i = 0; i < NF; ++i) fr[i] = lds_frag_k<OFF>(ka[i]);
+        x = zero16();
+        if constexpr (DK_ROLE && WIN) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 d = lds_f4(terms + decltype(stg)::value * 2 * PACK_TILE * 4 + decltype(sbc)::value * 128 + i * 32);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[4 * i + j] = d[j];
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(1);
-        x = zero16();
 #pragma unroll
         for (int i = 0; i < NF; ++i) x = MFMA(fr[i], own[i], x);
         __builtin_amdgcn_s_setprio(0);
@@ -555,12 +564,12 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             pr[i] = *reinterpret_cast<const f32x4*>(pbuf + SB * 4 * P_BYTES + i * 1024);
-            d[i] = lds_f4(terms + STG * 2 * PACK_TILE * 4 + SB * 128 + i * 32);
+            if (!WIN) d[i] = lds_f4(terms + STG * 2 * PACK_TILE * 4 + SB * 128 + i * 32);
         }
         bf16x8 fr[NF];
         fetch_t(stg, sbc, fr);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = pr[v >> 2][v & 3] * (x[v] - d[v >> 2][v & 3]);
+        for (int v = 0; v < 16; ++v) x[v] = pr[v >> 2][v & 3] * (WIN ? x[v] : x[v] - d[v >> 2][v & 3]);
         collect(fr);
     };
     // A sub-tile of 32 rows: all of it in the dV role; dP, after the rest of the sub-tile before, in the dK role.
@@ -710,6 +719,13 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
     }
     settle(l2);
     settle(dsum);
+    constexpr bool LESS = WIN && DH != 64;                 // the sums of dP begin with -D; at 64 there are 128 registers, and none for that
+    f32x16 less_d = zero16();
+    if constexpr (LESS) {
+#pragma unroll
+        for (int v = 0; v < 16; ++v) less_d[v] = -dsum;
+        keep_in_register(less_d);
+    }
     dma_wait();
     __syncthreads();
     bf16x8 qf[NF], dof[NF];
@@ -745,7 +761,7 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
 #pragma unroll
             for (int i = 0; i < 2 * NF; ++i) {
                 if (i < NF) x = MFMA(fr[i % W], qf[i], x);
-                else dp = MFMA(fr[i % W], dof[i - NF], dp);
+                else dp = MFMA(fr[i % W], dof[i - NF], LESS && i == NF ? less_d : dp);
                 fr[i % W] = fetch(i + W);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -761,7 +777,7 @@ __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStri
                 for (int v = 0; v < 16; ++v) x[v] = (v >> 2) * 8 + (v & 3) >= from || (v >> 2) * 8 + (v & 3) < stay ? x[v] : -INFINITY;
             }
 #pragma unroll
-            for (int v = 0; v < 16; ++v) dp[v] = fast_exp2(fmaf(x[v], c2, -l2)) * (dp[v] - dsum);
+            for (int v = 0; v < 16; ++v) dp[v] = fast_exp2(fmaf(x[v], c2, -l2)) * (LESS ? dp[v] : dp[v] - dsum);
             const bf16x8 g[2] = {pack_regs(dp, 0), pack_regs(dp, 8)};
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
@@ -874,11 +890,11 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
         ft.init(p.dh, n);
         ft.load(p, s, s.q, s.ld, qt, stage, wave);
         ft.load(p, s, dobase, s.ldo, qt, stage + TB, wave);
-        if (n < 2 * PACK_TILE) {                           // LSE of the tile's rows, then D
+        if (n < 2 * PACK_TILE) {                           // LSE of the tile's rows, then -D, which the sums of dP begin with
             const int r = qt * PACK_TILE + (n & (PACK_TILE - 1));
             const Row w = row_of(p, r);
             const int64_t at = s.row0 + (int64_t)w.q * p.nq + w.g;
-            rl = r >= rows ? 0.0f : n < PACK_TILE ? p.lse[at] * LOG2E : p.dsum[at];
+            rl = r >= rows ? 0.0f : n < PACK_TILE ? p.lse[at] * LOG2E : -p.dsum[at];
         }
     };
     auto r2s = [&](int stage) {
@@ -927,7 +943,13 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
 #pragma unroll
         for (int i = 0; i < W; ++i) fr[i] = fetch(i);
         __builtin_amdgcn_sched_barrier(0);
-        f32x16 x = zero16(), dp = zero16();
+        f32x16 x = zero16(), dp;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const f32x4 d = lds_f4(terms + STG * 2 * PACK_TILE * 4 + PACK_TILE * 4 + SB * 128 + i * 32);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) dp[4 * i + j] = d[j];
+        }
 #pragma unroll
         for (int i = 0; i < 2 * NF; ++i) {
             if (i < NF) x = MFMA(fr[i % W], kf[i], x);
@@ -946,11 +968,11 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const f32x4 l = lds_f4(terms + STG * 2 * PACK_TILE * 4 + SB * 128 + i * 32), d = lds_f4(terms + STG * 2 * PACK_TILE * 4 + PACK_TILE * 4 + SB * 128 + i * 32);
+            const f32x4 l = lds_f4(terms + STG * 2 * PACK_TILE * 4 + SB * 128 + i * 32);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 x[4 * i + j] = fast_exp2(fmaf(x[4 * i + j], c2, -l[j]));
-                dp[4 * i + j] = x[4 * i + j] * (dp[4 * i + j] - d[j]);
+                dp[4 * i + j] *= x[4 * i + j];
             }
         }
         const bf16x8 g[2] = {pack_regs(x, 0), pack_regs(x, 8)}, h[2] = {pack_regs(dp, 0), pack_regs(dp, 8)};
@@ -1051,6 +1073,10 @@ __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStr
     }
     settle(l2);
     settle(dsum);
+    f32x16 less_d;                                         // the sums of dP begin with -D
+#pragma unroll
+    for (int v = 0; v < 16; ++v) less_d[v] = -dsum;
+    keep_in_register(less_d);
     dma_wait();
     __syncthreads();
     bf16x8 qf[NF], dof[NF];
@@ -1071,9 +1097,9 @@ __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStr
 #pragma unroll
         for (int i = 0; i < NF; ++i) { fr[2 * i] = lds_frag_k<OFF>(ka[i]); fr[2 * i + 1] = lds_frag_k<OFF + TB>(ka[i]); }
         __builtin_amdgcn_sched_barrier(0);
-        f32x16 x = zero16(), dp = zero16();
+        f32x16 x = zero16(), dp;
 #pragma unroll
-        for (int i = 0; i < NF; ++i) { x = MFMA(fr[2 * i], qf[i], x); dp = MFMA(fr[2 * i + 1], dof[i], dp); }
+        for (int i = 0; i < NF; ++i) { x = MFMA(fr[2 * i], qf[i], x); dp = MFMA(fr[2 * i + 1], dof[i], i == 0 ? less_d : dp); }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int k = 0; k < NF; ++k) fr[k] = k & 1 ? lds_frag_t<OFF + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF>(ta[k >> 1][0], ta[k >> 1][1]);
@@ -1089,7 +1115,7 @@ __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStr
             for (int v = 0; v < 16; ++v) x[v] = (v >> 2) * 8 + (v & 3) >= from || (v >> 2) * 8 + (v & 3) < stay ? x[v] : -INFINITY;
         }
 #pragma unroll
-        for (int v = 0; v < 16; ++v) dp[v] = fast_exp2(fmaf(x[v], c2, -l2)) * (dp[v] - dsum);
+        for (int v = 0; v < 16; ++v) dp[v] *= fast_exp2(fmaf(x[v], c2, -l2));
         const bf16x8 g[2] = {pack_regs(dp, 0), pack_regs(dp, 8)};
 #pragma unroll
         for (int k = 0; k < NF; ++k) dq[k >> 1] = MFMA(fr[k], g[k & 1], dq[k >> 1]);
