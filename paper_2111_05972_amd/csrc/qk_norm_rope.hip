@@ -196,7 +196,7 @@ __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormPa
     request();
     angles_of(p, cs, m0, n);
     __syncthreads();
-    while (true) {                                                  // one way for the whole workgroup: the groups' first heads lie in order
+    while (true) {
         float r[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
@@ -374,9 +374,9 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
         const int e = i % (2 * E), slot = i / (2 * E) & (lanes - 1), side = i / (2 * E * lanes), el = place(slot, e);
         if (slot >= p.slots || el >= p.dh) continue;
         const float* from = (side ? sums_k : sums) + e * stride + slot;
-        float v = 0.0f;
+        double v = 0.0;                                             // up to 512 of them, see row_sums.h
         for (int g = 0; g < p.rows_at_once * p.at_once; ++g) v += from[g * lanes];
-        part[((int64_t)blockIdx.x * 2 + side) * p.dh + el] = v;
+        part[((int64_t)blockIdx.x * 2 + side) * p.dh + el] = (float)v;
     }
 }
 
