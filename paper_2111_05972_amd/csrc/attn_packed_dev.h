@@ -154,28 +154,29 @@ template <int DH> constexpr int dsum_lanes() { return DH <= 32 ? 4 : DH <= 64 ? 
 template <int LANES, typename T>
 __device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int wg, int wgs, int above) {
     constexpr int ROWS = 256 / LANES, AHEAD = 4;
-    const int c = (threadIdx.x % LANES) * 8;
-    const int64_t all = (int64_t)p.M * p.nq;
+    const int c = (threadIdx.x % LANES) * 8, mine = threadIdx.x / LANES;
+    const int64_t all = (int64_t)p.M * p.nq, step = (int64_t)wgs * ROWS;
     bool ours = false;
-    for (int64_t row0 = (int64_t)wg * ROWS + threadIdx.x / LANES; row0 < all; row0 += (int64_t)wgs * ROWS * AHEAD) {
+    for (int64_t first = (int64_t)wg * ROWS; first < all; first += AHEAD * step) {
         bool wanted[AHEAD];
         float x[AHEAD][8], y[AHEAD][8];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int64_t row = row0 + (int64_t)j * wgs * ROWS;
+            const int64_t row = first + j * step + mine;
             wanted[j] = row < all && p.plan[p.seen + (unsigned)row / (unsigned)p.nq] > above;
         }
         if (!ours && !(ours = pack_matches(reinterpret_cast<const PackHeader*>(p.plan + p.header), p))) return;
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int64_t row = row0 + (int64_t)j * wgs * ROWS;
+            const int64_t at = (first + j * step + mine) * p.dh + c;
             if (wanted[j] && c < p.dh) {
-                load8(p.o + row * p.dh + c, x[j]);
-                load8(p.d_o + row * p.dh + c, y[j]);
+                load8(p.o + at, x[j]);
+                load8(p.d_o + at, y[j]);
             }
         }
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
+            if (first + j * step >= all) break;                   // uniform
             float a = 0.0f;
             if (wanted[j] && c < p.dh) {
 #pragma unroll
@@ -183,7 +184,7 @@ __device__ __forceinline__ void dsum_rows(const PackParams<T>& p, int wg, int wg
             }
 #pragma unroll
             for (int off = LANES / 2; off > 0; off >>= 1) a += __shfl_xor(a, off, 64);
-            if (wanted[j] && c == 0) p.dsum[row0 + (int64_t)j * wgs * ROWS] = a;
+            if (wanted[j] && c == 0) p.dsum[first + j * step + mine] = a;
         }
     }
 }

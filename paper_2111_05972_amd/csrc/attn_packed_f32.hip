@@ -24,11 +24,25 @@ using FParams = PackParams<float>;
 using FStrip = Strip<float>;
 constexpr int QUARTERS = PACK_BLK / XT;
 
-// Of the 32-row tiles that an item counts, with a window without those it leaves out: the first key of tile t, and how many there are up to key `seen`.
-template <bool WIN> __device__ __forceinline__ int xfirst(const FParams& p, const FStrip& s, int t) {
-    return WIN ? (t & 1) * XT + tile_of(p, s, t >> 1) * PACK_TILE : t * XT;
-}
-template <bool WIN> __device__ __forceinline__ int xtiles(const FParams& p, const FStrip& s, int seen) { return (seen + XT - 1) / XT - (WIN ? 2 * s.it.skip : 0); }
+// The 32-key tiles of an item that rows of queries q_lo .. q_hi see (`seen`: the first key that none of them does): number i begins with key at(i).  With a window those of
+// the first keys, then those of the window: an item's 64-key tiles are a strip's, four times as many rows.
+template <bool WIN> struct XTiles {
+    int n, first, second, from;           // tiles; first ones; where the others begin, counted as the item does
+    const FParams& p;
+    const FStrip& s;
+    __device__ __forceinline__ XTiles(const FParams& p_, const FStrip& s_, int q_lo, int seen) : p(p_), s(s_) {
+        const int t0 = 2 * s.it.tile0, nt = min(2 * s.it.tile1, (seen + XT - 1) / XT - (WIN ? 2 * s.it.skip : 0));
+        first = WIN ? max(0, min(nt, (p.sinks + XT - 1) / XT) - t0) : 0;
+        second = WIN ? max(t0 + first, max(0, q_lo + 1 - p.window) / XT - 2 * s.it.skip) : t0;
+        from = t0;
+        n = first + max(0, nt - second);
+    }
+    __device__ __forceinline__ int at(int i) const {
+        if (!WIN) return (from + i) * XT;
+        const int t = i < first ? from + i : second + i - first;
+        return (t & 1) * XT + tile_of(p, s, t >> 1) * PACK_TILE;
+    }
+};
 // 32 rows of K or V from row `row0` on: zero past the sequence.
 __device__ __forceinline__ i32x4 xtile_rsrc(const float* base, int64_t ld, int row0, int rows, int dh) {
     const int left = rows - row0 < XT ? rows - row0 : XT;
@@ -120,19 +134,20 @@ __global__ __launch_bounds__(256) void attn_packed_f32_fwd_kernel(FParams p) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[d][v] = 0.0f;
     float m = -INFINITY, l = 0.0f;
-    const int t0 = 2 * s.it.tile0, seen = p.mask != PACK_ALL ? q_hi + 1 : len, nt = min(2 * s.it.tile1, xtiles<WIN>(p, s, seen));
+    const XTiles<WIN> tiles(p, s, q_lo, p.mask != PACK_ALL ? q_hi + 1 : len);
+    const int nt = tiles.n;
     char* kt_ = smem + wave * 2 * TB;
     const unsigned lk = (unsigned)(uintptr_t)(lds_void_ptr)kt_, lv = lk + TB;
     unsigned off[NL];
     xoffsets<DH>(off, s.ld, p.dh, lane);
-    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? xfirst<WIN>(p, s, t) : len, len, p.dh), lds, off, 0, s.ld); };
-    if (t0 + mine < nt) { fetch(s.k, lk, t0 + mine); fetch(s.v, lv, t0 + mine); }
-    for (int t = t0 + mine; t < nt; t += step) {
+    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? tiles.at(t) : len, len, p.dh), lds, off, 0, s.ld); };
+    if (mine < nt) { fetch(s.k, lk, mine); fetch(s.v, lv, mine); }
+    for (int t = mine; t < nt; t += step) {
         xwait<NL>();                                              // K of this tile (V is younger)
         f32x16 x = xscores<DH>(kt_, qr, lane);
         xreads_done();
         fetch(s.k, lk, t + step);                                    // past the last tile: zeros, so that the count of loads in flight stays
-        const int k0 = xfirst<WIN>(p, s, t);
+        const int k0 = tiles.at(t);
         const bool edge = k0 + XT > len || (p.mask != PACK_ALL && k0 + XT - 1 > q_lo) || (WIN && k0 < q_hi + 1 - p.window);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
@@ -248,19 +263,20 @@ __device__ __forceinline__ void f32_dq(char* smem, const FParams& p, const FStri
     for (int d = 0; d < DH / 32; ++d)
 #pragma unroll
         for (int v = 0; v < 16; ++v) acc[d][v] = 0.0f;
-    const int t0 = 2 * s.it.tile0, seen = p.mask != PACK_ALL ? q_hi + 1 : len, nt = min(2 * s.it.tile1, xtiles<WIN>(p, s, seen));
+    const XTiles<WIN> tiles(p, s, q_lo, p.mask != PACK_ALL ? q_hi + 1 : len);
+    const int nt = tiles.n;
     unsigned off[NL];
     xoffsets<DH>(off, s.ld, p.dh, lane);
-    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? xfirst<WIN>(p, s, t) : len, len, p.dh), lds, off, 0, s.ld); };
-    if (t0 + mine < nt) { fetch(s.v, lv, t0 + mine); fetch(s.k, lk, t0 + mine); }   // V is read first
-    for (int t = t0 + mine; t < nt; t += step) {
+    auto fetch = [&](const float* base, unsigned lds, int t) { xfetch<DH>(xtile_rsrc(base, s.ld, t < nt ? tiles.at(t) : len, len, p.dh), lds, off, 0, s.ld); };
+    if (mine < nt) { fetch(s.v, lv, mine); fetch(s.k, lk, mine); }   // V is read first
+    for (int t = mine; t < nt; t += step) {
         xwait<NL>();
         f32x16 dp = xscores<DH>(kt_ + TB, gr, lane);              // dP^T = V dO^T
         xreads_done();
         fetch(s.v, lv, t + step);
         xwait<NL>();
         const f32x16 x = xscores<DH>(kt_, qr, lane);
-        const int k0 = xfirst<WIN>(p, s, t);
+        const int k0 = tiles.at(t);
         const bool edge = k0 + XT > len || (p.mask != PACK_ALL && k0 + XT - 1 > q_lo) || (WIN && k0 < q_hi + 1 - p.window);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
