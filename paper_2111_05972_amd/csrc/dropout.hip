@@ -8,6 +8,8 @@
 //
 // A workgroup has a strip of columns and some rows, a thread eight columns and every so many rows, four of them requested at once.  Sums
 // of dbias stay in registers until the workgroup's rows are through, are joined in LDS and left for row_sums.h: no atomics.
+// Bound by memory: 4096 rows of 12288 in bf16 with bias and residual, 302 MB in 55 us (5.5 TB/s); backward 201 MB in 40 (5.0) and 4.8 for the sums.  The generator's 20 products of
+// 32 x 32 bits for eight elements are half to two thirds of the vector units' time beside that.  4001 rows of 1280 in float 41 MB in 9.1 us and 9.6; 64 x 1024 3 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

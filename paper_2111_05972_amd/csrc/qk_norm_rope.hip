@@ -3,10 +3,14 @@
 // and backward, with g = turn back(dy) and everything worked out again from x:
 //   dx = rstd (g gamma - xh mean(g gamma xh)),  dgamma = sum of g xh over rows (and heads, where one row of weights is for all)
 //
-// Bound by memory.  A group of 1 to 64 neighbouring lanes has a head of a row, a lane two units of 16 bytes of it: the two places of the pairs that it turns,
-// or neighbours where a pair lies in one unit.  Where the halves of a rotation are not whole units, a head's values go through LDS to their partners.  Sums
-// over a head take log2(lanes) steps inside the wavefront.  A group keeps its head over the rows of its workgroup, with gamma and the sums of dgamma in
-// registers; angles as in rope.hip, one per (token, pair) for all heads.  dgamma: sums of a workgroup in LDS, then row_sums.h; no atomics.
+// Bound by memory, with vector work close behind (80 % of the vector units' time: widening, the norm and the rotation are about ten operations an element).  A
+// group of 1 to 64 neighbouring lanes has a head of a row, a lane two units of it: the two places of the pairs that it turns, or any two where a pair lies in
+// one unit; units of neighbouring lanes are neighbours (units of a lane side by side took 46.8 us instead of 34.1 in float).  A unit is 16 bytes, or 8 or 4 where the
+// halves of a rotation are no multiple of that; where these are not even, a head's values go through LDS to their partners.  Sums over a head take log2(lanes) steps
+// inside the wavefront.  Angles are one per (token, pair) for all heads, through LDS.  Backward: a group keeps its head over the rows of its workgroup, with gamma and the
+// sums of dgamma in registers; a workgroup's sums are joined in LDS and left for row_sums.h: no atomics.
+// 8192 tokens in bf16: 12 + 2 x 12 heads of 128, forward 151 MB in 25.6 us (5.9 TB/s), backward 201 MB in 39.7 (5.1) and 4.6 for the sums; 32 + 2 x 8 heads, weights for each head,
+// 201 MB in 39 (5.1) and 285 MB in 53 (5.4).  3001 tokens in float, 32 + 2 x 8 heads of 80: 92 MB in 19 us (4.9) and 130 MB in 24.8 (5.3).  64 tokens: 4 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,27 +39,41 @@ struct NormParams {
     int per_head;
 };
 
+// A unit: E elements of T, 16 bytes, or 8 or 4 where the halves of a rotation are no multiple of that.
 template <typename T> constexpr int unit() { return 16 / sizeof(T); }
-typedef unsigned raw_t __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void widen(const raw_t& u, float (&v)[8]) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(u[i] << 16); v[2 * i + 1] = __uint_as_float(u[i] & 0xffff0000u); }
+template <int WORDS> struct RawOf { typedef unsigned type __attribute__((ext_vector_type(WORDS))); };
+template <> struct RawOf<1> { typedef unsigned type; };
+template <typename T, int E> using Raw = typename RawOf<E * sizeof(T) / 4>::type;
+template <typename R> __device__ __forceinline__ unsigned word(const R& u, int i) {
+    if constexpr (sizeof(R) == 4) return u;
+    else return u[i];
 }
-__device__ __forceinline__ void widen(const raw_t& u, float (&v)[4]) {
+template <typename T, int E> __device__ __forceinline__ void widen(const Raw<T, E>& u, float (&v)[E]) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(u[i]);
+        for (int i = 0; i < E; ++i) v[i] = __uint_as_float(word(u, i));
+    } else {
+#pragma unroll
+        for (int i = 0; i < E / 2; ++i) { v[2 * i] = __uint_as_float(word(u, i) << 16); v[2 * i + 1] = __uint_as_float(word(u, i) & 0xffff0000u); }
+    }
 }
-__device__ __forceinline__ raw_t narrow(const float (&v)[8]) {
-    raw_t u;
+template <typename T, int E> __device__ __forceinline__ Raw<T, E> narrow(const float (&v)[E]) {
+    constexpr int WORDS = E * sizeof(T) / 4;
+    unsigned w[WORDS];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-        u[i] = (unsigned)__builtin_bit_cast(unsigned short, (bf16_t)v[2 * i]) | ((unsigned)__builtin_bit_cast(unsigned short, (bf16_t)v[2 * i + 1]) << 16);
+    for (int i = 0; i < WORDS; ++i)
+        w[i] = sizeof(T) == 4 ? __float_as_uint(v[i])
+                              : (unsigned)__builtin_bit_cast(unsigned short, (bf16_t)v[2 * i % E]) | ((unsigned)__builtin_bit_cast(unsigned short, (bf16_t)v[(2 * i + 1) % E]) << 16);
+    Raw<T, E> u;
+    if constexpr (WORDS == 1) u = w[0];
+    else
+#pragma unroll
+        for (int i = 0; i < WORDS; ++i) u[i] = w[i];
     return u;
 }
-__device__ __forceinline__ raw_t narrow(const float (&v)[4]) { return raw_t{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])}; }
 
 // The compiler is to widen again what it has widened before: 8 registers of a row kept instead of 16.
-__device__ __forceinline__ void again(raw_t& u) { asm volatile("" : "+v"(u)); }
+template <typename R> __device__ __forceinline__ void again(R& u) { asm volatile("" : "+v"(u)); }
 
 // Sums over aligned groups of `lanes` lanes (a power of two), in all of them.
 template <int CTRL> __device__ __forceinline__ float add_dpp(float x) { return x + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xf, 0xf, true)); }
@@ -90,17 +108,17 @@ __device__ __forceinline__ float2 angle(double where, double freq, float factor,
 }
 
 // What a lane has of a head.
-template <typename T, int MODE>
+template <int MODE, int E>
 struct Slot {
-    static constexpr int E = unit<T>();
     int number, a, b;                                             // its two units begin at elements a and b
     bool turned, has_a, has_b;
     __device__ __forceinline__ Slot(const NormParams& p, int slot) {
         const int half = p.rot / 2, turning = MODE == HALVES ? half / E : 0;
         number = slot;
         turned = MODE == HALVES && slot < turning;
-        a = MODE == HALVES && !turned ? p.rot + (slot - turning) * 2 * E : slot * (turned ? E : 2 * E);
-        b = turned ? a + half : a + E;
+        // neighbouring lanes have neighbouring units, so that a load or store of theirs is one piece
+        a = MODE == HALVES && !turned ? p.rot + (slot - turning) * E : slot * E;
+        b = a + (turned ? half : (p.slots - turning) * E);
         has_a = slot < p.slots;
         has_b = has_a && b < p.dh;
     }
@@ -164,12 +182,13 @@ template <typename T> __device__ __forceinline__ const T* weights_of(const NormP
 }
 
 // Forward: a group takes every so many heads of its workgroup's rows, AHEAD of them at a time, whose loads are out before the angles are worked out.
-template <typename T, int MODE>
+template <typename T, int MODE, int E>
 __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormParams p, const T* x, T* out, const T* gamma_q, const T* gamma_k) {
-    constexpr int E = unit<T>(), AHEAD = 4;
+    using raw_t = Raw<T, E>;
+    constexpr int AHEAD = 4;
     extern __shared__ __attribute__((aligned(16))) float2 cs[];                       // [token][angle], then APART: [group][dh] floats
     const int group = threadIdx.x / p.lanes, groups = FWD_THREADS / p.lanes;
-    const Slot<T, MODE> s(p, threadIdx.x & (p.lanes - 1));
+    const Slot<MODE, E> s(p, threadIdx.x & (p.lanes - 1));
     const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.row_heads * p.dh;
     const int n = (int)(p.M - m0 < p.tokens ? p.M - m0 : p.tokens);
     float* const mine = reinterpret_cast<float*>(cs + p.tokens * p.angles) + group * p.dh;
@@ -183,7 +202,7 @@ __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormPa
             tk[j] = token;
             hd[j] = head;
             const T* from = x + (m0 + token) * row + (int64_t)head * p.dh;
-            xr[j][0] = xr[j][1] = raw_t{0u, 0u, 0u, 0u};
+            xr[j][0] = xr[j][1] = raw_t{};
             if (token < n) {
                 if (s.has_a) xr[j][0] = *reinterpret_cast<const raw_t*>(from + s.a);
                 if (s.has_b) xr[j][1] = *reinterpret_cast<const raw_t*>(from + s.b);
@@ -201,8 +220,8 @@ __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormPa
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
             float x0[E], x1[E];
-            widen(xr[j][0], x0);
-            widen(xr[j][1], x1);
+            widen<T, E>(xr[j][0], x0);
+            widen<T, E>(xr[j][1], x1);
             r[j] = 0.0f;
 #pragma unroll
             for (int e = 0; e < E; ++e) r[j] = fmaf(x0[e], x0[e], fmaf(x1[e], x1[e], r[j]));
@@ -217,20 +236,20 @@ __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormPa
             raw_t o0 = xr[j][0], o1 = xr[j][1];
             if (hd[j] < p.normed) {
                 const T* w = weights_of(p, gamma_q, gamma_k, hd[j]);
-                const float rstd = 1.0f / sqrtf(fmaf(r[j], p.inv_dh, p.eps));
+                const float rstd = rsqrtf(fmaf(r[j], p.inv_dh, p.eps));
                 float x0[E], x1[E], g0[E], g1[E];
-                widen(s.has_a ? *reinterpret_cast<const raw_t*>(w + s.a) : raw_t{0u, 0u, 0u, 0u}, g0);
-                widen(s.has_b ? *reinterpret_cast<const raw_t*>(w + s.b) : raw_t{0u, 0u, 0u, 0u}, g1);
-                widen(xr[j][0], x0);
-                widen(xr[j][1], x1);
+                widen<T, E>(s.has_a ? *reinterpret_cast<const raw_t*>(w + s.a) : raw_t{}, g0);
+                widen<T, E>(s.has_b ? *reinterpret_cast<const raw_t*>(w + s.b) : raw_t{}, g1);
+                widen<T, E>(xr[j][0], x0);
+                widen<T, E>(xr[j][1], x1);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
                     x0[e] = x0[e] * rstd * g0[e];
                     x1[e] = x1[e] * rstd * g1[e];
                 }
                 s.turn(p, x0, x1, cs + tk[j] * p.angles, mine);
-                o0 = narrow(x0);
-                o1 = narrow(x1);
+                o0 = narrow<T, E>(x0);
+                o1 = narrow<T, E>(x1);
             }
             T* to = out + (m0 + tk[j]) * row + (int64_t)hd[j] * p.dh;
             if (s.has_a) __builtin_nontemporal_store(o0, reinterpret_cast<raw_t*>(to + s.a));
@@ -242,12 +261,12 @@ __global__ __launch_bounds__(FWD_THREADS, 4) void qk_norm_rope_fwd_kernel(NormPa
 }
 
 // Backward: a group keeps its head over the rows of its workgroup, with gamma and the sums of dgamma in registers.
-template <typename T, int MODE>
-__global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParams p, const T* x, const T* up, T* out, const T* gamma_q, const T* gamma_k, float* part) {
-    constexpr int E = unit<T>();
+template <typename T, int MODE, int E>
+__global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormParams p, const T* x, const T* up, T* out, const T* gamma_q, const T* gamma_k, float* part) {
+    using raw_t = Raw<T, E>;
     extern __shared__ __attribute__((aligned(16))) float2 cs[];                       // [token][angle], then floats
     const int t = threadIdx.x, threads = blockDim.x, lanes = p.lanes, group = t / lanes;
-    const Slot<T, MODE> s(p, t & (lanes - 1));
+    const Slot<MODE, E> s(p, t & (lanes - 1));
     const int row_lane = group / p.at_once, head_lane = group - row_lane * p.at_once;
     const bool has_a = s.has_a && row_lane < p.rows_at_once, has_b = s.has_b && row_lane < p.rows_at_once;
     const int64_t m0 = (int64_t)blockIdx.x * p.tokens, row = (int64_t)p.row_heads * p.dh;
@@ -257,12 +276,12 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
     const int stride = threads + 1, each = p.at_once * lanes;
     float* const sums_k = sums + 2 * E * stride;
     float* const mine = sums_k + group * p.dh;                                        // APART: this group's head
-    struct Raw { raw_t x[2], up[2]; };
-    Raw one;
-    auto request = [&](Raw& r, int h, int k, int end) __attribute__((always_inline)) {
+    struct Both { raw_t x[2], up[2]; };
+    Both one;
+    auto request = [&](Both& r, int h, int k, int end) __attribute__((always_inline)) {
         const bool in = k < end && h < p.heads, wanted = in && h < p.normed;
         const int64_t at = (m0 + k) * row + (int64_t)h * p.dh;
-        r.x[0] = r.x[1] = r.up[0] = r.up[1] = raw_t{0u, 0u, 0u, 0u};
+        r.x[0] = r.x[1] = r.up[0] = r.up[1] = raw_t{};
         if (wanted && has_a) r.x[0] = *reinterpret_cast<const raw_t*>(x + at + s.a);
         if (wanted && has_b) r.x[1] = *reinterpret_cast<const raw_t*>(x + at + s.b);
         if (in && has_a) r.up[0] = *reinterpret_cast<const raw_t*>(up + at + s.a);
@@ -282,7 +301,7 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
 #pragma unroll
     for (int e = 0; e < E; ++e) d0[e] = d1[e] = 0.0f;
     auto place = [&](int slot, int e) {                             // element of the head that is number e of the slot
-        const Slot<T, MODE> o(p, slot);
+        const Slot<MODE, E> o(p, slot);
         return e < E ? o.a + e : o.b + e - E;
     };
     bool left = false;
@@ -290,7 +309,7 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
     for (int h0 = 0; h0 < p.heads; h0 += p.at_once) {
         const int h = h0 + head_lane;
         const bool normed = h < p.normed;
-        raw_t w0 = {0u, 0u, 0u, 0u}, w1 = w0;
+        raw_t w0{}, w1{};
         if (!p.per_head && h >= p.nq && !left) { leave(sums); left = true; }
         if (normed) {
             const T* w = weights_of(p, gamma_q, gamma_k, h);
@@ -304,15 +323,15 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
                 angles_of(p, cs, m0 + c0, end - c0);
                 __syncthreads();
             }
-            auto work = [&](Raw& r, int k) __attribute__((always_inline)) {
+            auto work = [&](Both& r, int k) __attribute__((always_inline)) {
                 float v0[E], v1[E], sum[2] = {0.0f, 0.0f};          // dy turned back; sums of x^2 and g gamma x
-                widen(r.up[0], v0);
-                widen(r.up[1], v1);
+                widen<T, E>(r.up[0], v0);
+                widen<T, E>(r.up[1], v1);
                 s.turn(p, v0, v1, cs + (min(k, end - 1) - c0) * p.angles, mine);
                 auto add = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E]) __attribute__((always_inline)) {
                     float x[E], g[E];
-                    widen(xraw, x);
-                    widen(w, g);
+                    widen<T, E>(xraw, x);
+                    widen<T, E>(w, g);
 #pragma unroll
                     for (int e = 0; e < E; ++e) { sum[0] = fmaf(x[e], x[e], sum[0]); sum[1] = fmaf(v[e] * g[e], x[e], sum[1]); }
                 };
@@ -325,18 +344,18 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
                 again(w1);
                 raw_t o0 = r.up[0], o1 = r.up[1];
                 if (normed && k < end) {
-                    const float rstd = 1.0f / sqrtf(fmaf(sum[0], p.inv_dh, p.eps)), c = rstd * sum[1] * p.inv_dh;
+                    const float rstd = rsqrtf(fmaf(sum[0], p.inv_dh, p.eps)), c = rstd * sum[1] * p.inv_dh;
                     auto finish = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E], float (&d)[E]) __attribute__((always_inline)) {
                         float x[E], g[E];
-                        widen(xraw, x);
-                        widen(w, g);
+                        widen<T, E>(xraw, x);
+                        widen<T, E>(w, g);
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
                             const float u = x[e] * rstd;
                             d[e] = fmaf(v[e], u, d[e]);
                             x[e] = rstd * fmaf(v[e], g[e], -u * c);
                         }
-                        return narrow(x);
+                        return narrow<T, E>(x);
                     };
                     o0 = finish(r.x[0], w0, v0, d0);
                     o1 = finish(r.x[1], w1, v1, d1);
@@ -383,20 +402,19 @@ __global__ __launch_bounds__(MAX_THREADS) void qk_norm_rope_bwd_kernel(NormParam
 // Workgroups of backward, each of which leaves sums: two to a compute unit at most.
 int64_t tokens_each(int64_t M) { const int64_t groups = 2 * (int64_t)compute_units(); return (M + groups - 1) / groups; }
 
-template <typename T, int MODE>
+template <typename T, int MODE, int E>
 hipError_t launch_fwd(const QkNormArgs& a, NormParams& p) {
     // heads of a group: one batch, fewer where units would be left without rows
     const int groups = FWD_THREADS / p.lanes;
     const int64_t most = std::max(1, FWD_HEADS * groups / p.heads), spread = (a.M + 4 * compute_units() - 1) / (4 * compute_units());
     p.tokens = (int)std::min<int64_t>(std::min(most, spread), std::max(1, ANGLES / p.angles));
     const size_t lds = (size_t)p.tokens * p.angles * sizeof(float2) + (MODE == APART ? (size_t)groups * a.dh * sizeof(float) : 0);
-    hipLaunchKernelGGL((qk_norm_rope_fwd_kernel<T, MODE>), dim3((unsigned)((a.M + p.tokens - 1) / p.tokens)), dim3(FWD_THREADS), lds, a.stream, p, (const T*)a.qkv,
+    hipLaunchKernelGGL((qk_norm_rope_fwd_kernel<T, MODE, E>), dim3((unsigned)((a.M + p.tokens - 1) / p.tokens)), dim3(FWD_THREADS), lds, a.stream, p, (const T*)a.qkv,
                        (T*)a.out, (const T*)a.gamma_q, (const T*)a.gamma_k);
     return hipGetLastError();
 }
-template <typename T, int MODE>
+template <typename T, int MODE, int E>
 hipError_t launch_bwd(const QkNormArgs& a, NormParams& p) {
-    constexpr int E = unit<T>();
     // Threads, heads at a time and rows at a time: as many lanes at work as there may be, and few rows more than two workgroups to a unit leave each.
     // A third of the lanes idle costs 6 % (8192 tokens, 32 + 2 x 8 heads of 128: 62 -> 58 us with 512 instead of 384 threads), a quarter more rows a quarter (12 + 2 x 12 heads: 39 -> 48).
     const int64_t spread = tokens_each(a.M);
@@ -421,27 +439,36 @@ hipError_t launch_bwd(const QkNormArgs& a, NormParams& p) {
     const dim3 grid((unsigned)((a.M + p.tokens - 1) / p.tokens));
     const size_t apart = MODE == APART ? (size_t)(threads / p.lanes) * a.dh * sizeof(float) : 0, sums = (size_t)(2 * E * (threads + 1)) * sizeof(float);
     const size_t lds = (size_t)p.chunk * p.angles * sizeof(float2) + sums + std::max(apart, a.per_head ? 0 : sums);
-    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&qk_norm_rope_bwd_kernel<T, MODE>), hipFuncAttributeMaxDynamicSharedMemorySize, 112 << 10);
+    static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&qk_norm_rope_bwd_kernel<T, MODE, E>), hipFuncAttributeMaxDynamicSharedMemorySize, 112 << 10);
     if (attr != hipSuccess) return attr;
-    hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, MODE>), grid, dim3((unsigned)threads), lds, a.stream, p, (const T*)a.qkv, (const T*)a.dqkv, (T*)a.out,
+    hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, MODE, E>), grid, dim3((unsigned)threads), lds, a.stream, p, (const T*)a.qkv, (const T*)a.dqkv, (T*)a.out,
                        (const T*)a.gamma_q, (const T*)a.gamma_k, (float*)a.ws);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     const int64_t cols = (a.per_head ? p.normed : 2) * (int64_t)a.dh;
     return row_sums<T>(grid.x, cols, (a.per_head ? a.nq : 1) * (int64_t)a.dh, (const float*)a.ws, a.dgamma_q, a.dgamma_k, a.stream);
 }
-template <typename T, int MODE>
+template <typename T, int MODE, int E>
 hipError_t launch(const QkNormArgs& a, NormParams& p, bool bwd) {
-    constexpr int E = unit<T>();
-    p.slots = MODE == HALVES ? a.rot / 2 / E + ((a.dh - a.rot) / E + 1) / 2 : (a.dh + 2 * E - 1) / (2 * E);
+    const int turning = MODE == HALVES ? a.rot / 2 / E : 0;
+    p.slots = MODE == HALVES ? turning + ((a.dh - a.rot) / E + 1) / 2 : (a.dh + 2 * E - 1) / (2 * E);
     for (p.lanes = 1; p.lanes < p.slots; p.lanes *= 2) {}
     p.angles = MODE == NEIGHBOURS ? p.slots * E : a.rot / 2;
-    return bwd ? launch_bwd<T, MODE>(a, p) : launch_fwd<T, MODE>(a, p);
+    return bwd ? launch_bwd<T, MODE, E>(a, p) : launch_fwd<T, MODE, E>(a, p);
 }
 template <typename T>
 hipError_t run(const QkNormArgs& a, NormParams& p, bool bwd) {
-    if (a.adjacent) return launch<T, NEIGHBOURS>(a, p, bwd);
-    return a.rot % (2 * unit<T>()) == 0 ? launch<T, HALVES>(a, p, bwd) : launch<T, APART>(a, p, bwd);
+    constexpr int W = unit<T>();
+    if (a.adjacent) return launch<T, NEIGHBOURS, W>(a, p, bwd);
+    const int half = a.rot / 2;
+    if (half % W == 0) return launch<T, HALVES, W>(a, p, bwd);
+    // Smaller units as long as a wavefront has lanes enough for a head of them: bf16, 8192 tokens, 32 + 2 x 8 heads of 104 turned whole, both directions, 145 us through
+    // LDS and 79 in units of 8 bytes.  Of 4 bytes: heads of 32 turned by 4 53 and 38, of 64 by 12 68 and 63, but of 80 by 20 88 and 104, of 256 by 20 191 and 260 (forward
+    // 37 and 39, 77 and 66).
+    if (half % (W / 2) == 0 && a.dh <= 64 * W) return launch<T, HALVES, W / 2>(a, p, bwd);
+    if constexpr (W == 8)
+        if (half % 2 == 0 && a.dh <= (bwd ? 64 : 256)) return launch<T, HALVES, 2>(a, p, bwd);
+    return launch<T, APART, W>(a, p, bwd);
 }
 }  // namespace
 
