@@ -10,7 +10,7 @@
 // inside the wavefront.  Angles are one per (token, pair) for all heads, through LDS.  Backward: a group keeps its head over the rows of its workgroup, with gamma and the
 // sums of dgamma in registers; a workgroup's sums are joined in LDS and left for row_sums.h: no atomics.
 // 8192 tokens in bf16: 12 + 2 x 12 heads of 128, forward 151 MB in 25.6 us (5.9 TB/s), backward 201 MB in 39.7 (5.1) and 4.6 for the sums; 32 + 2 x 8 heads, weights for each head,
-// 201 MB in 39 (5.1) and 285 MB in 53 (5.4).  3001 tokens in float, 32 + 2 x 8 heads of 80: 92 MB in 19 us (4.9) and 130 MB in 24.8 (5.3).  64 tokens: 4 us, a launch.
+// neighbouring pairs, 201 MB in 32.7 (6.2) and 285 MB in 50.8 (5.6).  3001 tokens in float, 32 + 2 x 8 heads of 80: 92 MB in 19 us (4.9) and 130 MB in 24.8 (5.3).  64 tokens: 4 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
