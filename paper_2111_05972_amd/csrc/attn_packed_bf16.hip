@@ -441,7 +441,7 @@ __device__ __forceinline__ void dq_rows_again(float* q_s, const Params& p, const
 // dV; w + 4 works out dP and accumulates dK from the same probabilities, which it gets through LDS in float one sub-tile of 32 rows
 // later.  Tiles of 64 flattened rows: Q, LSE and D through three stages, as dK still reads the tile before, dO through two.
 // Bound by LDS: every 32 keys read the tile of Q and of dO twice, 256 KiB and 64 of P against four products of 64 x 128 x 128, and the three kinds of work
-// add up: 2.75 us a tile, 0.78 PFLOP/s over the chip.  12 documents of 8192 tokens, 16 / 2 heads of 128: 334 workgroups of 128 us, before those of dQ.
+// add up: 2.75 us a tile, 0.78 PFLOP/s over the chip.  Taken where strips are few, and up to head size 64 where they are long (see small_pays).
 constexpr int WAVES8 = 512;
 constexpr int P_BYTES = 32 * 32 * 4;
 template <int DH> constexpr int dkv_lds() { return 5 * tile_bytes<DH>() + 3 * 2 * PACK_TILE * 4 + 2 * 4 * P_BYTES; }
@@ -678,7 +678,7 @@ __device__ __forceinline__ void dkv_body(char* smem, const Params& p, const BStr
 // ---- dQ ---------------------------------------------------------------------------------------------------------------
 // Workgroup = (128 flattened rows, key head), 8 wavefronts: w takes 32 rows (w % 4) and one 32-key half (w / 4) of every tile; the
 // halves are added through LDS at the end.  Transposed score tile: lane = row.  1.18 us a tile, 1.36 PFLOP/s over the chip, and about 6 us to begin and
-// end a strip (item 0.9, loads 2.6 to 3.2, end 2.2): 1038 workgroups of 22 us in the batch above, both lists in one launch of 276 us.
+// end a strip (item 0.9, loads 2.6 to 3.2, end 2.2).
 template <int DH> constexpr int dq_lds() { return std::max(6 * tile_bytes<DH>(), 4 * 64 * (DH / 2) * 4); }
 template <int DH, int MASK>
 __device__ __forceinline__ void dq_body(char* smem, const Params& p, const BStrip& s) {
@@ -861,16 +861,56 @@ __global__ __launch_bounds__(WAVES8, DH <= 64 ? 4 : 2) void attn_packed_bwd_kern
     else dkv_body<DH, MASK, true>(smem, p, s);
 }
 
-// ---- backward where strips fill the chip, head sizes up to 64 ---------------------------------------------------------------
-// Four wavefronts to a strip, three workgroups to a unit.  A wavefront has 32 keys (32 rows) with both of their sums: it works out scores and dP once
-// and takes P and dS to dV and dK from its own registers, so that neither P goes through LDS nor a tile of dQ's sums is joined at the end.  Longer per
-// strip, as two wavefronts share that work above, hence for many strips only (see small_pays).
-// LDS: two stages of a tile pair (Q and dO, or K and V), 2 TB each, and 2 TB more; the strip's own rows lie in the second stage and behind it until they are in registers.
-template <int DH> constexpr int small_lds() { return 6 * tile_bytes<DH>() + 2 * 2 * PACK_TILE * 4; }
+// ---- backward where strips fill the chip ------------------------------------------------------------------------------------
+// Four wavefronts to a strip, two workgroups to a unit, three up to head size 64, whose steps do not wait for each other.  A wavefront has 32 keys (32 rows)
+// with both of their sums: it works out scores and dP once and takes P and dS to dV and dK from its own registers, so that neither P goes through LDS nor a
+// tile of dQ's sums is joined at the end.  Longer per strip, as two wavefronts share that work above, hence for many strips only (see small_pays).
+// Bound by the products, the softmax and the LDS reads of a step (at 128 67 fragments of 1 KB to 32 products), which two workgroups hide in part: 8192 tokens, 16 / 2 heads
+// of 128, causal, the whole pass 886 us instead of 989 in one document, 112 instead of 135 in 16, 75 instead of 98 in 512; 16384 with a window of 512, 8 heads, 180 instead of 215.
+// Registers: 128 of sums and 64 of K and V at head size 128 leave 64.  So three of K's eight fragments lie in LDS, read while scores and dP have no registers
+// yet, fragments of tiles come through a window of three, and addresses are worked out where they are read.  With 12 registers to memory, whose loads wait for
+// the requested tile as well, the pass above took 1150 us.
+// LDS: LSE and -D of the rows of two stages; two stages of a tile pair (Q and dO, or K and V), 2 TB each; up to head size 96 2 TB more, so that the strip's own
+// rows, which lie in the second stage and behind it until they are in registers, come with the first tile; else they take both stages before it.
+constexpr int SMALL_TERMS = 2 * 2 * PACK_TILE * 4;        // first, so that no offset of a read passes 64 KiB
+template <int DH> constexpr bool small_apart() { return DH <= 96; }
+template <int DH> constexpr int small_own() { return small_apart<DH>() ? 2 * tile_bytes<DH>() : 0; }
+template <int DH> constexpr int small_park() { return DH == 128 ? 3 : 0; }
+template <int DH> constexpr int small_lds() { return SMALL_TERMS + 4 * tile_bytes<DH>() + small_own<DH>() + WAVES4 * 16 * small_park<DH>(); }
+// Addresses of a wavefront's fragments in a stage: kept for all steps up to head size 96; at 128 worked out where they are read, from three that stay, as the
+// registers are taken.  Column 16 ks (32 dt) of a row of 256 bytes differs from column 0 in bits that the swizzle only flips.
+template <int DH> struct SmallFrags {
+    static constexpr bool KEPT = DH < 128;
+    static constexpr int NF = DH / 16, NT = DH / 32;
+    unsigned ka[KEPT ? NF : 1], ta[KEPT ? NT : 1][2];
+    __device__ __forceinline__ void init(unsigned at, int lane) {
+#pragma unroll
+        for (int ks = 0; ks < (KEPT ? NF : 1); ++ks) { ka[ks] = at + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
+#pragma unroll
+        for (int dt = 0; dt < (KEPT ? NT : 1); ++dt)
+#pragma unroll
+            for (int g = 0; g < 2; ++g) { ta[dt][g] = at + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(ta[dt][g]); }
+    }
+    // at ^ by, worked out here and not once for all steps; stages begin at multiples of 256 bytes
+    static __device__ __forceinline__ unsigned moved(unsigned at, unsigned by) {
+        unsigned x;
+        if (by == 0) return at;
+        asm volatile("v_xor_b32 %0, %1, %2" : "=v"(x) : "i"(by), "v"(at));
+        return x;
+    }
+    template <int OFF> __device__ __forceinline__ bf16x8 k(int ks) const {
+        if constexpr (KEPT) return lds_frag_k<OFF>(ka[ks]);
+        else return lds_frag_k<OFF>(moved(ka[0], (unsigned)ks * 32u));
+    }
+    template <int OFF> __device__ __forceinline__ bf16x8 t(int dt) const {
+        if constexpr (KEPT) return lds_frag_t<OFF>(ta[dt][0], ta[dt][1]);
+        else return lds_frag_t<OFF>(moved(ta[0][0], (unsigned)dt * 64u), moved(ta[0][1], (unsigned)dt * 64u));
+    }
+};
 template <int DH, int MASK>
 __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BStrip& s) {
     constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
-    constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2, TERMS = 6 * TB;
+    constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2, OWN = small_own<DH>();
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
     const int len = s.it.len, rows = s.rows, G = p.G;
@@ -881,7 +921,7 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
 #pragma unroll
     for (int dt = 0; dt < NT; ++dt) { dk[dt] = zero16(); dv[dt] = zero16(); }
     const int qt0 = s.it.tile0, ntiles = s.it.tile1;
-    const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem;
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_void_ptr)smem + SMALL_TERMS;
     float rl = 0.0f;
     auto g2r = [&](int qt, unsigned stage) {
         int n = t;                                         // what follows from it is worked out for every tile again: kept, it spilled the loop
@@ -898,32 +938,44 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
         }
     };
     auto r2s = [&](int stage) {
-        if (t < 2 * PACK_TILE) reinterpret_cast<float*>(smem + TERMS)[stage * 2 * PACK_TILE + t] = rl;
+        if (t < 2 * PACK_TILE) reinterpret_cast<float*>(smem)[stage * 2 * PACK_TILE + t] = rl;
     };
-    unsigned ka[NF], ta[NT][2];
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
-#pragma unroll
-    for (int dt = 0; dt < NT; ++dt)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) { ta[dt][g] = lds0 + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(ta[dt][g]); }
-    const unsigned terms = lds0 + TERMS + half * 16;
-    g2r(qt0, lds0);
-    r2s(0);
+    SmallFrags<DH> frags;
+    frags.init(lds0, lane);
+    const unsigned terms = lds0 - SMALL_TERMS + half * 16;
+    if constexpr (small_apart<DH>()) {
+        g2r(qt0, lds0);
+        r2s(0);
+    }
     {
         unsigned off[NCHUNKS<DH, WAVES4>];
         dma_offsets<DH, WAVES4>(off, s.ld, p.dh, t);
         for (int j = 0; j < 2; ++j) {
-            tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + (2 + j) * TB, off, 0, wave);
-            tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + (4 + j) * TB, off, 0, wave);
+            tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + OWN + j * TB, off, 0, wave);
+            tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, s.it.first + j * PACK_TILE, len, p.dh), lds0 + OWN + (2 + j) * TB, off, 0, wave);
         }
     }
     dma_wait();
     __syncthreads();
-    bf16x8 kf[NF], vf[NF];
-    strip_frags<DH>(kf, lds0 + 2 * TB, wave, lane);
-    strip_frags<DH>(vf, lds0 + 4 * TB, wave, lane);
+    constexpr int PARK = small_park<DH>();
+    bf16x8 kf[NF - PARK], vf[NF];
+    const unsigned park = lds0 + OWN + 4 * TB + wave * PARK * 1024 + lane * 16;
+    {
+        bf16x8 all[NF];
+        strip_frags<DH>(all, lds0 + OWN, wave, lane);
+#pragma unroll
+        for (int i = 0; i < NF; ++i)
+            if (i < PARK) *reinterpret_cast<__attribute__((address_space(3))) bf16x8*>((uintptr_t)(park + i * 1024)) = all[i];
+            else kf[i - PARK] = all[i];
+    }
+    strip_frags<DH>(vf, lds0 + OWN + 2 * TB, wave, lane);
     __syncthreads();                                       // the second stage is free
+    if constexpr (!small_apart<DH>()) {
+        g2r(qt0, lds0);
+        r2s(0);
+        dma_wait();
+        __syncthreads();
+    }
     const int see_lo = __builtin_amdgcn_readfirstlane(CAUSAL ? k0 * G - 31 : 0), see_hi = __builtin_amdgcn_readfirstlane(k0 >= len ? 0 : WIN && k0 >= p.sinks ? min(rows, (min(k0 + 31, len - 1) + p.window) * G) : rows);
     const int gone = WIN && k0 + 31 >= p.sinks ? __builtin_amdgcn_readfirstlane((max(k0, p.sinks) + p.window) * G) : 0x7fffffff;
     auto slot = [&](int qt, auto stg, auto sbc) __attribute__((always_inline)) {
@@ -931,35 +983,52 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
         const int qs0 = qt * PACK_TILE + SB * 32;
         if (qs0 < see_lo || qs0 >= see_hi) return;         // wavefront-uniform
         // the fragments of the four products (Q, dO, then both transposed) through a window of W: with NF of them the loop spilled
-        constexpr int W = NF > 2 ? NF / 2 : NF;
+        constexpr int W = DH > 64 ? 3 : NF > 2 ? NF / 2 : NF;
         bf16x8 fr[W];
         auto fetch = [&](int i) __attribute__((always_inline)) {       // i is a compile-time constant after unrolling
-            if (i < NF) return lds_frag_k<OFF>(ka[i]);
-            if (i < 2 * NF) return lds_frag_k<OFF + TB>(ka[i - NF]);
+            if (i < NF) return frags.template k<OFF>(i);
+            if (i < 2 * NF) return frags.template k<OFF + TB>(i - NF);
             const int k = i < 3 * NF ? i - 2 * NF : i - 3 * NF;
-            if (i < 3 * NF) return k & 1 ? lds_frag_t<OFF + TB + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF + TB>(ta[k >> 1][0], ta[k >> 1][1]);
-            return k & 1 ? lds_frag_t<OFF + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF>(ta[k >> 1][0], ta[k >> 1][1]);
+            if (i < 3 * NF) return k & 1 ? frags.template t<OFF + TB + 16 * DH * 2>(k >> 1) : frags.template t<OFF + TB>(k >> 1);
+            return k & 1 ? frags.template t<OFF + 16 * DH * 2>(k >> 1) : frags.template t<OFF>(k >> 1);
         };
 #pragma unroll
         for (int i = 0; i < W; ++i) fr[i] = fetch(i);
         __builtin_amdgcn_sched_barrier(0);
+        bf16x8 parked[PARK + 1];
+        unsigned from_park = park;
+        keep_in_register(from_park);                       // read for every slot, not kept
+#pragma unroll
+        for (int i = 0; i < PARK; ++i) parked[i] = *reinterpret_cast<lds_bf16x8_cptr>((uintptr_t)(from_park + i * 1024));
+        __builtin_amdgcn_sched_barrier(0);
         f32x16 x = zero16(), dp;
+        auto less_d = [&]() __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const f32x4 d = lds_f4(terms + STG * 2 * PACK_TILE * 4 + PACK_TILE * 4 + SB * 128 + i * 32);
+            for (int i = 0; i < 4; ++i) {
+                const f32x4 d = lds_f4(terms + STG * 2 * PACK_TILE * 4 + PACK_TILE * 4 + SB * 128 + i * 32);
 #pragma unroll
-            for (int j = 0; j < 4; ++j) dp[4 * i + j] = d[j];
-        }
+                for (int j = 0; j < 4; ++j) dp[4 * i + j] = d[j];
+            }
+        };
+        if (PARK == 0) less_d();
 #pragma unroll
         for (int i = 0; i < 2 * NF; ++i) {
-            if (i < NF) x = MFMA(fr[i % W], kf[i], x);
+            if (i < PARK) x = MFMA(fr[i % W], parked[i], x);
+            else if (i < NF) x = MFMA(fr[i % W], kf[i - PARK], x);
             else dp = MFMA(fr[i % W], vf[i - NF], dp);
             fr[i % W] = fetch(i + W);
             __builtin_amdgcn_sched_barrier(0);
+            if (PARK > 0 && i == NF - 2) {                 // as late as registers are short
+                less_d();
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
         if (qs0 + 31 >= rows || k0 + 31 >= len || (CAUSAL && (k0 + 31) * G > qs0) || (WIN && qs0 + 31 >= gone)) {   // wavefront-uniform: diagonal or an end
-            const int from = kv < len ? (CAUSAL ? kv * G : 0) - qs0 - 4 * half : 1 << 30;
-            const int to = (WIN && kv >= p.sinks ? min(rows, (min(kv, len) + p.window) * G) : rows) - qs0 - 4 * half;
+            int l = lane;
+            keep_in_register(l);                           // what follows from it is worked out here: kept, it spilled
+            const int key = k0 + (l & 31), first = qs0 + 4 * (l >> 5);
+            const int from = key < len ? (CAUSAL ? key * G : 0) - first : 1 << 30;
+            const int to = (WIN && key >= p.sinks ? min(rows, (min(key, len) + p.window) * G) : rows) - first;
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int r = 8 * (v >> 2) + (v & 3);
@@ -978,10 +1047,10 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
         const bf16x8 g[2] = {pack_regs(x, 0), pack_regs(x, 8)}, h[2] = {pack_regs(dp, 0), pack_regs(dp, 8)};
 #pragma unroll
         for (int k = 0; k < 2 * NF; ++k) {
-            if (k < NF) dv[k >> 1] = MFMA(fr[k % W], g[k & 1], dv[k >> 1]);
-            else dk[(k - NF) >> 1] = MFMA(fr[k % W], h[k & 1], dk[(k - NF) >> 1]);
+            if (k < NF) dv[k >> 1] = MFMA(fr[(2 * NF + k) % W], g[k & 1], dv[k >> 1]);
+            else dk[(k - NF) >> 1] = MFMA(fr[(2 * NF + k) % W], h[k & 1], dk[(k - NF) >> 1]);
             if (k + W < 2 * NF) {
-                fr[k % W] = fetch(2 * NF + k + W);
+                fr[(2 * NF + k) % W] = fetch(2 * NF + k + W);
                 __builtin_amdgcn_sched_barrier(0);
             }
         }
@@ -1038,7 +1107,7 @@ __device__ __forceinline__ void dkv_small(char* smem, const Params& p, const BSt
 template <int DH, int MASK>
 __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStrip& s) {
     constexpr bool CAUSAL = MASK != PACK_ALL, WIN = MASK == PACK_WINDOW;
-    constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2;
+    constexpr int TB = tile_bytes<DH>(), NF = DH / 16, NT = DH / 32, HALF = 32 * DH * 2, OWN = small_own<DH>();
     constexpr int NCH = NCHUNKS<DH, WAVES4>;
     const int t = threadIdx.x, lane = t & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(t >> 6);
@@ -1064,12 +1133,12 @@ __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStr
         tile_dma<DH, WAVES4>(tile_rsrc(s.k, s.ld, kt * PACK_TILE, len, p.dh), stage, off, 0, wave);
         tile_dma<DH, WAVES4>(tile_rsrc(s.v, s.ld, kt * PACK_TILE, len, p.dh), stage + TB, off, 0, wave);
     };
-    fetch_tile(tile0, lds0);
+    if constexpr (small_apart<DH>()) fetch_tile(tile0, lds0);
     FlatTile<DH, WAVES4> ft;
     ft.init(p.dh, t);
     for (int j = 0; j < 2; ++j) {
-        ft.load(p, s, s.q, s.ld, s.it.first / PACK_TILE + j, lds0 + (2 + j) * TB, wave);
-        ft.load(p, s, dobase, s.ldo, s.it.first / PACK_TILE + j, lds0 + (4 + j) * TB, wave);
+        ft.load(p, s, s.q, s.ld, s.it.first / PACK_TILE + j, lds0 + OWN + j * TB, wave);
+        ft.load(p, s, dobase, s.ldo, s.it.first / PACK_TILE + j, lds0 + OWN + (2 + j) * TB, wave);
     }
     settle(l2);
     settle(dsum);
@@ -1080,29 +1149,36 @@ __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStr
     dma_wait();
     __syncthreads();
     bf16x8 qf[NF], dof[NF];
-    strip_frags<DH>(qf, lds0 + 2 * TB, wave, lane);
-    strip_frags<DH>(dof, lds0 + 4 * TB, wave, lane);
+    strip_frags<DH>(qf, lds0 + OWN, wave, lane);
+    strip_frags<DH>(dof, lds0 + OWN + 2 * TB, wave, lane);
     __syncthreads();                                       // the second stage is free
-    unsigned ka[NF], ta[NT][2];
-#pragma unroll
-    for (int ks = 0; ks < NF; ++ks) { ka[ks] = lds0 + frag_k_off<DH>(0, ks, lane); keep_in_register(ka[ks]); }
-#pragma unroll
-    for (int dt = 0; dt < NT; ++dt)
-#pragma unroll
-        for (int g = 0; g < 2; ++g) { ta[dt][g] = lds0 + frag_t_off<DH>(dt * 32, 0, g, lane); keep_in_register(ta[dt][g]); }
+    if constexpr (!small_apart<DH>()) {
+        fetch_tile(tile0, lds0);
+        dma_wait();
+        __syncthreads();
+    }
+    SmallFrags<DH> frags;
+    frags.init(lds0, lane);
     auto slot = [&](int kv0, auto stg, auto sbc) __attribute__((always_inline)) {
         constexpr int OFF = decltype(stg)::value * 2 * TB + decltype(sbc)::value * HALF;
         if (kv0 >= kv_end || (WIN && kv0 + 32 <= q_lo + 1 - p.window && kv0 >= p.sinks)) return;   // wavefront-uniform
-        bf16x8 fr[2 * NF];
+        constexpr int H = NF > 6 ? 2 : 1;                     // fragments of a half of the head at a time where registers are short
+        bf16x8 fr[2 * NF / H];
 #pragma unroll
-        for (int i = 0; i < NF; ++i) { fr[2 * i] = lds_frag_k<OFF>(ka[i]); fr[2 * i + 1] = lds_frag_k<OFF + TB>(ka[i]); }
+        for (int i = 0; i < NF / H; ++i) { fr[2 * i] = frags.template k<OFF>(i); fr[2 * i + 1] = frags.template k<OFF + TB>(i); }
         __builtin_amdgcn_sched_barrier(0);
         f32x16 x = zero16(), dp;
 #pragma unroll
-        for (int i = 0; i < NF; ++i) { x = MFMA(fr[2 * i], qf[i], x); dp = MFMA(fr[2 * i + 1], dof[i], i == 0 ? less_d : dp); }
+        for (int i = 0; i < NF; ++i) {
+            constexpr int F = NF / H;
+            x = MFMA(fr[2 * (i % F)], qf[i], x);
+            if (i + F < NF) fr[2 * (i % F)] = frags.template k<OFF>(i + F);
+            dp = MFMA(fr[2 * (i % F) + 1], dof[i], i == 0 ? less_d : dp);
+            if (i + F < NF) { fr[2 * (i % F) + 1] = frags.template k<OFF + TB>(i + F); __builtin_amdgcn_sched_barrier(0); }
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int k = 0; k < NF; ++k) fr[k] = k & 1 ? lds_frag_t<OFF + 16 * DH * 2>(ta[k >> 1][0], ta[k >> 1][1]) : lds_frag_t<OFF>(ta[k >> 1][0], ta[k >> 1][1]);
+        for (int k = 0; k < NF; ++k) fr[k] = k & 1 ? frags.template t<OFF + 16 * DH * 2>(k >> 1) : frags.template t<OFF>(k >> 1);
         __builtin_amdgcn_sched_barrier(0);
         if (r0 + 31 >= s.rows || kv0 + 31 >= len || (CAUSAL && kv0 + 31 > q_lo)) {
             const int seen = valid ? min(CAUSAL ? me.q : len, len - 1) - kv0 - half * 4 : -1;
@@ -1155,8 +1231,8 @@ __device__ __forceinline__ void dq_small(char* smem, const Params& p, const BStr
 }
 
 template <int DH, int MASK>
-__global__ __launch_bounds__(WAVES4, 3) void attn_packed_bwd_small_kernel(Params p) {
-    extern __shared__ __attribute__((aligned(16))) char smem[];
+__global__ __launch_bounds__(WAVES4, DH <= 64 ? 3 : 2) void attn_packed_bwd_small_kernel(Params p) {
+    extern __shared__ __attribute__((aligned(256))) char smem[];
     const int of_kv = (int)min((unsigned)reinterpret_cast<const PackHeader*>(p.plan + p.header)->items[1], (unsigned)p.kv_items) * p.nkv, wg = blockIdx.x;
     BStrip s;
     if (wg >= of_kv) {
@@ -1165,11 +1241,15 @@ __global__ __launch_bounds__(WAVES4, 3) void attn_packed_bwd_small_kernel(Params
         dkv_small<DH, MASK>(smem, p, s);
     }
 }
-// By the tiles of rows that a strip of keys visits, as far as the host can tell (sequences of average length), and strips.  us, eight wavefronts and four, 8 heads of
-// 64 unless said otherwise: 64 sequences of 64 tokens, causal 23.6 and 20.2, of 128 without a mask 37.0 and 31.9, 512 of 16 98.5 and 76.6, 8 of 2048, causal 160 and
-// 148, a window of 256, 8 / 4 heads, 16384 tokens 78.9 and 61.7, 8192 tokens (256 strips) 47.7 and 48.8; but a window of 1500 174 and 193, 8 sequences of 2048 of 16 / 4 heads 325 and 349, one
-// of 8192 276 and 316.
+// Above head size 64 by strips, of both sides and with a part of one for every sequence.  us, eight wavefronts and four, causal, heads of 128: 2500 tokens, 4 / 1 heads 34 and
+// 37 in 4 sequences (107 strips), 17 and 20 in 100 (295); 1500, 16 / 2, 43 and 48 in 4 (206), 24 and 21 in 100 (411); 1500, 8 / 8, 30 and 31 in 4, 22 and 20 in 20 (347); 2500,
+// 16 / 2, 68 and 59 in 4 (359), 40 and 32 in 100; from 500 strips on 2 to 28 % less, but for 3500, 16 / 2, in 20, 51.5 and 53.4.
+// Up to 64, where two workgroups of eight wavefronts share a unit, by the tiles of rows that a strip of keys visits, as far as the host can tell (sequences of average length),
+// and strips.  8 heads of 64 unless said otherwise: 64 sequences of 64 tokens, causal 23.6 and 20.2, of 128 without a mask 37.0 and 31.9, 512 of 16 98.5 and 76.6, 8 of 2048,
+// causal 160 and 148, a window of 256, 8 / 4 heads, 16384 tokens 78.9 and 61.7, 8192 tokens (256 strips) 47.7 and 48.8; but a window of 1500 174 and 193, 8 sequences of 2048 of
+// 16 / 4 heads 325 and 349, one of 8192 276 and 316.
 bool small_pays(const PackAttnArgs& a) {
+    if (a.dh > 64) return 3 * (a.M * (a.nq + a.nkv) / PACK_BLK + a.sequences * a.nkv) >= 4 * compute_units();
     int64_t tokens = a.M / a.sequences;
     if (a.mask == PACK_WINDOW) tokens = std::min<int64_t>(tokens, (int64_t)a.window + PACK_BLK);
     const int64_t tiles = tokens * (a.nq / a.nkv) / PACK_TILE;
@@ -1206,12 +1286,12 @@ hipError_t run_bwd(const PackAttnArgs& a) {
     if (e != hipSuccess) return e;
     p.kv_items = (int)L.cap[1];
     const dim3 grid((unsigned)((L.cap[0] + L.cap[1]) * a.nkv));
-    bool small = false;
-    if constexpr (DH <= 64) {
-        small = small_pays(a);
-        if (small) hipLaunchKernelGGL((attn_packed_bwd_small_kernel<DH, MASK>), grid, dim3(WAVES4), small_lds<DH>(), a.stream, p);
-    }
-    if (!small) {
+    if (small_pays(a)) {
+        constexpr int lds = small_lds<DH>();
+        static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_bwd_small_kernel<DH, MASK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+        if (attr != hipSuccess) return attr;
+        hipLaunchKernelGGL((attn_packed_bwd_small_kernel<DH, MASK>), grid, dim3(WAVES4), lds, a.stream, p);
+    } else {
         constexpr int lds = std::max(dkv_lds<DH>(), dq_lds<DH>());
         static const hipError_t attr = hipFuncSetAttribute(reinterpret_cast<const void*>(&attn_packed_bwd_kernel<DH, MASK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds);
         if (attr != hipSuccess) return attr;
