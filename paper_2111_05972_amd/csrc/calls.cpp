@@ -2,7 +2,7 @@
 // about 1 us here and 4 to 5 there (argument by argument, and a method call of Python's for each pointer), against 3 to 5 us of the shortest kernels.
 //
 // open(path) looks the entry points up in the library at `path`; the functions have their names and take their arguments by place.  A pointer is None, an address, or
-// anything with data_ptr() (a tensor) or cuda_stream (a stream).  Numbers that do not fit their argument raise OverflowError.  Other threads run during a call.
+// anything with data_ptr() (a tensor) or cuda_stream (a stream), or what int() takes.  Numbers that do not fit their argument raise OverflowError.  Other threads run during a call.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
@@ -33,6 +33,19 @@ void* table[COUNT];
 PyObject *data_ptr_name, *cuda_stream_name;
 PyTypeObject* stream_type;      // of the last object that had no data_ptr(): asked for its stream at once
 
+// What int() takes (numpy's integers), or the value of a ctypes pointer, None included.
+PyObject* other_number(PyObject* o) {
+    PyObject* number = PyNumber_Long(o);
+    if (number) return number;
+    PyErr_Clear();
+    PyObject* value = PyObject_GetAttrString(o, "value");
+    if (value) {
+        number = value == Py_None ? PyLong_FromLong(0) : PyNumber_Index(value);
+        Py_DECREF(value);
+    }
+    if (!number) PyErr_Format(PyExc_TypeError, "a pointer is None, an address, a tensor or a stream, not %s", Py_TYPE(o)->tp_name);
+    return number;
+}
 bool address(PyObject* o, void** out) {
     if (o == Py_None) { *out = nullptr; return true; }
     PyObject* number = nullptr;
@@ -51,7 +64,8 @@ bool address(PyObject* o, void** out) {
                 Py_INCREF(Py_TYPE(o));
                 Py_XSETREF(stream_type, Py_TYPE(o));
             } else if (PyErr_ExceptionMatches(PyExc_AttributeError)) {
-                PyErr_Format(PyExc_TypeError, "a pointer is None, an address, a tensor or a stream, not %s", Py_TYPE(o)->tp_name);
+                PyErr_Clear();
+                number = other_number(o);
             }
         }
         if (!number) return false;
