@@ -11,6 +11,9 @@
 // grows with the length, so the rows of a batch may be any number of bytes.  A tile of Q and dO holds flattened rows; their
 // addresses come from a division by G of a number below 64 + G, one multiplication.
 //
+// With a window only the tiles that some row of a strip sees are visited (tile_of, pack_tiles), and only those at an edge of what is seen are masked.  Backward has
+// two forms, of eight wavefronts to a strip and of four (small_pays).
+//
 // Precision.  Probabilities and dS are rounded to bf16 as matrix operands, at every head size (attn_bf16.hip keeps them float at head sizes other than 64
 // and 128): each is off by at most 2^-8 of itself, and these roundings have no common sign.  Sums, statistics and D are float.
 // Against 64 bits o and dqkv are 1.4 times as far off as their rounding alone.
@@ -86,7 +89,8 @@ template <int DH> __device__ __forceinline__ void strip_frags(bf16x8 (&f)[DH / 1
 // ---- forward ----------------------------------------------------------------------------------------------------------
 // Workgroup = (128 flattened rows, key head), four wavefronts of 32 rows each, two workgroups to a unit; K and V in tiles of 64 through two LDS
 // stages.  Bound by what the products, the softmax and the LDS reads of a step take one after another: 16384 tokens in 3 documents, 12 / 4 heads of 128, causal
-// 389 us, 971 TFLOP/s (a library product of 8192^3 reaches 1370 to 1600); 12 documents of 8192 tokens, 16 / 2 heads 87 us.  Eight wavefronts, two to 32 rows with half of each tile's keys, halve the chain of dependent steps but read K and V by rows twice:
+// 389 us, 971 TFLOP/s (a library product of 8192^3 reaches 1370 to 1600); 12 documents of 8192 tokens, 16 / 2 heads 87 us.  32000 tokens
+// in 3, 12 / 4 heads, a window of 4096 and 16 first keys 677 us (1.0 PFLOP/s of the pairs that are seen); 16384 in 2, 8 / 4 heads of 64, a window of 256 26 us.  Eight wavefronts, two to 32 rows with half of each tile's keys, halve the chain of dependent steps but read K and V by rows twice:
 // where a unit has one strip they took -5 to +10 % of the time, where it has two up to 38 % more (4096 tokens of 32 to 800, 16 / 2 heads of 128).
 constexpr int WAVES4 = 256;
 template <int DH> constexpr int fwd_lds() { return 4 * tile_bytes<DH>(); }
