@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_math.h"
 #include "kernels.h"
@@ -135,14 +136,23 @@ struct Slot {
             }
         } else if constexpr (MODE == NEIGHBOURS) {
             if (!has_a) return;
+            // a pair past `rot` is left alone: turned by nothing, an infinity would make NaN of its partner
+            auto pairs = [&](auto whole, float (&v)[E], int at) __attribute__((always_inline)) {
 #pragma unroll
-            for (int e = 0; e < E / 2; ++e) {
-                const float2 r = w[a / 2 + e], s = w[b / 2 + e];
-                const float u = v0[2 * e], z = v1[2 * e];
-                v0[2 * e] = fmaf(u, r.x, -v0[2 * e + 1] * r.y);
-                v0[2 * e + 1] = fmaf(u, r.y, v0[2 * e + 1] * r.x);
-                v1[2 * e] = fmaf(z, s.x, -v1[2 * e + 1] * s.y);
-                v1[2 * e + 1] = fmaf(z, s.y, v1[2 * e + 1] * s.x);
+                for (int e = 0; e < E; e += 2) {
+                    const float2 r = w[(at + e) / 2];
+                    const float x = v[e], y = v[e + 1];
+                    const bool in = whole || at + e < p.rot;
+                    v[e] = in ? fmaf(x, r.x, -y * r.y) : x;
+                    v[e + 1] = in ? fmaf(x, r.y, y * r.x) : y;
+                }
+            };
+            if (p.rot == p.dh) {                                  // uniform
+                pairs(std::true_type{}, v0, a);
+                pairs(std::true_type{}, v1, b);
+            } else {
+                if (a < p.rot) pairs(std::false_type{}, v0, a);
+                if (b < p.rot) pairs(std::false_type{}, v1, b);
             }
         } else {
             // one wavefront writes and reads: what it has written is there once its LDS counter says so
