@@ -14,7 +14,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "device_math.h"
 #include "kernels.h"
@@ -26,7 +25,7 @@ namespace {
 constexpr int FWD_THREADS = 256, FWD_HEADS = 4;   // heads that a group of lanes takes
 constexpr int MAX_THREADS = 512;
 constexpr int ANGLES = 4096;            // (token, pair) values of a workgroup at most: 32 KiB of LDS
-enum Mode { HALVES = 0, NEIGHBOURS = 1, APART = 2 };     // APART: halves that are not whole units
+enum Mode { HALVES = 0, NEIGHBOURS = 1, APART = 2, NEIGHBOURS_SOME = 3 };     // APART: halves that are not whole units; SOME: not the whole head is turned
 
 struct NormParams {
     int64_t M, seq;
@@ -134,25 +133,18 @@ struct Slot {
                 v0[e] = fmaf(u, r.x, -v1[e] * r.y);
                 v1[e] = fmaf(u, r.y, v1[e] * r.x);
             }
-        } else if constexpr (MODE == NEIGHBOURS) {
+        } else if constexpr (MODE == NEIGHBOURS || MODE == NEIGHBOURS_SOME) {
             if (!has_a) return;
-            // a pair past `rot` is left alone: turned by nothing, an infinity would make NaN of its partner
-            auto pairs = [&](auto whole, float (&v)[E], int at) __attribute__((always_inline)) {
+            // SOME: a pair past `rot` is left alone, as an infinity turned by nothing would make NaN of its partner
 #pragma unroll
-                for (int e = 0; e < E; e += 2) {
-                    const float2 r = w[(at + e) / 2];
-                    const float x = v[e], y = v[e + 1];
-                    const bool in = whole || at + e < p.rot;
-                    v[e] = in ? fmaf(x, r.x, -y * r.y) : x;
-                    v[e + 1] = in ? fmaf(x, r.y, y * r.x) : y;
-                }
-            };
-            if (p.rot == p.dh) {                                  // uniform
-                pairs(std::true_type{}, v0, a);
-                pairs(std::true_type{}, v1, b);
-            } else {
-                if (a < p.rot) pairs(std::false_type{}, v0, a);
-                if (b < p.rot) pairs(std::false_type{}, v1, b);
+            for (int e = 0; e < E / 2; ++e) {
+                const float2 r = w[a / 2 + e], s = w[b / 2 + e];
+                const float u = v0[2 * e], x = v0[2 * e + 1], z = v1[2 * e], y = v1[2 * e + 1];
+                const bool one = MODE == NEIGHBOURS || a + 2 * e < p.rot, two = MODE == NEIGHBOURS || b + 2 * e < p.rot;
+                v0[2 * e] = one ? fmaf(u, r.x, -x * r.y) : u;
+                v0[2 * e + 1] = one ? fmaf(u, r.y, x * r.x) : x;
+                v1[2 * e] = two ? fmaf(z, s.x, -y * s.y) : z;
+                v1[2 * e + 1] = two ? fmaf(z, s.y, y * s.x) : y;
             }
         } else {
             // one wavefront writes and reads: what it has written is there once its LDS counter says so
@@ -463,13 +455,13 @@ hipError_t launch(const QkNormArgs& a, NormParams& p, bool bwd) {
     const int turning = MODE == HALVES ? a.rot / 2 / E : 0;
     p.slots = MODE == HALVES ? turning + ((a.dh - a.rot) / E + 1) / 2 : (a.dh + 2 * E - 1) / (2 * E);
     for (p.lanes = 1; p.lanes < p.slots; p.lanes *= 2) {}
-    p.angles = MODE == NEIGHBOURS ? p.slots * E : a.rot / 2;
+    p.angles = MODE == NEIGHBOURS || MODE == NEIGHBOURS_SOME ? p.slots * E : a.rot / 2;
     return bwd ? launch_bwd<T, MODE, E>(a, p) : launch_fwd<T, MODE, E>(a, p);
 }
 template <typename T>
 hipError_t run(const QkNormArgs& a, NormParams& p, bool bwd) {
     constexpr int W = unit<T>();
-    if (a.adjacent) return launch<T, NEIGHBOURS, W>(a, p, bwd);
+    if (a.adjacent) return a.rot == a.dh ? launch<T, NEIGHBOURS, W>(a, p, bwd) : launch<T, NEIGHBOURS_SOME, W>(a, p, bwd);
     const int half = a.rot / 2;
     if (half % W == 0) return launch<T, HALVES, W>(a, p, bwd);
     // Smaller units as long as a wavefront has lanes enough for a head of them: bf16, 8192 tokens, 32 + 2 x 8 heads of 104 turned whole, both directions, 145 us through
