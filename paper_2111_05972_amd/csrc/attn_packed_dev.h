@@ -29,7 +29,8 @@ struct PackParams {
 // Whether the plan at hand was made for this call.
 template <typename T>
 __device__ __forceinline__ bool pack_matches(const PackHeader* h, const PackParams<T>& p) {
-    return h->sequences == p.sequences && h->tokens == p.M && h->nq == p.nq && h->nkv == p.nkv && h->mask == p.mask && h->window == p.window && h->sinks == p.sinks;
+    // no word waits for the one before: behind && each was a load of its own
+    return ((h->sequences ^ p.sequences) | (h->tokens ^ p.M) | (h->nq ^ p.nq) | (h->nkv ^ p.nkv) | (h->mask ^ p.mask) | (h->window ^ p.window) | (h->sinks ^ p.sinks)) == 0;
 }
 // What a workgroup works on.
 template <typename T>
