@@ -51,8 +51,9 @@ struct PlanParams {
 };
 
 // Strip `i` of a sequence: its first row or key and its tiles.
-__device__ __forceinline__ PackTiles strip_of(const PlanParams& p, int side, int len, int i) {
-    return pack_tiles(p.mask, p.window, p.sinks, (unsigned)(p.nq / p.nkv), side, len, i * PACK_BLK);
+template <bool WIN> __device__ __forceinline__ int mask_of(const PlanParams& p) { return WIN ? PACK_WINDOW : p.mask == PACK_CAUSAL ? PACK_CAUSAL : PACK_ALL; }
+template <bool WIN> __device__ __forceinline__ PackTiles strip_of(const PlanParams& p, int side, int len, int i) {
+    return pack_tiles(mask_of<WIN>(p), p.window, p.sinks, (unsigned)(p.nq / p.nkv), side, len, i * PACK_BLK);
 }
 // Longest first, `top` above the longest.  Strips of up to LEVEL tiles, which memory bounds and not their length, stay in the order of the
 // rows: sorted, the units would all read the same part of every sequence at a time, and where lengths are equal and even those parts lie on the same channels
@@ -63,7 +64,8 @@ __device__ __forceinline__ int bucket_of(int tiles, int top) {
     return BUCKETS - 1 - min(BUCKETS - 1, (int)((float)max(tiles, LEVEL) * ((float)(BUCKETS - 1) / (float)top)));
 }
 
-__global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
+// WIN: with a window, whose questions took the others 0.4 to 0.6 us.
+template <bool WIN> __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
     __shared__ int tmp[PLAN_THREADS / 64];
     __shared__ int hist[2][BUCKETS];
     __shared__ int longest[2], slots[2], joins[2], first_short[2];
@@ -96,8 +98,8 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                 }
                 p.plan[m] = (int)m - begin[lo];
                 const int at = (int)m - begin[lo];
-                int seen = p.mask != PACK_ALL ? at + 1 : begin[lo + 1] - begin[lo];
-                if (p.mask == PACK_WINDOW) seen = min(seen, p.window) + min(p.sinks, max(0, seen - p.window));
+                int seen = WIN || p.mask != PACK_ALL ? at + 1 : begin[lo + 1] - begin[lo];
+                if (WIN) seen = min(seen, p.window) + min(p.sinks, max(0, seen - p.window));
                 p.plan[p.L.seen + m] = seen;
             }
             __syncthreads();
@@ -145,7 +147,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
         int most = 0;
         for (int k = t; k < carry[side]; k += PLAN_THREADS) {
             const int b = find(pre, k);
-            const PackTiles s = strip_of(p, side, start[b + 1] - start[b], k - pre[b]);
+            const PackTiles s = strip_of<WIN>(p, side, start[b + 1] - start[b], k - pre[b]);
             mine += (unsigned)(s.tile1 - s.tile0);
             most = max(most, s.tile1 - s.tile0);
         }
@@ -170,7 +172,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void pack_plan_kernel(PlanParams p) {
                 it.t0 = start[b];
                 it.len = start[b + 1] - start[b];
                 it.first = (k - pre[b]) * PACK_BLK;
-                const PackTiles s = strip_of(p, side, it.len, k - pre[b]);
+                const PackTiles s = strip_of<WIN>(p, side, it.len, k - pre[b]);
                 const int a = s.tile0, z = s.tile1;
                 it.skip = s.skip;
                 it.chunks = (z - a + chunk - 1) / chunk;
@@ -229,7 +231,7 @@ hipError_t pack_plan(int64_t sequences, int64_t M, const int* offsets, int nq, i
     p.L = pack_layout(sequences, M, nq, nkv, p.shares);
     static_assert(BUCKETS == PLAN_THREADS && NEAR > PLAN_THREADS, "a thread to a bucket, 1024 sequences and an end in LDS");
     const int64_t groups = std::min<int64_t>((M + PLAN_THREADS - 1) / PLAN_THREADS, 1024);
-    hipLaunchKernelGGL(pack_plan_kernel, dim3((unsigned)(1 + groups)), dim3(PLAN_THREADS), 0, s, p);
+    hipLaunchKernelGGL(mask == PACK_WINDOW ? pack_plan_kernel<true> : pack_plan_kernel<false>, dim3((unsigned)(1 + groups)), dim3(PLAN_THREADS), 0, s, p);
     return hipGetLastError();
 }
 
