@@ -13,6 +13,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_math.h"
 #include "kernels.h"
@@ -62,16 +63,20 @@ __device__ __forceinline__ void drop8(float (&v)[8], const Words& q, unsigned th
 template <typename T, bool BIAS, bool RESID, bool SUMS>
 __global__ __launch_bounds__(DT) void dropout_kernel(DropParams p, const T* in, const T* bias, const T* resid, T* out, float* part, T* dbias) {
     constexpr int AHEAD = 4;
-    __shared__ float red[SUMS ? DT : 1][9];
+    // Sums over rows.  Of float: four rows in 32 bits, from there on in 64, as a chain of a thread's rows (193 for 65536 rows of 12288) took dbias to ten times the
+    // error of one rounding.  Of bf16, which is off by up to 2^-8 of itself in the end: 32 bits.
+    using sum_t = std::conditional_t<sizeof(T) == 4, double, float>;
+    __shared__ sum_t red[SUMS ? DT : 1][9];
     const int t = threadIdx.x, lane = t / p.cu, c = t - lane * p.cu, unit = blockIdx.x * p.cu + c;
     const bool mine = lane < p.lanes && unit < p.units;
     const int64_t end = min(p.M, ((int64_t)blockIdx.y + 1) * p.rows);
-    float sum[8] = {}, b[8] = {};
+    sum_t sum[8] = {};
+    float b[8] = {};
     if (mine) {
         const unsigned long long seed = p.rng[0], step = p.rng[1];
         if (BIAS) load8(bias + 8 * unit, b);
         for (int64_t m0 = (int64_t)blockIdx.y * p.rows + lane; m0 < end; m0 += AHEAD * p.lanes) {
-            float v[AHEAD][8], r[AHEAD][8];
+            float v[AHEAD][8], r[AHEAD][8], some[8] = {};
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 const int64_t m = m0 + j * p.lanes;
@@ -92,9 +97,12 @@ __global__ __launch_bounds__(DT) void dropout_kernel(DropParams p, const T* in, 
                     for (int e = 0; e < 8; ++e) v[j][e] += r[j][e];
                 if (SUMS)
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) sum[e] += v[j][e];
+                    for (int e = 0; e < 8; ++e) some[e] += v[j][e];
                 store8_nt(out + m * p.N + 8 * unit, v[j]);
             }
+            if (SUMS)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) sum[e] += some[e];
         }
     }
     if constexpr (SUMS) {
@@ -104,10 +112,10 @@ __global__ __launch_bounds__(DT) void dropout_kernel(DropParams p, const T* in, 
         for (int i = t; i < 8 * p.cu; i += DT) {
             const int u = blockIdx.x * p.cu + i / 8;
             if (u >= p.units) break;
-            float s = red[i / 8][i % 8];
+            sum_t s = red[i / 8][i % 8];
             for (int l = 1; l < p.lanes; ++l) s += red[l * p.cu + i / 8][i % 8];
-            if (gridDim.y == 1) dbias[8 * u + i % 8] = from_f32<T>(s);
-            else part[(int64_t)blockIdx.y * p.N + 8 * u + i % 8] = s;
+            if (gridDim.y == 1) dbias[8 * u + i % 8] = from_f32<T>((float)s);
+            else part[(int64_t)blockIdx.y * p.N + 8 * u + i % 8] = (float)s;
         }
     }
 }
