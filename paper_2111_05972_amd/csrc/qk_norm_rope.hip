@@ -14,6 +14,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "device_math.h"
 #include "kernels.h"
@@ -291,17 +292,19 @@ __global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormPa
     };
     request(one, head_lane, row_lane, min(n, p.chunk));
     angles_of(p, cs, m0, min(n, p.chunk));
-    float d0[E], d1[E];
+    // sums of dgamma: of float in 64 bits (a chain of 400 rows in 32 took them to five times one rounding's error), of bf16, which is off by up to 2^-8 in the end, in 32
+    using sum_t = std::conditional_t<sizeof(T) == 4, double, float>;
+    sum_t d0[E], d1[E];
     auto leave = [&](float* to) __attribute__((always_inline)) {    // this thread's sums, and begin again
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-            to[e * stride + t] = d0[e];
-            to[(E + e) * stride + t] = d1[e];
-            d0[e] = d1[e] = 0.0f;
+            to[e * stride + t] = (float)d0[e];
+            to[(E + e) * stride + t] = (float)d1[e];
+            d0[e] = d1[e] = 0;
         }
     };
 #pragma unroll
-    for (int e = 0; e < E; ++e) d0[e] = d1[e] = 0.0f;
+    for (int e = 0; e < E; ++e) d0[e] = d1[e] = 0;
     auto place = [&](int slot, int e) {                             // element of the head that is number e of the slot
         const Slot<MODE, E> o(p, slot);
         return e < E ? o.a + e : o.b + e - E;
@@ -347,14 +350,15 @@ __global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormPa
                 raw_t o0 = r.up[0], o1 = r.up[1];
                 if (normed && k < end) {
                     const float rstd = rsqrtf(fmaf(sum[0], p.inv_dh, p.eps)), c = rstd * sum[1] * p.inv_dh;
-                    auto finish = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E], float (&d)[E]) __attribute__((always_inline)) {
+                    auto finish = [&](const raw_t& xraw, const raw_t& w, const float (&v)[E], sum_t (&d)[E]) __attribute__((always_inline)) {
                         float x[E], g[E];
                         widen<T, E>(xraw, x);
                         widen<T, E>(w, g);
 #pragma unroll
                         for (int e = 0; e < E; ++e) {
                             const float u = x[e] * rstd;
-                            d[e] = fmaf(v[e], u, d[e]);
+                            if constexpr (sizeof(T) == 4) d[e] += v[e] * u;
+                            else d[e] = fmaf(v[e], u, d[e]);
                             x[e] = rstd * fmaf(v[e], g[e], -u * c);
                         }
                         return narrow<T, E>(x);
@@ -380,9 +384,9 @@ __global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormPa
         for (int i = t; i < each * 2 * E; i += threads) {
             const int e = i % (2 * E), at = i / (2 * E), slot = at & (lanes - 1), head = h0 + at / lanes, el = place(slot, e);
             if (slot >= p.slots || head >= p.normed || el >= p.dh) continue;
-            float v = sums[e * stride + at];
+            sum_t v = sums[e * stride + at];
             for (int r = 1; r < p.rows_at_once; ++r) v += sums[e * stride + r * each + at];
-            part[((int64_t)blockIdx.x * p.normed + head) * p.dh + el] = v;
+            part[((int64_t)blockIdx.x * p.normed + head) * p.dh + el] = (float)v;
         }
         __syncthreads();
     }
