@@ -246,7 +246,7 @@ int tp_layer_slice_epilogue_bwd(int dtype, int act, int64_t M, int64_t N, const 
  * step mod 2^32, step / 2^32) and the key (seed mod 2^32, seed / 2^32) gives four words; u = 16 bits of word e / 2, the lower ones where e is even.
  * keep = u >= t, t = min(65535, floor(65536 p + 1/2)), scale = 65536 / (65536 - t).  What is dropped does not matter, infinities and NaN included.
  * p in [0, 1).  N, first_col and width multiples of 8, site < 2^20, M and width below 2^31, (first_row + M) width / 8 up to 2^44 (TPL_EUNSUPPORTED: others).
- * out may be in or resid itself, din may be dout, but they may not overlap otherwise (TPL_EINVAL).  rng 8-byte aligned.
+ * out may be in or resid itself, din may be dout; otherwise nothing that is written, dbias and ws among it, may overlap another tensor (TPL_EINVAL).  rng 8-byte aligned.
  * ws_bytes >= tp_layer_dropout_workspace_bytes(M, N). */
 int tp_layer_dropout_fwd(int dtype, int64_t M, int64_t N, double p, const uint64_t* rng, int64_t site, int64_t first_row, int64_t first_col,
                          int64_t width, const void* in, const void* bias, const void* resid, void* out, void* hip_stream);
@@ -341,7 +341,7 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
  *   backward: g = turn back(dqkv); dx = rstd (g gamma - x rstd mean_dh(g gamma x rstd)); dv is copied;  dgamma = sum g x rstd
  * gamma_q, dgamma_q, gamma_k, dgamma_k (dtype): [dh] for all heads, dgamma the sum over rows and heads; with per_head != 0 [nq, dh] and [nkv, dh], a
  * row for each head.  Backward takes the qkv of before the norm and works rstd out again.  out may be qkv itself (forward; the input of backward is then gone) or dqkv
- * itself (backward): then v is not touched; otherwise tensors may not overlap (TPL_EINVAL).  eps >= 0, finite.  Squares are summed in float.  M < 2^24, at most
+ * itself (backward): then v is not touched; otherwise nothing that is written, dgamma and ws among it, may overlap another tensor (TPL_EINVAL).  eps >= 0, finite.  Squares are summed in float.  M < 2^24, at most
  * 4096 heads of a kind, dh a multiple of 8 up to 512 (TPL_EUNSUPPORTED: others).  ws_bytes >= tp_layer_qk_norm_rope_workspace_bytes(...).
  * Results are deterministic. */
 int tp_layer_qk_norm_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, int pairs, const double* freq, float factor,

@@ -933,9 +933,19 @@ int tp_layer_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int rot, in
     return rope_call(true, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, dqkv, out, hip_stream);
 }
 
-static bool overlap(const void* a, const void* b, int64_t bytes) {
-    const uintptr_t lo = std::min((uintptr_t)a, (uintptr_t)b), hi = std::max((uintptr_t)a, (uintptr_t)b);
-    return hi - lo < (uintptr_t)bytes;
+// Memory that a call reads or writes; p: NULL where it is not passed.
+struct Span { const void* p; int64_t bytes; };
+static bool overlap(const Span& a, const Span& b) {
+    const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
+    return a.p && b.p && (x < y ? y - x < (uintptr_t)a.bytes : x - y < (uintptr_t)b.bytes);
+}
+// Whether one of `outs` overlaps another or one of `ins`.
+static bool any_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+    for (const Span* a = outs.begin(); a != outs.end(); ++a) {
+        for (const Span* b = a + 1; b != outs.end(); ++b) if (overlap(*a, *b)) return true;
+        for (const Span& b : ins) if (overlap(*a, b)) return true;
+    }
+    return false;
 }
 static int qk_norm_check(int dtype, int64_t M, int nq, int nkv, int dh) {
     if (dtype != TPL_F32 && dtype != TPL_BF16) return TPL_EINVAL;
@@ -960,7 +970,9 @@ int tp_layer_qk_norm_rope_fwd(int dtype, int64_t M, int nq, int nkv, int dh, int
     QkNormArgs a{};
     const int rc = qk_norm_args(a, dtype, M, nq, nkv, dh, rot, pairs, freq, factor, positions, seq, gamma_q, gamma_k, per_head, eps, qkv, out, hip_stream);
     if (rc) return rc;
-    if (qkv != out && overlap(qkv, out, M * ((int64_t)nq + 2 * nkv) * dh * (dtype == TPL_BF16 ? 2 : 4))) return TPL_EINVAL;
+    const int64_t es = dtype == TPL_BF16 ? 2 : 4, bytes = M * ((int64_t)nq + 2 * nkv) * dh * es, row = dh * es;
+    if (any_overlap({{out, bytes}}, {{qkv != out ? qkv : nullptr, bytes}, {freq, rot / 2 * 8}, {positions, 4 * M}, {gamma_q, per_head ? nq * row : row},
+                                     {gamma_k, per_head ? nkv * row : row}})) return TPL_EINVAL;
     return hip_rc(qk_norm_rope(a, false));
 }
 size_t tp_layer_qk_norm_rope_workspace_bytes(int dtype, int64_t M, int nq, int nkv, int dh) {
@@ -975,9 +987,12 @@ int tp_layer_qk_norm_rope_bwd(int dtype, int64_t M, int nq, int nkv, int dh, int
     if (!dqkv || !dgamma_q || !dgamma_k || !ws) return TPL_EINVAL;
     const void* ptrs[] = {dqkv, dgamma_q, dgamma_k, ws};
     for (const void* q : ptrs) if (misaligned(q)) return TPL_EALIGN;
-    const int64_t bytes = M * ((int64_t)nq + 2 * nkv) * dh * (dtype == TPL_BF16 ? 2 : 4);
-    if ((dqkv != out && overlap(dqkv, out, bytes)) || overlap(qkv, out, bytes)) return TPL_EINVAL;
-    if (ws_bytes < tp_layer_qk_norm_rope_workspace_bytes(dtype, M, nq, nkv, dh)) return TPL_EWORKSPACE;
+    const int64_t es = dtype == TPL_BF16 ? 2 : 4, bytes = M * ((int64_t)nq + 2 * nkv) * dh * es, row = dh * es, of_q = per_head ? nq * row : row, of_k = per_head ? nkv * row : row;
+    const size_t need = tp_layer_qk_norm_rope_workspace_bytes(dtype, M, nq, nkv, dh);
+    if (ws_bytes < need) return TPL_EWORKSPACE;
+    // dqkv where it is `out` itself stands there
+    if (any_overlap({{out, bytes}, {dgamma_q, of_q}, {dgamma_k, of_k}, {ws, (int64_t)need}},
+                    {{qkv, bytes}, {dqkv != out ? dqkv : nullptr, bytes}, {freq, rot / 2 * 8}, {positions, 4 * M}, {gamma_q, of_q}, {gamma_k, of_k}})) return TPL_EINVAL;
     a.dqkv = dqkv; a.dgamma_q = dgamma_q; a.dgamma_k = dgamma_k; a.ws = ws;
     return hip_rc(qk_norm_rope(a, true));
 }
@@ -1001,8 +1016,8 @@ int tp_layer_dropout_fwd(int dtype, int64_t M, int64_t N, double p, const uint64
     const int rc = dropout_args(a, dtype, M, N, p, rng, site, first_row, first_col, width, in, out, hip_stream);
     if (rc) return rc;
     if (misaligned(bias) || misaligned(resid)) return TPL_EALIGN;
-    const int64_t bytes = M * N * (dtype == TPL_BF16 ? 2 : 4);
-    if ((in != out && overlap(in, out, bytes)) || (resid && resid != out && overlap(resid, out, bytes))) return TPL_EINVAL;
+    const int64_t es = dtype == TPL_BF16 ? 2 : 4, bytes = M * N * es;
+    if (any_overlap({{out, bytes}}, {{in != out ? in : nullptr, bytes}, {resid != out ? resid : nullptr, bytes}, {bias, N * es}, {rng, 16}})) return TPL_EINVAL;
     a.bias = bias; a.resid = resid;
     return hip_rc(dropout(a));
 }
@@ -1017,8 +1032,10 @@ int tp_layer_dropout_bwd(int dtype, int64_t M, int64_t N, double p, const uint64
     if (rc) return rc;
     if (dbias && !ws) return TPL_EINVAL;
     if (misaligned(dbias) || misaligned(ws)) return TPL_EALIGN;
-    if (dout != din && overlap(dout, din, M * N * (dtype == TPL_BF16 ? 2 : 4))) return TPL_EINVAL;
-    if (dbias && ws_bytes < tp_layer_dropout_workspace_bytes(M, N)) return TPL_EWORKSPACE;
+    const size_t need = tp_layer_dropout_workspace_bytes(M, N);
+    if (dbias && ws_bytes < need) return TPL_EWORKSPACE;
+    const int64_t es = dtype == TPL_BF16 ? 2 : 4, bytes = M * N * es;
+    if (any_overlap({{din, bytes}, {dbias, N * es}, {dbias ? ws : nullptr, (int64_t)need}}, {{dout != din ? dout : nullptr, bytes}, {rng, 16}})) return TPL_EINVAL;
     a.dbias = dbias; a.ws = ws;
     return hip_rc(dropout(a));
 }
