@@ -1,9 +1,11 @@
-"""Binding of libtp_layer.so: same names as the C ABI, argument marshalling only (csrc/calls.cpp, and ctypes where arguments are structures).
+"""Binding of libtp_layer.so: same names as the C ABI, argument marshalling only (csrc/calls.cpp, and ctypes where arguments are structures
+or that module is not built for this Python).
 
 Device buffers are anything with a `.data_ptr()` (torch tensors) or plain integer addresses.
 There is no fallback: if the shared library is missing, loading raises.
 """
 import ctypes
+import operator
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -48,6 +50,46 @@ class TpLayerError(RuntimeError):
     def __init__(self, status, what):
         self.status = status
         super().__init__(f"{what}: {tp_layer_strerror(status)} (status {status})")
+
+
+# What csrc/calls.cpp takes for the arguments of a call, for ctypes where that module is not built.
+def _whole(lo, hi):
+    def take(x):
+        x = operator.index(x)
+        if not lo <= x <= hi:
+            raise OverflowError("a number does not fit its argument")
+        return x
+    return take
+
+
+def _address(x):
+    """None, an address, anything with data_ptr() (a tensor) or cuda_stream (a stream), what int() takes, or a ctypes pointer."""
+    if x is None or isinstance(x, int):
+        return x
+    if hasattr(x, "data_ptr"):
+        return x.data_ptr()
+    if hasattr(x, "cuda_stream"):
+        return x.cuda_stream
+    if isinstance(x, _vp):
+        return x.value
+    try:
+        return int(x)
+    except (TypeError, ValueError):
+        raise TypeError(f"a pointer is None, an address, a tensor or a stream, not {type(x).__name__}") from None
+
+
+_TAKES = {_vp: _address, ctypes.c_int: _whole(-2 ** 31, 2 ** 31 - 1), ctypes.c_int64: _whole(-2 ** 63, 2 ** 63 - 1), ctypes.c_size_t: _whole(0, 2 ** 63 - 1),
+          ctypes.c_float: lambda x: ctypes.c_float(x).value, ctypes.c_double: lambda x: ctypes.c_double(x).value}
+
+
+def _through_ctypes(fn):
+    takes = [_TAKES[a] for a in fn.argtypes]
+
+    def call(*args):
+        if len(args) != len(takes):
+            raise TypeError(f"{len(args)} arguments instead of {len(takes)}")
+        return fn(*[take(x) for take, x in zip(takes, args)])
+    return call
 
 
 _lib = None
@@ -131,16 +173,19 @@ def load_library():
     for name, (res, args) in sig.items():
         fn = getattr(lib, name)
         fn.restype, fn.argtypes = res, args
-    # Entry points that take numbers and pointers only: called from C, with the same arguments, at a quarter of the time.  Tensors and streams
-    # may be passed as they are.
+    # Entry points that take numbers and pointers only: called from C, with the same arguments, at a quarter of the time, where that module was built
+    # for this Python.  Tensors and streams may be passed as they are.
     try:
         from . import _calls
-    except ImportError as e:
-        raise ImportError("the module that calls the library is missing: build it with `python -m paper_2111_05972_amd.build`") from e
-    _calls.open(path)
-    for name in sig:
+    except ImportError:
+        _calls = None
+    else:
+        _calls.open(path)
+    for name, (_, args) in sig.items():
         if hasattr(_calls, name):
             setattr(lib, name, getattr(_calls, name))
+        elif _calls is None and name != "tp_layer_rope_frequencies" and all(a in _TAKES for a in args):     # that one fills an array of ctypes
+            setattr(lib, name, _through_ctypes(getattr(lib, name)))
     _lib = lib
     return lib
 
