@@ -53,9 +53,13 @@ class TpLayerError(RuntimeError):
 
 
 # What csrc/calls.cpp takes for the arguments of a call, for ctypes where that module is not built.
+def _value(x):
+    return x.value if isinstance(x, ctypes._SimpleCData) else x
+
+
 def _whole(lo, hi):
     def take(x):
-        x = operator.index(x)
+        x = operator.index(_value(x))
         if not lo <= x <= hi:
             raise OverflowError("a number does not fit its argument")
         return x
@@ -70,8 +74,8 @@ def _address(x):
         return x.data_ptr()
     if hasattr(x, "cuda_stream"):
         return x.cuda_stream
-    if isinstance(x, _vp):
-        return x.value
+    if isinstance(x, ctypes._SimpleCData):
+        return _address(x.value)
     try:
         return int(x)
     except (TypeError, ValueError):
@@ -79,7 +83,7 @@ def _address(x):
 
 
 _TAKES = {_vp: _address, ctypes.c_int: _whole(-2 ** 31, 2 ** 31 - 1), ctypes.c_int64: _whole(-2 ** 63, 2 ** 63 - 1), ctypes.c_size_t: _whole(0, 2 ** 63 - 1),
-          ctypes.c_float: lambda x: ctypes.c_float(x).value, ctypes.c_double: lambda x: ctypes.c_double(x).value}
+          ctypes.c_float: lambda x: ctypes.c_float(_value(x)).value, ctypes.c_double: lambda x: ctypes.c_double(_value(x)).value}
 
 
 def _through_ctypes(fn):

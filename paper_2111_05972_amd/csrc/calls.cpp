@@ -2,7 +2,7 @@
 // about 1 us here and 4 to 5 there (argument by argument, and a method call of Python's for each pointer), against 3 to 5 us of the shortest kernels.
 //
 // open(path) looks the entry points up in the library at `path`; the functions have their names and take their arguments by place.  A pointer is None, an address, or
-// anything with data_ptr() (a tensor) or cuda_stream (a stream), or what int() takes.  Numbers that do not fit their argument raise OverflowError.  Other threads run during a call.
+// anything with data_ptr() (a tensor) or cuda_stream (a stream), what int() takes or a ctypes pointer; numbers may be ctypes' too.  Numbers that do not fit their argument raise OverflowError.  Other threads run during a call.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 #include <dlfcn.h>
@@ -32,13 +32,22 @@ enum Index { ENTRY_POINTS(X) COUNT };
 void* table[COUNT];
 PyObject *data_ptr_name, *cuda_stream_name;
 PyTypeObject* stream_type;      // of the last object that had no data_ptr(): asked for its stream at once
+PyObject* ctypes_value;         // the class of ctypes' numbers and pointers
 
+// The value of one of those (a new reference), or null without an error.
+PyObject* value_of(PyObject* o) {
+    const int is = PyObject_IsInstance(o, ctypes_value);
+    if (is <= 0) { PyErr_Clear(); return nullptr; }
+    PyObject* value = PyObject_GetAttrString(o, "value");
+    if (!value) PyErr_Clear();
+    return value;
+}
 // What int() takes (numpy's integers), or the value of a ctypes pointer, None included.
 PyObject* other_number(PyObject* o) {
     PyObject* number = PyNumber_Long(o);
     if (number) return number;
     PyErr_Clear();
-    PyObject* value = PyObject_GetAttrString(o, "value");
+    PyObject* value = value_of(o);
     if (value) {
         number = value == Py_None ? PyLong_FromLong(0) : PyNumber_Index(value);
         Py_DECREF(value);
@@ -74,6 +83,21 @@ bool address(PyObject* o, void** out) {
     Py_DECREF(number);
     return !(*out == nullptr && PyErr_Occurred());
 }
+template <typename T> bool convert(PyObject* o, T* out);
+// A number that ctypes made, after the error that it is none.
+template <typename T> bool of_ctypes(PyObject* o, T* out) {
+    if (!PyErr_ExceptionMatches(PyExc_TypeError)) return false;
+    PyObject *type, *error, *trace;
+    PyErr_Fetch(&type, &error, &trace);
+    PyObject* value = value_of(o);
+    if (!value) { PyErr_Restore(type, error, trace); return false; }
+    Py_XDECREF(type);
+    Py_XDECREF(error);
+    Py_XDECREF(trace);
+    const bool ok = convert(value, out);
+    Py_DECREF(value);
+    return ok;
+}
 template <typename T> bool convert(PyObject* o, T* out) {
     if constexpr (std::is_pointer_v<T>) {
         void* p;
@@ -83,10 +107,10 @@ template <typename T> bool convert(PyObject* o, T* out) {
     } else if constexpr (std::is_floating_point_v<T>) {
         const double v = PyFloat_AsDouble(o);
         *out = (T)v;
-        return !(v == -1.0 && PyErr_Occurred());
+        return !(v == -1.0 && PyErr_Occurred()) || of_ctypes(o, out);
     } else {
         const long long v = PyLong_AsLongLong(o);
-        if (v == -1 && PyErr_Occurred()) return false;
+        if (v == -1 && PyErr_Occurred()) return of_ctypes(o, out);
         const bool fits = std::is_signed_v<T> ? v >= (long long)std::numeric_limits<T>::min() && v <= (long long)std::numeric_limits<T>::max() : v >= 0;
         if (!fits) { PyErr_SetString(PyExc_OverflowError, "a number does not fit its argument"); return false; }
         *out = (T)v;
@@ -142,6 +166,11 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", nullptr, -1, methods, nul
 }  // namespace
 
 PyMODINIT_FUNC PyInit__calls() {
+    PyObject* ctypes = PyImport_ImportModule("_ctypes");
+    if (!ctypes) return nullptr;
+    ctypes_value = PyObject_GetAttrString(ctypes, "_SimpleCData");
+    Py_DECREF(ctypes);
+    if (!ctypes_value) return nullptr;
     data_ptr_name = PyUnicode_InternFromString("data_ptr");
     cuda_stream_name = PyUnicode_InternFromString("cuda_stream");
     return data_ptr_name && cuda_stream_name ? PyModule_Create(&module) : nullptr;
