@@ -204,7 +204,8 @@ def _ptr(x):
 
 
 def _nbytes(x):
-    return getattr(x, "nbytes", None)
+    n = getattr(x, "nbytes", None)
+    return x.numel() * x.element_size() if n is None and hasattr(x, "numel") else n
 
 
 def _stream(stream):
