@@ -7,7 +7,7 @@ import paper_2111_05972_amd as pkg
 import test_abi_block_host as block
 import test_abi_packed_host as packed
 import test_abi_window_host as window
-import test_binding_ctypes_values as values
+import test_binding_ctypes_values as numbers
 import test_binding_pointers as pointers
 from paper_2111_05972_amd import binding
 
@@ -21,7 +21,7 @@ def without_module(monkeypatch):
 
 
 def _cases():
-    for m in (pointers, values, block, window, packed):
+    for m in (pointers, numbers, block, window, packed):
         for name in sorted(vars(m)):
             if not name.startswith("test_"):
                 continue
