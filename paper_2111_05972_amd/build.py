@@ -31,7 +31,8 @@ def _run(cmd, verbose):
 
 
 def build(verbose=False, extra=(), out=LIB):
-    """Every source is compiled, side by side, and linked into `out`; then the module that calls it."""
+    """Every source is compiled, side by side, and linked into `out`; then, for the package's own library, the module that calls it (without Python's headers
+    there is none, and ctypes calls the library)."""
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     with tempfile.TemporaryDirectory() as tmp:
         objects = [os.path.join(tmp, s + ".o") for s in SOURCES]
@@ -39,8 +40,9 @@ def build(verbose=False, extra=(), out=LIB):
         with ThreadPoolExecutor(JOBS) as pool:
             text = list(pool.map(compile_one, SOURCES, objects))
         text.append(_run([hipcc, "--offload-arch=gfx950", "-fPIC", "-shared"] + objects + ["-o", out], verbose))
-    text.append(_run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-I", sysconfig.get_paths()["include"], os.path.join(CSRC, "calls.cpp"),
-                      "-o", CALLS, "-ldl"], verbose))
+    include = sysconfig.get_paths()["include"]
+    if out == LIB and os.path.exists(os.path.join(include, "Python.h")):
+        text.append(_run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-I", include, os.path.join(CSRC, "calls.cpp"), "-o", CALLS, "-ldl"], verbose))
     return "\n".join(t for t in text if t)
 
 
