@@ -55,28 +55,33 @@ PyObject* other_number(PyObject* o) {
     if (!number) PyErr_Format(PyExc_TypeError, "a pointer is None, an address, a tensor or a stream, not %s", Py_TYPE(o)->tp_name);
     return number;
 }
+// Null without an error: it has no such attribute.
+PyObject* data_ptr_of(PyObject* o) {
+    PyObject* self[2] = {nullptr, o};
+    PyObject* number = PyObject_VectorcallMethod(data_ptr_name, self + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
+    if (!number && PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Clear();
+    return number;
+}
+PyObject* stream_of(PyObject* o) {
+    PyObject* number = PyObject_GetAttr(o, cuda_stream_name);
+    if (number && Py_TYPE(o) != stream_type) {
+        Py_INCREF(Py_TYPE(o));
+        Py_XSETREF(stream_type, Py_TYPE(o));
+    } else if (!number && PyErr_ExceptionMatches(PyExc_AttributeError)) {
+        PyErr_Clear();
+    }
+    return number;
+}
 bool address(PyObject* o, void** out) {
     if (o == Py_None) { *out = nullptr; return true; }
     PyObject* number = nullptr;
     if (PyLong_Check(o)) {
         number = Py_NewRef(o);
     } else {
-        if (Py_TYPE(o) != stream_type) {
-            PyObject* self[2] = {nullptr, o};
-            number = PyObject_VectorcallMethod(data_ptr_name, self + 1, 1 | PY_VECTORCALL_ARGUMENTS_OFFSET, nullptr);
-            if (!number && PyErr_ExceptionMatches(PyExc_AttributeError)) PyErr_Clear();
-            else if (!number) return false;
-        }
-        if (!number) {
-            number = PyObject_GetAttr(o, cuda_stream_name);
-            if (number) {
-                Py_INCREF(Py_TYPE(o));
-                Py_XSETREF(stream_type, Py_TYPE(o));
-            } else if (PyErr_ExceptionMatches(PyExc_AttributeError)) {
-                PyErr_Clear();
-                number = other_number(o);
-            }
-        }
+        const bool stream = Py_TYPE(o) == stream_type;
+        number = stream ? stream_of(o) : data_ptr_of(o);
+        if (!number && !PyErr_Occurred()) number = stream ? data_ptr_of(o) : stream_of(o);
+        if (!number && !PyErr_Occurred()) number = other_number(o);
         if (!number) return false;
     }
     *out = PyLong_AsVoidPtr(number);
