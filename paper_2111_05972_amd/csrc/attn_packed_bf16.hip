@@ -1247,11 +1247,13 @@ __global__ __launch_bounds__(WAVES4, DH <= 64 ? 3 : 2) void attn_packed_bwd_smal
 }
 // Above head size 64 by strips, of both sides and with a part of one for every sequence.  us, eight wavefronts and four, causal, heads of 128: 2500 tokens, 4 / 1 heads 34 and
 // 37 in 4 sequences (107 strips), 17 and 20 in 100 (295); 1500, 16 / 2, 43 and 48 in 4 (206), 24 and 21 in 100 (411); 1500, 8 / 8, 30 and 31 in 4, 22 and 20 in 20 (347); 2500,
-// 16 / 2, 68 and 59 in 4 (359), 40 and 32 in 100; from 500 strips on 2 to 28 % less, but for 3500, 16 / 2, in 20, 51.5 and 53.4.
+// 16 / 2, 68 and 59 in 4 (359), 40 and 32 in 100; from 500 strips on 2 to 28 % less, but for 3500, 16 / 2, in 20, 51.9 and 54.5, 6400, 10 / 2 heads of 80, in 64, 45.5 and 47.3, and 2910, 8 / 8 heads of 80, in 8, 33.1 and 34.3.
 // Up to 64, where two workgroups of eight wavefronts share a unit, by the tiles of rows that a strip of keys visits, as far as the host can tell (sequences of average length),
 // and strips.  8 heads of 64 unless said otherwise: 64 sequences of 64 tokens, causal 23.6 and 20.2, of 128 without a mask 37.0 and 31.9, 512 of 16 98.5 and 76.6, 8 of 2048,
 // causal 160 and 148, a window of 256, 8 / 4 heads, 16384 tokens 78.9 and 61.7, 8192 tokens (256 strips) 47.7 and 48.8; but a window of 1500 174 and 193, 8 sequences of 2048 of
 // 16 / 4 heads 325 and 349, one of 8192 276 and 316.
+// The average takes one long document among many short ones for short: 8000 tokens and 64 sequences of 3, 8 heads, causal 275 and 287, without a mask 513 and 476, 8129 and 63 of 1,
+// 16 / 4 heads, 616 and 590, 4000 and 100 of 9 99 and 94, 16000 and 200 of 16 1005 and 943.
 bool small_pays(const PackAttnArgs& a) {
     if (a.dh > 64) return 3 * (a.M * (a.nq + a.nkv) / PACK_BLK + a.sequences * a.nkv) >= 4 * compute_units();
     int64_t tokens = a.M / a.sequences;

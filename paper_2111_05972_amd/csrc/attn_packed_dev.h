@@ -71,7 +71,7 @@ __device__ __forceinline__ void strip_at(const PackParams<T>& p, int side, int i
     s.it = pack_items(p.plan, p.items[side])[n];
     set_strip(p, i - n * p.nkv, s);
 }
-// The keys of an item's tiles when tiles are left out: number `j` of them, counted without these, is key tile_key(j).
+// An item's tiles where some are left out: number `v`, counted without these, is tile tile_of(v) of the keys.
 template <typename T>
 __device__ __forceinline__ int tile_of(const PackParams<T>& p, const Strip<T>& s, int v) { return v * PACK_TILE >= p.sinks ? v + s.it.skip : v; }
 // Whether query q sees key j under a window.

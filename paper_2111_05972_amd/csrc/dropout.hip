@@ -4,12 +4,12 @@
 // seed.  So a slice draws its part of the tensor's mask whichever rank or launch works on it.
 //
 // An element is kept where its 16 bits are p 65536 (rounded) or more, and what is kept is multiplied by 65536 over the number of values that keep it:
-// the mean is exact, p is met to 2^-17.
+// the mean is exact, p is met to 2^-17; from 1 - 2^-17 on it is 1 - 2^-16, one value of 65536 that keeps.
 //
 // A workgroup has a strip of columns and some rows, a thread eight columns and every so many rows, four of them requested at once.  Sums
 // of dbias stay in registers until the workgroup's rows are through, are joined in LDS and left for row_sums.h: no atomics.
 // Bound by memory: 4096 rows of 12288 in bf16 with bias and residual, 302 MB in 55 us (5.5 TB/s); backward 201 MB in 40 (5.0) and 4.8 for the sums.  The generator's 20 products of
-// 32 x 32 bits for eight elements are half to two thirds of the vector units' time beside that.  4001 rows of 1280 in float 41 MB in 9.1 us and 9.6; 64 x 1024 3 us, a launch.
+// 32 x 32 bits for eight elements are half to two thirds of the vector units' time beside that.  4001 rows of 1280 in float 41 MB in 9.2 us and 10.0; 64 x 1024 3 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -63,8 +63,8 @@ __device__ __forceinline__ void drop8(float (&v)[8], const Words& q, unsigned th
 template <typename T, bool BIAS, bool RESID, bool SUMS>
 __global__ __launch_bounds__(DT) void dropout_kernel(DropParams p, const T* in, const T* bias, const T* resid, T* out, float* part, T* dbias) {
     constexpr int AHEAD = 4;
-    // Sums over rows.  Of float: four rows in 32 bits, from there on in 64, as a chain of a thread's rows (193 for 65536 rows of 12288) took dbias to ten times the
-    // error of one rounding.  Of bf16, which is off by up to 2^-8 of itself in the end: 32 bits.
+    // Sums over rows.  Of float: four rows in 32 bits, from there on in 64, as a chain of a thread's rows (193 for 65536 rows of 12288) took dbias to seven times the
+    // error of one rounding, so 1.5.  Of bf16, which is off by up to 2^-8 of itself in the end: 32 bits.
     using sum_t = std::conditional_t<sizeof(T) == 4, double, float>;
     __shared__ sum_t red[SUMS ? DT : 1][9];
     const int t = threadIdx.x, lane = t / p.cu, c = t - lane * p.cu, unit = blockIdx.x * p.cu + c;

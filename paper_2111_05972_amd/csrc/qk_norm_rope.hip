@@ -3,14 +3,15 @@
 // and backward, with g = turn back(dy) and everything worked out again from x:
 //   dx = rstd (g gamma - xh mean(g gamma xh)),  dgamma = sum of g xh over rows (and heads, where one row of weights is for all)
 //
-// Bound by memory, with vector work close behind (80 % of the vector units' time: widening, the norm and the rotation are about ten operations an element).  A
+// Bound by memory, with vector work close behind (72 % of the vector units' time in bf16, 58 in float: widening, the norm and the rotation are about ten operations an element;
+// reads of angles, 64 bytes from lane to lane with halves in bf16, keep LDS busy for 25 to 30 % of the cycles, 18 to 20 of them conflicts).  A
 // group of 1 to 64 neighbouring lanes has a head of a row, a lane two units of it: the two places of the pairs that it turns, or any two where a pair lies in
 // one unit; units of neighbouring lanes are neighbours (units of a lane side by side took 46.8 us instead of 34.1 in float).  A unit is 16 bytes, or 8 or 4 where the
 // halves of a rotation are no multiple of that; where these are not even, a head's values go through LDS to their partners.  Sums over a head take log2(lanes) steps
 // inside the wavefront.  Angles are one per (token, pair) for all heads, through LDS.  Backward: a group keeps its head over the rows of its workgroup, with gamma and the
 // sums of dgamma in registers; a workgroup's sums are joined in LDS and left for row_sums.h: no atomics.
 // 8192 tokens in bf16: 12 + 2 x 12 heads of 128, forward 151 MB in 25.6 us (5.9 TB/s), backward 201 MB in 39.7 (5.1) and 4.6 for the sums; 32 + 2 x 8 heads, weights for each head,
-// neighbouring pairs, 201 MB in 32.7 (6.2) and 285 MB in 50.8 (5.6).  3001 tokens in float, 32 + 2 x 8 heads of 80: 92 MB in 19 us (4.9) and 130 MB in 24.8 (5.3).  64 tokens: 4 us, a launch.
+// neighbouring pairs, 201 MB in 32.7 (6.2) and 285 MB in 50.8 (5.6).  3001 tokens in float, 32 + 2 x 8 heads of 80: 92 MB in 18.4 us (5.0) and 130 MB in 25.4 (5.1).  64 tokens: 4 us, a launch.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -172,7 +173,7 @@ struct Slot {
         }
     }
 };
-// The angles of tokens m0 .. m0 + n into LDS; past the last pair: as it is.
+// The angles of tokens m0 .. m0 + n into LDS; past the last pair none that counts.
 __device__ __forceinline__ void angles_of(const NormParams& p, float2* cs, int64_t m0, int n) {
     for (int i = threadIdx.x; i < n * p.angles; i += blockDim.x) {
         const int k = i / p.angles, f = i - k * p.angles;
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(MAX_THREADS, 4) void qk_norm_rope_bwd_kernel(NormPa
     };
     request(one, head_lane, row_lane, min(n, p.chunk));
     angles_of(p, cs, m0, min(n, p.chunk));
-    // sums of dgamma: of float in 64 bits (a chain of 400 rows in 32 took them to five times one rounding's error), of bf16, which is off by up to 2^-8 in the end, in 32
+    // sums of dgamma: of float in 64 bits (a chain of 400 rows in 32 took them to 5.5 times one rounding's error, so 2.9 at most, most of it the terms' own), of bf16, which is off by up to 2^-8 in the end, in 32
     using sum_t = std::conditional_t<sizeof(T) == 4, double, float>;
     sum_t d0[E], d1[E];
     auto leave = [&](float* to) __attribute__((always_inline)) {    // this thread's sums, and begin again
