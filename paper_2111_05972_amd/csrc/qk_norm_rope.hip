@@ -137,7 +137,8 @@ struct Slot {
             }
         } else if constexpr (MODE == NEIGHBOURS || MODE == NEIGHBOURS_SOME) {
             if (!has_a) return;
-            // SOME: a pair past `rot` is left alone, as an infinity turned by nothing would make NaN of its partner
+            // SOME: a pair past `rot` is left alone, as an infinity turned by nothing would make NaN of its partner (8192 tokens in bf16, 32 + 2 x 8 heads of 80 by 20, both
+            // directions, 67 -> 69 us; by branches instead of selections 70)
 #pragma unroll
             for (int e = 0; e < E / 2; ++e) {
                 const float2 r = w[a / 2 + e], s = w[b / 2 + e];
